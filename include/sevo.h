@@ -578,6 +578,158 @@ sevo_status sevo_moe_ffn(const sevo_model* m, int32_t layer, const void* h, int3
                          void* workspace, size_t workspace_bytes, void* stream);
 size_t sevo_moe_workspace_bytes(const sevo_model* m, int32_t n);
 
+/* ------------------------------------------------------------------ 8-bit layers
+ * A layer on 8-bit weights and activations: the norm writes 8-bit rows, the
+ * products read them, the SwiGLU between two products is quantised again.
+ *   codes   OCP e4m3 (4 exponent, 3 mantissa bits, largest value 448, no
+ *           infinity), one byte each; a value is code * scale of its block.
+ *   activations  codes row-major [m][k], k % 128 == 0; scales fp32 [k / 128][m]:
+ *           one for each row and 128 columns, block after block.
+ *   weights codes packed by sevo_pack_weight_fp8; scales fp32
+ *           [ceil(n_out / 128)][k / 128], row-major: one for each 128 x 128 block.
+ * Quantisation of a block y of 128 values: s = max(max |y| / 448, 2^-64), code =
+ * y / s rounded to nearest even.  A block that holds a NaN or an infinity gets
+ * the scale NaN and NaN codes, and so does every product that reads it. */
+#define SEVO_F32 0
+#define SEVO_BF16 1
+
+/* Residual add + RMSNorm with 8-bit output (sevo_add_rmsnorm for the products
+ * below):
+ *   x[r][:] += sum over s < n_partials of partials[s][r][:]  (in s order, each
+ *              added in fp32, written back; x unchanged when n_partials = 0)
+ *   y[r][:] = x[r][:] / sqrt(mean(x[r]^2) + eps) * gain     (fp32)
+ *   out, scales = y quantised;  out_bf16 = bf16(y) (NULL: not written; a MoE
+ *              layer's router reads it)
+ * x fp32 [rows][cols]; partials fp32 or bf16 (partial_type) [n_partials][rows]
+ * [cols], NULL when n_partials = 0; gain bf16 [cols]; out [rows][cols]; scales
+ * fp32 [cols / 128][rows]; out_bf16 row-major [rows][cols].  cols % 128 == 0, at
+ * most 32768; 0 <= n_partials <= 16.  A row's result does not depend on the
+ * other rows.  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP. */
+typedef struct {
+  int32_t rows, cols, n_partials, partial_type;
+  float eps;
+  float* x;
+  const void* partials;
+  const void* gain;
+  void* out;
+  float* scales;
+  void* out_bf16;
+} sevo_add_rmsnorm_fp8_args;
+
+sevo_status sevo_add_rmsnorm_fp8(const sevo_add_rmsnorm_fp8_args* a, void* stream);
+
+/* bf16 rows to 8 bits: swiglu 0: y = x, x [m][k] (attention outputs before the
+ * output projection); swiglu 1: y = silu(x[:, :k]) * x[:, k:], x [m][2 k] (a
+ * gate/up product before the down projection), in fp32.  ldx: row stride of x in
+ * elements, a multiple of 8, at least k (2 k); out [m][k]; scales [k / 128][m].
+ * k % 128 == 0.  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP. */
+sevo_status sevo_quantize_fp8(const void* x, int64_t ldx, int32_t m, int32_t k, int32_t swiglu,
+                              void* out, float* scales, void* stream);
+
+/* Row-major codes [n_out][k] (src) -> the packed 8-bit layout (dst, a separate
+ * buffer of n_out k bytes): superblocks of 64 rows, in them per 128-column step
+ * four fragments of 16 rows (2 KB); element (r, c) at
+ *   ((r/64 * k/128 + c/128) * 4 + (r/16) % 4) * 2048
+ *   + (16 ((c/16) % 8) + r % 16) * 16 + c % 16.
+ * n_out % 64 == 0, k % 128 == 0.  The matrices of E experts are packed in one
+ * call of E n_out rows.  A one-time preparation of model weights. */
+sevo_status sevo_pack_weight_fp8(const void* src, void* dst, int64_t n_out, int32_t k,
+                                 void* stream);
+
+/* Y = X W^T of 8-bit operands:
+ *   Y[r][c] = sum over blocks b of x_scales[b][r] w_scales[c / 128][b]
+ *             * (sum over k in b of X[r][k] W[c][k]), added in fp32.
+ * out_type SEVO_F32: out fp32, the inner sums exact to fp32 rounding (for the
+ * norm + RoPE + append and the sampler, which read fp32); SEVO_BF16: out bf16 (for
+ * the partials of sevo_add_rmsnorm_fp8 and for sevo_quantize_fp8), the inner
+ * sums within 2e-5 of the block's largest, by the faster 8-bit matrix instructions.
+ *   x [m][k], row stride ldx bytes (>= k, a multiple of 16); x_scales row stride
+ *   lds (>= m); w packed; out row stride ldo elements (>= n_out, a multiple of 4).
+ * n_out % 64 == 0, k % 128 == 0, k < 2^24.  The workspace is scratch of
+ * sevo_linear_fp8_workspace_bytes (0: may be NULL): calls that may overlap in time each need
+ * their own.  The same call gives the same bits; the bits of a row may depend on
+ * m (its plan).  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */
+typedef struct {
+  int32_t m, n_out, k, out_type;
+  int64_t ldx, lds, ldo;
+  const void* x;
+  const float* x_scales;
+  const void* w;
+  const float* w_scales;
+  void* out;
+  void* workspace;
+  size_t workspace_bytes;
+} sevo_linear_fp8_args;
+
+sevo_status sevo_linear_fp8(const sevo_linear_fp8_args* a, void* stream);
+size_t sevo_linear_fp8_workspace_bytes(int32_t m, int32_t n_out, int32_t k);
+
+/* Routing of n tokens from router logits fp32 [n][n_experts] (row stride ld):
+ *   score   p = softmax(logits) (SEVO_ROUTE_SOFTMAX) or sigmoid(logits)
+ *           (SEVO_ROUTE_SIGMOID), in float64
+ *   choice  c = p + bias (bias fp32 [n_experts], NULL: none): the balance bias
+ *           acts on the choice, not on the weights
+ *   groups  the experts in n_groups equal runs; the top_groups with the largest
+ *           sum of their group_best (1 or 2) largest c stay
+ *   experts the top_k largest c of those, largest first
+ *   weights p of each; renormalise 1: / (their sum + 1e-20); then * scaling
+ * Ties go to the lower group and the lower expert; a NaN is chosen after every
+ * other value, so top_k distinct experts always come back.
+ *   out_experts int32 [n][top_k]; out_weights fp32 [n][top_k].
+ * n_experts 1..256; top_k 1..16; n_experts % n_groups == 0, n_groups <= 64,
+ * group_best <= n_experts / n_groups, top_k <= top_groups n_experts / n_groups.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP. */
+#define SEVO_ROUTE_SOFTMAX 0
+#define SEVO_ROUTE_SIGMOID 1
+typedef struct {
+  int32_t n, n_experts, top_k, score, n_groups, top_groups, group_best, renormalise;
+  float scaling;
+  int64_t ld;
+  const float* logits;
+  const float* bias;
+  int32_t* out_experts;
+  float* out_weights;
+} sevo_moe_route_args;
+
+sevo_status sevo_moe_route(const sevo_moe_route_args* a, void* stream);
+
+/* The entry lists of a routing, which the grouped products read: entry t top_k +
+ * j (token t, slot j) goes to the list of experts[t][j], each list in entry
+ * order.  An id outside [0, n_experts) joins no list: products leave its output
+ * rows as they were.  experts int32 [n][top_k]; lists: a caller's buffer of
+ * sevo_moe_lists_bytes, its contents private.  n top_k <= 2^30, n_experts 1..256,
+ * top_k 1..16.  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */
+sevo_status sevo_moe_lists(const int32_t* experts, int32_t n, int32_t top_k, int32_t n_experts,
+                           void* lists, size_t lists_bytes, void* stream);
+size_t sevo_moe_lists_bytes(int32_t n, int32_t top_k, int32_t n_experts);
+
+/* The product of sevo_linear_fp8 with the weights of each entry's expert, out
+ * bf16:
+ *   down 0 (gate/up): x [n][k], a row per token;
+ *     out [n top_k][n_out]: out[t top_k + j] = x[t] W_e^T,  e = experts[t][j]
+ *   down 1: x [n top_k][k], a row per entry;
+ *     out [top_k][n][n_out]: out[j][t] = weights[t][j] * x[t top_k + j] W_e^T,
+ *     the partials that sevo_add_rmsnorm_fp8 adds in slot order
+ *   w [n_experts][n_out][k], each packed; w_scales [n_experts]
+ *   [ceil(n_out / 128)][k / 128]; weights fp32 [n][top_k] (down only); lists of
+ *   sevo_moe_lists for the same n, top_k and n_experts.
+ * ldx, lds as in sevo_linear_fp8; n_out % 64 == 0, k % 128 == 0; x and x_scales
+ * each below 2^31 bytes (UNSUPPORTED beyond: fewer tokens a call).
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP. */
+typedef struct {
+  int32_t n, top_k, n_experts, n_out, k, down;
+  int64_t ldx, lds;
+  const void* x;
+  const float* x_scales;
+  const void* w;
+  const float* w_scales;
+  const float* weights;
+  const void* lists;
+  void* out;
+} sevo_moe_linear_fp8_args;
+
+sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void* stream);
+
 /* ------------------------------------------------------------------ utilities */
 
 /* Streaming-read microbenchmark (measurement tooling, not part of the decode

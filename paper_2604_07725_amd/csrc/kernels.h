@@ -219,4 +219,77 @@ hipError_t launch_group_confidence(const float* conf_sum, const int32_t* counts,
                                    const int32_t* groups, int n_groups, int K, float* out,
                                    hipStream_t st);
 
+// ---- quant8.hip: 8-bit activations (e4m3 codes row-major, scales [cols / 128][rows])
+struct AddNormFp8Args {
+  int rows, cols, n_partials, partials_bf16;
+  float eps;
+  float* x;
+  const void* partials;  // [n_partials][rows][cols]
+  const bf16_t* gain;
+  uint8_t* out;
+  float* scales;
+  bf16_t* out_bf16;      // the normed rows in bf16 too (null: none)
+};
+hipError_t launch_add_rmsnorm_fp8(const AddNormFp8Args& a, hipStream_t st);
+// x [m][k] (swiglu: [m][2 k], gate columns then up) with row stride ldx
+hipError_t launch_quantize_fp8(const bf16_t* x, int64_t ldx, int m, int k, int swiglu, uint8_t* out,
+                               float* scales, hipStream_t st);
+// row-major codes [n][k] -> packed: superblocks of 64 rows, per 128-column step
+// four fragments of 16 rows (2 KB), each 128 runs of 16 bytes, run 16 (c / 16 % 8) + r % 16
+hipError_t launch_pack_weight_fp8(const uint8_t* src, uint8_t* dst, int64_t n, int k,
+                                  hipStream_t st);
+
+// ---- linear8.hip: block-scaled 8-bit products
+struct Linear8Args {
+  int m, n_out, k;
+  const uint8_t* x;  // [m][k], row stride ldx
+  int64_t ldx;
+  const float* xs;   // [k / 128][m], row stride lds
+  int64_t lds;
+  const uint8_t* w;  // packed [n_out][k]
+  const float* ws;   // [ceil(n_out / 128)][k / 128]
+  void* out;         // [m][n_out], row stride ldo
+  int64_t ldo;
+  int out_bf16;      // else fp32
+};
+struct Linear8Plan {
+  int splits = 1;    // K splits
+  int kb_chunk = 0;  // 128-column blocks per split
+  int rb = 4, mb = 1;
+};
+Linear8Plan plan_linear8(int m, int n_out, int k);
+size_t linear8_workspace_bytes(int m, int n_out, const Linear8Plan& p);
+hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* workspace,
+                          hipStream_t st);
+struct Moe8Args {
+  int n, top_k, n_experts, n_out, k;
+  int down;              // 0: x row = token, out row = entry; 1: x row = entry, out row = slot n + token
+  const uint8_t* x;
+  int64_t ldx;
+  const float* xs;
+  int64_t lds;
+  const uint8_t* w;      // [E][n_out][k], each packed
+  const float* ws;       // [E][ceil(n_out / 128)][k / 128]
+  const float* weights;  // [n][top_k] (down)
+  const int32_t* offsets;   // [E + 1]
+  const int32_t* assign;    // entries t top_k + slot, expert-major
+  const int32_t* tile_off;  // [E + 1] first tile of each expert
+  bf16_t* out;
+};
+// entries per tile of tile_off
+int moe8_tile_rows(int64_t entries, int n_experts);
+hipError_t launch_moe8(const Moe8Args& a, hipStream_t st);
+
+// ---- moe_route.hip
+struct MoeRouteArgs {
+  int n, n_experts, top_k, sigmoid, n_groups, top_groups, group_best, renormalise;
+  float scaling;
+  int64_t ld;
+  const float* logits;
+  const float* bias;
+  int32_t* out_experts;
+  float* out_weights;
+};
+hipError_t launch_moe_route8(const MoeRouteArgs& a, hipStream_t st);
+
 }  // namespace sevo

@@ -183,17 +183,6 @@ hipError_t launch_pack_kv(const bf16_t* k_src, const bf16_t* v_src, size_t tiles
   return hipGetLastError();
 }
 
-// Workgroups are dealt to the 8 XCDs round robin.  Workgroup b of n takes row
-// xcd_row(b, n), so that 16 consecutive rows -- a block of the tiled layout, a
-// KV page -- are written through one XCD's L2: dealt row by row, eight L2s each
-// held (and wrote back) a part of every line (8192 x 4096
-// norms 77 -> 56 us, 8146 tokens of RoPE and append 88 -> 82).
-__device__ __forceinline__ int xcd_row(int b, int n) {
-  if (b >= (n & ~127)) return b;
-  const int j = b >> 3;
-  return ((j >> 4) * 8 + (b & 7)) * 16 + (j & 15);
-}
-
 // One wave per (candidate, head); the QKV projection given as the fp32
 // split-K partials of the GEMM, summed here in split order.
 __global__ __launch_bounds__(64) void qk_norm_rope_append_kernel(RopeAppendArgs a) {

@@ -1427,6 +1427,231 @@ SEVO_API sevo_status sevo_prefill_confidence(sevo_model* m, const sevo_prefill_a
   return e == hipSuccess ? SEVO_OK : hip_fail(e, "prefill (sequence confidence)");
 }
 
+// ------------------------------------------------------------------ 8-bit layers
+namespace {
+
+bool bad_ptr(const void* p) { return !p || !aligned16(p); }
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+// shape rules shared by the products
+sevo_status check_fp8_product(int n_out, int k, int64_t ldx) {
+  if (n_out < 1 || k < 1) return fail(SEVO_ERR_INVALID_ARGUMENT, "n_out %d, k %d", n_out, k);
+  if (n_out % 64 || k % 128 || k >= 1 << 24)
+    return fail(SEVO_ERR_UNSUPPORTED, "n_out %d must be a multiple of 64 and k %d of 128 below 2^24",
+                n_out, k);
+  if (ldx < k || ldx % 16 || ldx >= 1 << 26)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "ldx %lld must be a multiple of 16 in [k, 2^26)",
+                (long long)ldx);
+  return SEVO_OK;
+}
+
+sevo_status check_moe_shape(int n, int top_k, int n_experts) {
+  if (n_experts < 1 || n_experts > 256 || top_k < 1 || top_k > 16 || top_k > n_experts)
+    return fail(SEVO_ERR_UNSUPPORTED, "n_experts %d (1..256), top_k %d (1..16, at most n_experts)",
+                n_experts, top_k);
+  if (n < 0 || (int64_t)n * top_k > kMoeMaxEntries)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "n %d outside [0, 2^30 / top_k]", n);
+  return SEVO_OK;
+}
+
+// the parts of a lists buffer, in int32
+struct ListsLayout {
+  size_t offsets, tiles, assign, scratch, total;
+};
+ListsLayout lists_layout(int n, int top_k, int n_experts) {
+  const size_t nk = (size_t)n * top_k;
+  ListsLayout L;
+  L.offsets = 0;
+  L.tiles = round_up(n_experts + 1, 64);
+  L.assign = 2 * L.tiles;
+  L.scratch = L.assign + round_up(nk, 64);
+  L.total = L.scratch + round_up(sevo::moe_plan_scratch_bytes((int)nk, n_experts) / 4, 64);
+  return L;
+}
+
+}  // namespace
+
+SEVO_API sevo_status sevo_add_rmsnorm_fp8(const sevo_add_rmsnorm_fp8_args* a, void* stream) {
+  if (!a) return fail(SEVO_ERR_INVALID_ARGUMENT, "null args");
+  if (a->rows < 0 || a->cols < 1 || a->n_partials < 0 || a->n_partials > 16 || !(a->eps > 0.f))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "rows %d, cols %d, n_partials %d (0..16), eps %g",
+                a->rows, a->cols, a->n_partials, a->eps);
+  if (a->partial_type != SEVO_F32 && a->partial_type != SEVO_BF16)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "partial_type %d", a->partial_type);
+  if (a->cols % 128 || a->cols > 32768)
+    return fail(SEVO_ERR_UNSUPPORTED, "cols %d must be a multiple of 128, at most 32768", a->cols);
+  if (a->rows == 0) return SEVO_OK;
+  if (bad_ptr(a->x) || bad_ptr(a->gain) || bad_ptr(a->out) || bad_ptr(a->scales) ||
+      (a->n_partials > 0 && bad_ptr(a->partials)) || (a->out_bf16 && !aligned16(a->out_bf16)))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  sevo::AddNormFp8Args n;
+  n.rows = a->rows; n.cols = a->cols; n.n_partials = a->n_partials;
+  n.partials_bf16 = a->partial_type == SEVO_BF16;
+  n.eps = a->eps; n.x = a->x; n.partials = a->partials;
+  n.gain = static_cast<const sevo::bf16_t*>(a->gain);
+  n.out = static_cast<uint8_t*>(a->out); n.scales = a->scales;
+  n.out_bf16 = static_cast<sevo::bf16_t*>(a->out_bf16);
+  hipError_t e = sevo::launch_add_rmsnorm_fp8(n, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_add_rmsnorm_fp8");
+}
+
+SEVO_API sevo_status sevo_quantize_fp8(const void* x, int64_t ldx, int32_t m, int32_t k,
+                                       int32_t swiglu, void* out, float* scales, void* stream) {
+  if (m < 0 || k < 1 || (swiglu != 0 && swiglu != 1))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "m %d, k %d, swiglu %d", m, k, swiglu);
+  if (k % 128 || k >= 1 << 24)
+    return fail(SEVO_ERR_UNSUPPORTED, "k %d must be a multiple of 128 below 2^24", k);
+  if (ldx < (int64_t)k * (1 + swiglu) || ldx % 8)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "ldx %lld must be a multiple of 8, at least the row",
+                (long long)ldx);
+  if (m == 0) return SEVO_OK;
+  if (bad_ptr(x) || bad_ptr(out) || bad_ptr(scales))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  hipError_t e = sevo::launch_quantize_fp8(static_cast<const sevo::bf16_t*>(x), ldx, m, k, swiglu,
+                                           static_cast<uint8_t*>(out), scales,
+                                           static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_quantize_fp8");
+}
+
+SEVO_API sevo_status sevo_pack_weight_fp8(const void* src, void* dst, int64_t n_out, int32_t k,
+                                          void* stream) {
+  if (n_out < 0 || k < 1) return fail(SEVO_ERR_INVALID_ARGUMENT, "negative size");
+  if (n_out % 64 || k % 128 || k >= 1 << 24 || n_out > ((int64_t)1 << 40) / k)
+    return fail(SEVO_ERR_UNSUPPORTED,
+                "n_out %lld must be a multiple of 64 and k %d of 128 below 2^24 (2^40 codes at most)",
+                (long long)n_out, k);
+  if (n_out == 0) return SEVO_OK;
+  if (bad_ptr(src) || bad_ptr(dst) || overlap(src, (size_t)n_out * k, dst, (size_t)n_out * k))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null, misaligned or overlapping buffer");
+  hipError_t e = sevo::launch_pack_weight_fp8(static_cast<const uint8_t*>(src),
+                                              static_cast<uint8_t*>(dst), n_out, k,
+                                              static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_pack_weight_fp8");
+}
+
+SEVO_API size_t sevo_linear_fp8_workspace_bytes(int32_t m, int32_t n_out, int32_t k) {
+  if (m <= 0 || n_out <= 0 || k <= 0 || n_out % 64 || k % 128 || k >= 1 << 24) return 0;
+  return sevo::linear8_workspace_bytes(m, n_out, sevo::plan_linear8(m, n_out, k));
+}
+
+SEVO_API sevo_status sevo_linear_fp8(const sevo_linear_fp8_args* a, void* stream) {
+  if (!a) return fail(SEVO_ERR_INVALID_ARGUMENT, "null args");
+  if (a->m < 0 || (a->out_type != SEVO_F32 && a->out_type != SEVO_BF16))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "m %d, out_type %d", a->m, a->out_type);
+  if (sevo_status s = check_fp8_product(a->n_out, a->k, a->ldx)) return s;
+  if (a->lds < a->m || a->lds >= 1 << 29)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "lds %lld outside [m, 2^29)", (long long)a->lds);
+  if (a->ldo < a->n_out || a->ldo % 4)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "ldo %lld must be a multiple of 4, at least n_out",
+                (long long)a->ldo);
+  if (a->m == 0) return SEVO_OK;
+  if (bad_ptr(a->x) || !a->x_scales || bad_ptr(a->w) || !a->w_scales || bad_ptr(a->out))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  const sevo::Linear8Plan p = sevo::plan_linear8(a->m, a->n_out, a->k);
+  const size_t need = sevo::linear8_workspace_bytes(a->m, a->n_out, p);
+  if (need > 0) {
+    if (bad_ptr(a->workspace)) return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned workspace");
+    if (a->workspace_bytes < need)
+      return fail(SEVO_ERR_WORKSPACE_TOO_SMALL, "product needs %zu workspace bytes, got %zu", need,
+                  a->workspace_bytes);
+  }
+  sevo::Linear8Args l;
+  l.m = a->m; l.n_out = a->n_out; l.k = a->k;
+  l.x = static_cast<const uint8_t*>(a->x); l.ldx = a->ldx;
+  l.xs = a->x_scales; l.lds = a->lds;
+  l.w = static_cast<const uint8_t*>(a->w); l.ws = a->w_scales;
+  l.out = a->out; l.ldo = a->ldo; l.out_bf16 = a->out_type == SEVO_BF16;
+  hipError_t e = sevo::launch_linear8(l, p, static_cast<float*>(a->workspace),
+                                      static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_linear_fp8");
+}
+
+SEVO_API sevo_status sevo_moe_route(const sevo_moe_route_args* a, void* stream) {
+  if (!a) return fail(SEVO_ERR_INVALID_ARGUMENT, "null args");
+  if (sevo_status s = check_moe_shape(a->n, a->top_k, a->n_experts)) return s;
+  if ((a->score != SEVO_ROUTE_SOFTMAX && a->score != SEVO_ROUTE_SIGMOID) ||
+      (a->renormalise != 0 && a->renormalise != 1) || !std::isfinite(a->scaling))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "score %d, renormalise %d, scaling %g", a->score,
+                a->renormalise, a->scaling);
+  if (a->n_groups < 1 || a->n_groups > 64 || a->n_experts % a->n_groups || a->top_groups < 1 ||
+      a->top_groups > a->n_groups || a->group_best < 1 || a->group_best > 2 ||
+      a->group_best > a->n_experts / a->n_groups ||
+      a->top_k > a->top_groups * (a->n_experts / a->n_groups))
+    return fail(SEVO_ERR_INVALID_ARGUMENT,
+                "n_groups %d, top_groups %d, group_best %d do not fit %d experts, %d a token",
+                a->n_groups, a->top_groups, a->group_best, a->n_experts, a->top_k);
+  if (a->ld < a->n_experts) return fail(SEVO_ERR_INVALID_ARGUMENT, "ld %lld", (long long)a->ld);
+  if (a->n == 0) return SEVO_OK;
+  if (!a->logits || !a->out_experts || !a->out_weights)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null pointer");
+  sevo::MoeRouteArgs r;
+  r.n = a->n; r.n_experts = a->n_experts; r.top_k = a->top_k;
+  r.sigmoid = a->score == SEVO_ROUTE_SIGMOID;
+  r.n_groups = a->n_groups; r.top_groups = a->top_groups; r.group_best = a->group_best;
+  r.renormalise = a->renormalise; r.scaling = a->scaling; r.ld = a->ld;
+  r.logits = a->logits; r.bias = a->bias;
+  r.out_experts = a->out_experts; r.out_weights = a->out_weights;
+  hipError_t e = sevo::launch_moe_route8(r, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_moe_route");
+}
+
+SEVO_API size_t sevo_moe_lists_bytes(int32_t n, int32_t top_k, int32_t n_experts) {
+  if (n <= 0 || top_k < 1 || top_k > 16 || n_experts < 1 || n_experts > 256 ||
+      (int64_t)n * top_k > kMoeMaxEntries)
+    return 0;
+  return lists_layout(n, top_k, n_experts).total * 4;
+}
+
+SEVO_API sevo_status sevo_moe_lists(const int32_t* experts, int32_t n, int32_t top_k,
+                                    int32_t n_experts, void* lists, size_t lists_bytes,
+                                    void* stream) {
+  if (sevo_status s = check_moe_shape(n, top_k, n_experts)) return s;
+  if (n == 0) return SEVO_OK;
+  if (!experts || bad_ptr(lists)) return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  const ListsLayout L = lists_layout(n, top_k, n_experts);
+  if (lists_bytes < L.total * 4)
+    return fail(SEVO_ERR_WORKSPACE_TOO_SMALL, "lists need %zu bytes, got %zu", L.total * 4,
+                lists_bytes);
+  int32_t* p = static_cast<int32_t*>(lists);
+  hipError_t e = sevo::launch_moe_plan(experts, n * top_k, n_experts, p + L.offsets, p + L.assign,
+                                       static_cast<hipStream_t>(stream), p + L.tiles,
+                                       sevo::moe8_tile_rows((int64_t)n * top_k, n_experts),
+                                       p + L.scratch);
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_moe_lists");
+}
+
+SEVO_API sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void* stream) {
+  if (!a) return fail(SEVO_ERR_INVALID_ARGUMENT, "null args");
+  if (sevo_status s = check_moe_shape(a->n, a->top_k, a->n_experts)) return s;
+  if (a->down != 0 && a->down != 1) return fail(SEVO_ERR_INVALID_ARGUMENT, "down %d", a->down);
+  if (sevo_status s = check_fp8_product(a->n_out, a->k, a->ldx)) return s;
+  const int64_t rows = a->down ? (int64_t)a->n * a->top_k : a->n;
+  if (a->lds < rows) return fail(SEVO_ERR_INVALID_ARGUMENT, "lds %lld < rows", (long long)a->lds);
+  if (a->n == 0) return SEVO_OK;
+  if (rows * a->ldx >= (int64_t)1 << 31 || a->lds >= ((int64_t)1 << 31) / 4 / (a->k / 128))
+    return fail(SEVO_ERR_UNSUPPORTED, "x or x_scales of 2^31 bytes or more: fewer tokens a call");
+  if (bad_ptr(a->x) || !a->x_scales || bad_ptr(a->w) || !a->w_scales || bad_ptr(a->lists) ||
+      bad_ptr(a->out) || (a->down && !a->weights))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  const ListsLayout L = lists_layout(a->n, a->top_k, a->n_experts);
+  const int32_t* p = static_cast<const int32_t*>(a->lists);
+  sevo::Moe8Args m;
+  m.n = a->n; m.top_k = a->top_k; m.n_experts = a->n_experts; m.n_out = a->n_out; m.k = a->k;
+  m.down = a->down;
+  m.x = static_cast<const uint8_t*>(a->x); m.ldx = a->ldx;
+  m.xs = a->x_scales; m.lds = a->lds;
+  m.w = static_cast<const uint8_t*>(a->w); m.ws = a->w_scales;
+  m.weights = a->weights;
+  m.offsets = p + L.offsets; m.assign = p + L.assign; m.tile_off = p + L.tiles;
+  m.out = static_cast<sevo::bf16_t*>(a->out);
+  hipError_t e = sevo::launch_moe8(m, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_moe_linear_fp8");
+}
+
 // ------------------------------------------------------------------ utilities
 SEVO_API sevo_status sevo_fill_normal_bf16(void* dst, int64_t count, uint64_t key, int64_t offset,
                                            float mul, float add, int32_t use_add, void* stream) {

@@ -24,6 +24,9 @@ OK, INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY, HIP, BAD_
 LINEAR_STORE, LINEAR_ADD, LINEAR_SWIGLU = 0, 1, 2
 LINEAR_X_TILED, LINEAR_OUT_TILED = 1, 2
 PACK_PLAIN, PACK_GATE_UP = 0, 1
+F32, BF16 = 0, 1                           # SEVO_F32, SEVO_BF16
+ROUTE_SOFTMAX, ROUTE_SIGMOID = 0, 1
+SCALE_BLOCK = 128                          # columns (weights: rows and columns) of an 8-bit scale
 # projection weights held in the packed layout, and how each is packed
 PACKED_WEIGHTS = {"w_qkv": PACK_PLAIN, "w_o": PACK_PLAIN, "w_gate_up": PACK_GATE_UP,
                   "w_down": PACK_PLAIN, "lm_head": PACK_PLAIN, "w_router": PACK_PLAIN,
@@ -105,6 +108,31 @@ class LinearArgs(C.Structure):
                 ("workspace", vp), ("workspace_bytes", sz)]
 
 
+class AddRmsnormFp8Args(C.Structure):
+    _fields_ = [("rows", i32), ("cols", i32), ("n_partials", i32), ("partial_type", i32),
+                ("eps", f32), ("x", vp), ("partials", vp), ("gain", vp), ("out", vp),
+                ("scales", vp), ("out_bf16", vp)]
+
+
+class LinearFp8Args(C.Structure):
+    _fields_ = [("m", i32), ("n_out", i32), ("k", i32), ("out_type", i32), ("ldx", i64),
+                ("lds", i64), ("ldo", i64), ("x", vp), ("x_scales", vp), ("w", vp),
+                ("w_scales", vp), ("out", vp), ("workspace", vp), ("workspace_bytes", sz)]
+
+
+class MoeRouteArgs(C.Structure):
+    _fields_ = [("n", i32), ("n_experts", i32), ("top_k", i32), ("score", i32),
+                ("n_groups", i32), ("top_groups", i32), ("group_best", i32),
+                ("renormalise", i32), ("scaling", f32), ("ld", i64), ("logits", vp),
+                ("bias", vp), ("out_experts", vp), ("out_weights", vp)]
+
+
+class MoeLinearFp8Args(C.Structure):
+    _fields_ = [("n", i32), ("top_k", i32), ("n_experts", i32), ("n_out", i32), ("k", i32),
+                ("down", i32), ("ldx", i64), ("lds", i64), ("x", vp), ("x_scales", vp),
+                ("w", vp), ("w_scales", vp), ("weights", vp), ("lists", vp), ("out", vp)]
+
+
 _SIGS = {
     "sevo_status_string": ([i32], C.c_char_p),
     "sevo_last_error": ([], C.c_char_p),
@@ -137,6 +165,15 @@ _SIGS = {
     "sevo_qk_norm_rope_append": ([vp, i32, vp, i32, vp, vp, i32, i64, vp, vp, vp], i32),
     "sevo_fill_normal_bf16": ([vp, i64, u64, i64, f32, f32, i32, vp], i32),
     "sevo_validate_paging": ([vp, vp, i32, i32, i64, vp], i32),
+    "sevo_add_rmsnorm_fp8": ([C.POINTER(AddRmsnormFp8Args), vp], i32),
+    "sevo_quantize_fp8": ([vp, i64, i32, i32, i32, vp, vp, vp], i32),
+    "sevo_pack_weight_fp8": ([vp, vp, i64, i32, vp], i32),
+    "sevo_linear_fp8": ([C.POINTER(LinearFp8Args), vp], i32),
+    "sevo_linear_fp8_workspace_bytes": ([i32, i32, i32], sz),
+    "sevo_moe_route": ([C.POINTER(MoeRouteArgs), vp], i32),
+    "sevo_moe_lists": ([vp, i32, i32, i32, vp, sz, vp], i32),
+    "sevo_moe_lists_bytes": ([i32, i32, i32], sz),
+    "sevo_moe_linear_fp8": ([C.POINTER(MoeLinearFp8Args), vp], i32),
     "sevo_profile_begin": ([i32, C.c_uint32], i32),
     "sevo_profile_end": ([C.POINTER(f32), C.POINTER(i32)], i32),
 }
@@ -574,6 +611,223 @@ def sevo_moe_ffn(model: Model, layer: int, h_tiled, n: int, stream=None, partial
     _check(lib().sevo_moe_ffn(model.handle, int(layer), _p(h_tiled), int(n), _p(ex), _p(wt),
                               _p(part), _p(ws), ws.numel(), _stream(stream)))
     return ex, wt, part
+
+
+# ------------------------------------------------------------------ 8-bit layers
+def _need(name, t, dtype, shape=None, device=None, contiguous=True):
+    """Raises ValueError unless t is a tensor of this type, shape and device, rows
+    contiguous (``contiguous``: all of it)."""
+    types = dtype if isinstance(dtype, tuple) else (dtype,)
+    if t.dtype not in types:
+        raise ValueError(f"{name}: {t.dtype}, expected {' or '.join(map(str, types))}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    if not contiguous and t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+
+
+def _ld(t):
+    """Row stride of a 2-d tensor (one row has none of its own)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _call(name, device, stream, *args):
+    """The C call on the tensors' device, by default on its current stream."""
+    with torch.cuda.device(device):
+        _check(getattr(lib(), name)(*args, _stream(stream)))
+
+
+def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16=None,
+                         stream=None):
+    """x fp32 [rows, cols] += the partials [S, rows, cols] (fp32 or bf16, in s
+    order; None for none), in place; returns RMSNorm(x) * gain in 8 bits: codes
+    float8_e4m3fn [rows, cols] and scales fp32 [cols / 128, rows].  ``out_bf16``
+    (bf16 [rows, cols]) receives the normed rows too."""
+    rows, cols = x.shape
+    dev = x.device
+    _need("x", x, torch.float32)
+    _need("gain", gain, torch.bfloat16, (cols,), dev)
+    S = 0
+    if partials is not None and partials.shape[0] > 0:
+        S = partials.shape[0]
+        _need("partials", partials, (torch.float32, torch.bfloat16), (S, rows, cols), dev)
+    if out is None:
+        out = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=dev)
+    if scales is None:
+        scales = torch.empty(cols // SCALE_BLOCK, rows, dtype=torch.float32, device=dev)
+    _need("out", out, torch.float8_e4m3fn, (rows, cols), dev)
+    _need("scales", scales, torch.float32, (cols // SCALE_BLOCK, rows), dev)
+    if out_bf16 is not None:
+        _need("out_bf16", out_bf16, torch.bfloat16, (rows, cols), dev)
+    a = AddRmsnormFp8Args(
+        rows=rows, cols=cols, n_partials=S,
+        partial_type=BF16 if S and partials.dtype == torch.bfloat16 else F32, eps=float(eps),
+        x=_p(x), partials=_p(partials) if S else None, gain=_p(gain), out=_p(out),
+        scales=_p(scales), out_bf16=_p(out_bf16))
+    _call("sevo_add_rmsnorm_fp8", dev, stream, C.byref(a))
+    return out, scales
+
+
+def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
+    """bf16 rows [m, k] (row stride from the tensor) to codes float8_e4m3fn [m, k]
+    and scales fp32 [k / 128, m]; with ``swiglu`` of silu(gate) * up, x [m, 2 k]
+    holding the gate columns, then the up columns."""
+    _need("x", x, torch.bfloat16, contiguous=False)
+    m, k = x.shape
+    if swiglu:
+        if k % 2:
+            raise ValueError("x: an odd number of gate and up columns")
+        k //= 2
+    dev = x.device
+    if out is None:
+        out = torch.empty(m, k, dtype=torch.float8_e4m3fn, device=dev)
+    if scales is None:
+        scales = torch.empty(k // SCALE_BLOCK, m, dtype=torch.float32, device=dev)
+    _need("out", out, torch.float8_e4m3fn, (m, k), dev)
+    _need("scales", scales, torch.float32, (k // SCALE_BLOCK, m), dev)
+    _call("sevo_quantize_fp8", dev, stream, _p(x), _ld(x), m, k, 1 if swiglu else 0, _p(out),
+          _p(scales))
+    return out, scales
+
+
+def sevo_pack_weight_fp8(src, dst=None, stream=None):
+    """Row-major codes float8_e4m3fn [n_out, k] (or [E, n_out, k], the experts of a
+    layer) -> a new tensor of the same shape in the packed 8-bit layout."""
+    if src.dim() not in (2, 3):
+        raise ValueError("src: [n_out, k] or [E, n_out, k]")
+    _need("src", src, torch.float8_e4m3fn)
+    if src.shape[-2] % 64:
+        raise ValueError("src: n_out must be a multiple of 64")
+    if dst is None:
+        dst = torch.empty_like(src)
+    _need("dst", dst, torch.float8_e4m3fn, src.shape, src.device)
+    k = src.shape[-1]
+    _call("sevo_pack_weight_fp8", src.device, stream, _p(src), _p(dst), src.numel() // max(k, 1), k)
+    return dst
+
+
+def sevo_linear_fp8_workspace_bytes(m, n_out, k) -> int:
+    return int(lib().sevo_linear_fp8_workspace_bytes(m, n_out, k))
+
+
+def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16, workspace=None,
+                    stream=None):
+    """Y = X W^T of 8-bit operands: x codes [m, k] (row stride from the tensor) with
+    scales [k / 128, m], w packed codes [n_out, k] (``sevo_pack_weight_fp8``) with
+    scales [ceil(n_out / 128), k / 128].  Y bf16, or fp32 (``out_dtype``, or the
+    type of ``out``, whose row stride is kept).  ``workspace``: a caller's uint8
+    buffer of sevo_linear_fp8_workspace_bytes (else one is allocated)."""
+    f8 = torch.float8_e4m3fn
+    m, k = x.shape
+    n_out = w.shape[0]
+    dev = x.device
+    _need("x", x, f8, contiguous=False)
+    _need("x_scales", x_scales, torch.float32, (k // SCALE_BLOCK, m), dev, contiguous=False)
+    _need("w", w, f8, (n_out, k), dev)
+    _need("w_scales", w_scales, torch.float32, (-(-n_out // SCALE_BLOCK), k // SCALE_BLOCK), dev)
+    if out is None:
+        out = torch.empty(m, n_out, dtype=out_dtype, device=dev)
+    _need("out", out, (torch.float32, torch.bfloat16), (m, n_out), dev, contiguous=False)
+    if workspace is None:
+        need = sevo_linear_fp8_workspace_bytes(m, n_out, k)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    a = LinearFp8Args(m=m, n_out=n_out, k=k, out_type=F32 if out.dtype == torch.float32 else BF16,
+                      ldx=_ld(x), lds=_ld(x_scales), ldo=_ld(out), x=_p(x), x_scales=_p(x_scales),
+                      w=_p(w), w_scales=_p(w_scales), out=_p(out), workspace=_p(workspace),
+                      workspace_bytes=0 if workspace is None else workspace.numel())
+    _call("sevo_linear_fp8", dev, stream, C.byref(a))
+    return out
+
+
+def sevo_moe_route(logits, top_k, score="softmax", bias=None, n_groups=1, top_groups=1,
+                   group_best=1, renormalise=True, scaling=1.0, out_experts=None,
+                   out_weights=None, stream=None):
+    """(experts int32 [n, top_k], weights fp32 [n, top_k]) of router logits fp32
+    [n, n_experts] (row stride from the tensor): ``score`` "softmax" or "sigmoid",
+    a balance ``bias`` fp32 [n_experts] on the choice, the ``top_groups`` of
+    ``n_groups`` expert groups by the sum of their ``group_best`` best."""
+    if score not in ("softmax", "sigmoid"):
+        raise ValueError(f"score: {score!r}")
+    _need("logits", logits, torch.float32, contiguous=False)
+    n, E = logits.shape
+    dev = logits.device
+    if bias is not None:
+        _need("bias", bias, torch.float32, (E,), dev)
+    if out_experts is None:
+        out_experts = torch.empty(n, top_k, dtype=torch.int32, device=dev)
+    if out_weights is None:
+        out_weights = torch.empty(n, top_k, dtype=torch.float32, device=dev)
+    _need("out_experts", out_experts, torch.int32, (n, top_k), dev)
+    _need("out_weights", out_weights, torch.float32, (n, top_k), dev)
+    a = MoeRouteArgs(n=n, n_experts=E, top_k=int(top_k),
+                     score=ROUTE_SIGMOID if score == "sigmoid" else ROUTE_SOFTMAX,
+                     n_groups=int(n_groups), top_groups=int(top_groups),
+                     group_best=int(group_best), renormalise=1 if renormalise else 0,
+                     scaling=float(scaling), ld=_ld(logits), logits=_p(logits), bias=_p(bias),
+                     out_experts=_p(out_experts), out_weights=_p(out_weights))
+    _call("sevo_moe_route", dev, stream, C.byref(a))
+    return out_experts, out_weights
+
+
+class MoeLists:
+    """The entry lists of a routing (``sevo_moe_lists``) and the sizes they are for."""
+
+    def __init__(self, n, top_k, n_experts, buffer):
+        self.n, self.top_k, self.n_experts, self.buffer = n, top_k, n_experts, buffer
+
+
+def sevo_moe_lists_bytes(n, top_k, n_experts) -> int:
+    return int(lib().sevo_moe_lists_bytes(n, top_k, n_experts))
+
+
+def sevo_moe_lists(experts, n_experts, buffer=None, stream=None) -> MoeLists:
+    """Entry lists of experts int32 [n, top_k] for ``sevo_moe_linear_fp8``.
+    ``buffer``: a caller's uint8 buffer of sevo_moe_lists_bytes."""
+    _need("experts", experts, torch.int32)
+    n, top_k = experts.shape
+    if buffer is None:
+        buffer = torch.empty(sevo_moe_lists_bytes(n, top_k, n_experts), dtype=torch.uint8,
+                             device=experts.device)
+    _need("buffer", buffer, torch.uint8, None, experts.device)
+    _call("sevo_moe_lists", experts.device, stream, _p(experts), n, top_k, int(n_experts),
+          _p(buffer), buffer.numel())
+    return MoeLists(n, top_k, int(n_experts), buffer)
+
+
+def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None, out=None,
+                        stream=None):
+    """The experts' products of a routing, bf16.  Without ``weights``: gate/up, x
+    codes [n, k], returns [n * top_k, n_out].  With ``weights`` fp32 [n, top_k]:
+    down, x codes [n * top_k, k], returns the weighted partials [top_k, n, n_out].
+    w packed codes [E, n_out, k], w_scales [E, ceil(n_out / 128), k / 128]."""
+    f8 = torch.float8_e4m3fn
+    n, top_k, E = lists.n, lists.top_k, lists.n_experts
+    down = weights is not None
+    rows, k = x.shape
+    n_out = w.shape[1]
+    dev = x.device
+    _need("x", x, f8, (n * top_k if down else n, k), contiguous=False)
+    _need("x_scales", x_scales, torch.float32, (k // SCALE_BLOCK, rows), dev, contiguous=False)
+    _need("w", w, f8, (E, n_out, k), dev)
+    _need("w_scales", w_scales, torch.float32,
+          (E, -(-n_out // SCALE_BLOCK), k // SCALE_BLOCK), dev)
+    _need("lists", lists.buffer, torch.uint8, None, dev)
+    if down:
+        _need("weights", weights, torch.float32, (n, top_k), dev)
+    shape = (top_k, n, n_out) if down else (n * top_k, n_out)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    _need("out", out, torch.bfloat16, shape, dev)
+    a = MoeLinearFp8Args(n=n, top_k=top_k, n_experts=E, n_out=n_out, k=k, down=1 if down else 0,
+                         ldx=_ld(x), lds=_ld(x_scales), x=_p(x), x_scales=_p(x_scales), w=_p(w),
+                         w_scales=_p(w_scales), weights=_p(weights), lists=_p(lists.buffer),
+                         out=_p(out))
+    _call("sevo_moe_linear_fp8", dev, stream, C.byref(a))
+    return out
 
 
 # ------------------------------------------------------------------ read probe
