@@ -255,7 +255,8 @@ struct Linear8Args {
 struct Linear8Plan {
   int splits = 1;    // K splits
   int kb_chunk = 0;  // 128-column blocks per split
-  int rb = 4, mb = 1;
+  int rb = 4, mb = 1;  // 16-row weight and activation blocks per workgroup
+  int tile = 0;        // 0: the stream; else a shape of LDS tiles
 };
 Linear8Plan plan_linear8(int m, int n_out, int k);
 size_t linear8_workspace_bytes(int m, int n_out, const Linear8Plan& p);
@@ -273,7 +274,8 @@ struct Moe8Args {
   const float* weights;  // [n][top_k] (down)
   const int32_t* offsets;   // [E + 1]
   const int32_t* assign;    // entries t top_k + slot, expert-major
-  const int32_t* tile_off;  // [E + 1] first tile of each expert
+  const int32_t* tile_off;  // [E + 1] first tile (of tile_rows entries) of each expert
+  int tile_rows;
   bf16_t* out;
 };
 // entries per tile of tile_off

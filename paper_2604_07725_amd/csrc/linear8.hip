@@ -320,15 +320,234 @@ __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
   }
 }
 
+// More rows: LDS tiles of BM x BN, eight waves in a grid of 8 / (BN / 64) x BN / 64,
+// each 16 XT rows x 64 columns.  A stage is one 128-column block: the X and W
+// codes go straight from global memory to LDS (16 bytes a lane), as do the
+// block's scales; NS stage buffers keep NS - 1 stages in flight.
+//   * W pieces are the 1 KB halves of the packed fragments;
+//   * an X piece is eight whole 128-byte rows.  Lane i brings row i % 8, run
+//     i / 8 of an even piece and run (i / 8) ^ 1 of an odd one, so the 16 lanes of a
+//     fragment read (eight rows of each) cover all 64 banks.
+// Grouped (GR): the m-tiles are tiles of the experts' lists and a tile's rows are
+// gathered per lane.
+template <int BM, int BN, int NS, bool EXACT, bool GR>
+__global__ __launch_bounds__(512) void tile8_kernel(Linear8Args a, int kb_chunk,
+                                                    float* __restrict__ part, int tiles_m, Moe8Args g) {
+  constexpr int WN = BN / 64, WM = 8 / WN, XT = BM / WM / 16;
+  static_assert(WN * WM == 8 && XT * WM * 16 == BM, "wave grid");
+  constexpr int XD = BM / 64, D = XD + BN / 64;      // X pieces and pieces of a wave and stage
+  constexpr int kScales = (BM + BN) * 128;           // byte offset of a stage's scales
+  constexpr int STAGE = kScales + 8 * 256;
+  static_assert(NS * STAGE <= 160 * 1024, "LDS");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[NS * STAGE];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  const int r = lane & 15, q = lane >> 4;
+  const int KB = a.k >> 7;
+  const int tiles_n = (a.n_out + BN - 1) / BN;
+
+  // tile order: a contiguous range of tiles per XCD, in groups of 1024 rows
+  if constexpr (GR) tiles_m = g.tile_off[g.n_experts] * (g.tile_rows / BM);
+  const int total = tiles_m * tiles_n;
+  int t = blockIdx.x;
+  if (GR && t >= total) return;  // uniform over the workgroup, before any barrier
+  {
+    const int per = total >> 3;
+    if (t < per * 8) t = (t & 7) * per + (t >> 3);
+  }
+  constexpr int GM = 1024 / BM;
+  const int first_m = t / (GM * tiles_n) * GM;
+  const int gsize = min(GM, tiles_m - first_m);
+  const int in_group = t - first_m * tiles_n;
+  const int tm = first_m + in_group % gsize, tn = in_group / gsize;
+  int m0 = tm * BM;
+  const int n0 = tn * BN;
+  int rows = a.m, ent0 = 0;
+  if constexpr (GR) {
+    const int sub = g.tile_rows / BM, tile = tm / sub;
+    int lo = 0, hi = g.n_experts;  // tile_off[lo] <= tile < tile_off[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (g.tile_off[mid] <= tile) lo = mid;
+      else hi = mid;
+    }
+    ent0 = g.offsets[lo];
+    rows = g.offsets[lo + 1] - ent0;
+    m0 = ((tile - g.tile_off[lo]) * sub + tm % sub) * BM;
+    if (m0 >= rows) return;  // uniform, before any barrier
+    a.w += (size_t)lo * a.n_out * a.k;
+    a.ws += (size_t)lo * ((a.n_out + 127) >> 7) * KB;
+  }
+  // the row of X that row i of the tile's matrix reads (rows past the end: the last)
+  auto x_row = [&](int i) {
+    i = min(i, rows - 1);
+    if constexpr (GR) {
+      const int asg = g.assign[ent0 + i];
+      return g.down ? asg : asg / g.top_k;
+    } else {
+      return i;
+    }
+  };
+
+  const int st0 = GR ? 0 : blockIdx.y * kb_chunk;
+  const int nst = GR ? KB : min(KB - st0, kb_chunk);
+
+  // ---- this wave's direct loads of a stage: D pieces and 64 scales.  Every
+  // offset is in range: rows are clamped, stages past the last are not issued.
+  struct Load {
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t voff, soff, step;
+  };
+  auto rsrc = [](const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7FFFFFFF, 0x00020000);
+  };
+  Load ld[D], ls;
+#pragma unroll
+  for (int i = 0; i < D; ++i) {
+    const int f = wave + 8 * i;
+    Load& l = ld[i];
+    if (i < XD) {
+      const int run = (lane >> 3) ^ (f & 1);
+      const int base = GR ? 0 : min(m0 + 8 * f, rows - 1);
+      const int row = x_row(m0 + 8 * f + (lane & 7));
+      l.r = rsrc(a.x + (size_t)base * a.ldx);
+      l.voff = (uint32_t)((size_t)(row - base) * a.ldx) + 16 * run;
+      l.soff = st0 * 128u;
+      l.step = 128;
+    } else {
+      const int c = f - 8 * XD;  // 1 KB half c % 2 of fragment c / 2
+      const int sb = min((n0 >> 6) + (c >> 3), (a.n_out >> 6) - 1);
+      l.r = rsrc(a.w + (size_t)sb * KB * 8192);
+      l.voff = (c & 7) * 1024 + lane * 16;
+      l.soff = st0 * 8192u;
+      l.step = 8192;
+    }
+  }
+  if (wave < XD) {  // 64 of the rows' scales
+    ls.r = rsrc(GR ? a.xs : a.xs + (size_t)st0 * a.lds);
+    ls.voff = 4u * x_row(m0 + 64 * wave + lane);
+    ls.soff = 0;
+    ls.step = (uint32_t)a.lds * 4;
+  } else {          // the weight blocks' scales (lane % 2: the tile's 128-column blocks)
+    const int nb = min((n0 >> 7) + (lane & 1), ((a.n_out + 127) >> 7) - 1);
+    ls.r = rsrc(a.ws);
+    ls.voff = 4u * nb * KB;
+    ls.soff = 4u * st0;
+    ls.step = 4;
+  }
+  auto issue = [&](int st) {
+    uint8_t* so = smem + (st % NS) * STAGE;
+#pragma unroll
+    for (int i = 0; i < D; ++i)
+      dma16(ld[i].r, ld[i].voff + (ld[i].soff + st * ld[i].step), so + (wave + 8 * i) * 1024);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        ls.r, (__attribute__((address_space(3))) void*)(so + kScales + 256 * wave), 4,
+        (int)(ls.voff + (ls.soff + st * ls.step)), 0, 0, 0);
+  };
+
+  f32x4 acc[XT][4];
+#pragma unroll
+  for (int i = 0; i < XT; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // LDS byte offsets of this lane's runs, in a stage
+  const int x_off = wm * XT * 2048 + (r >> 3) * 1024 + (((q ^ (r >> 3)) * 8) + (r & 7)) * 16;
+  const int w_off = BM * 128 + wn * 8192 + lane * 16;
+  const int sx_off = kScales + (wm * XT * 16 + r) * 4;
+  const int sw_off = kScales + 256 * 7 + (wn >> 1) * 4;
+
+  for (int st = 0; st < NS - 1 && st < nst; ++st) issue(st);
+  for (int kt = 0; kt < nst; ++kt) {
+    // stage kt has landed in every wave's part, and every wave has read stage kt - 1
+    if (NS > 2 && kt + NS - 2 < nst) wait_vmcnt<(NS - 2) * (D + 1)>();
+    else wait_vmcnt<0>();
+    wait_lgkm0();
+    lds_barrier();
+    if (kt + NS - 1 < nst) issue(kt + NS - 1);
+    const uint8_t* so = smem + (kt % NS) * STAGE;
+    Frag8 wf[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        wf[j].u[h] = *reinterpret_cast<const u32x4*>(so + w_off + 2048 * j + 1024 * h);
+    const float sw = *reinterpret_cast<const float*>(so + sw_off);
+    const Operand<EXACT> wo[4] = {Operand<EXACT>(wf[0]), Operand<EXACT>(wf[1]), Operand<EXACT>(wf[2]),
+                                  Operand<EXACT>(wf[3])};
+#pragma unroll
+    for (int i = 0; i < XT; ++i) {
+      Frag8 xf;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        xf.u[h] = *reinterpret_cast<const u32x4*>(so + x_off + 2048 * i + 512 * h);
+      const float s = *reinterpret_cast<const float*>(so + sx_off + 64 * i) * sw;
+      const Operand<EXACT> xo(xf);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) add_scaled(acc[i][j], block_product(wo[j], xo), s);
+    }
+  }
+
+  // ---- epilogue: lane holds row r and columns 4 q .. + 3 of each 16 x 16 tile
+#pragma unroll
+  for (int i = 0; i < XT; ++i) {
+    const int row = m0 + (wm * XT + i) * 16 + r;
+    if (row >= rows) continue;
+    float wt = 1.f;
+    size_t out_row = row;
+    if constexpr (GR) {
+      const int asg = g.assign[ent0 + row];
+      out_row = asg;
+      if (g.down) {
+        const int tok = asg / g.top_k;
+        out_row = (size_t)(asg - tok * g.top_k) * g.n + tok;
+        wt = g.weights[asg];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int col = n0 + wn * 64 + 16 * j + 4 * q;
+      if (col >= a.n_out) continue;
+      if (!GR && part)
+        *reinterpret_cast<f32x4*>(part + ((size_t)blockIdx.y * a.m + row) * a.n_out + col) = acc[i][j];
+      else
+        store4(a.out, out_row * a.ldo + col, GR ? acc[i][j] * wt : acc[i][j], a.out_bf16);
+    }
+  }
+}
+
 // ------------------------------------------------------------------ plans and launches
+namespace {
+
+struct Tile {
+  int bm, bn;
+};
+constexpr Tile kTiles[] = {{256, 256}, {128, 256}, {128, 128}};
+
+}  // namespace
+
 Linear8Plan plan_linear8(int m, int n_out, int k) {
   Linear8Plan p;
-  p.mb = m > 32 ? 4 : m > 16 ? 2 : 1;
   const int KB = k >> 7, nrb = n_out >> 4;
-  const int mt = (m + 16 * p.mb - 1) / (16 * p.mb);
-  p.rb = 4;
   int s = 1;
-  while (s < 8 && (long)((nrb + p.rb - 1) / p.rb) * mt * s < 256 && KB >= 8 * s) s *= 2;
+  if (m > 64) {
+    p.tile = 3;
+    for (int i = 0; i < 3; ++i) {
+      const long tiles = (long)((m + kTiles[i].bm - 1) / kTiles[i].bm) * ((n_out + kTiles[i].bn - 1) / kTiles[i].bn);
+      if (tiles >= 200) {
+        p.tile = i + 1;
+        break;
+      }
+    }
+    const Tile& t = kTiles[p.tile - 1];
+    const long tiles = (long)((m + t.bm - 1) / t.bm) * ((n_out + t.bn - 1) / t.bn);
+    while (s < 8 && tiles * s < 200 && KB >= 8 * s) s *= 2;
+  } else {
+    p.mb = m > 32 ? 4 : m > 16 ? 2 : 1;
+    p.rb = 4;
+    while (s < 8 && (long)((nrb + p.rb - 1) / p.rb) * s < 256 && KB >= 8 * s) s *= 2;
+  }
   p.kb_chunk = (KB + s - 1) / s;
   p.splits = (KB + p.kb_chunk - 1) / p.kb_chunk;
   return p;
@@ -350,6 +569,20 @@ hipError_t run_linear8(const Linear8Args& a, const Linear8Plan& p, float* part, 
   return hipGetLastError();
 }
 
+template <int BM, int BN, int NS>
+hipError_t run_tile8(const Linear8Args& a, const Linear8Plan& p, float* part, hipStream_t st) {
+  const int tiles_m = (a.m + BM - 1) / BM;
+  const dim3 grid(tiles_m * ((a.n_out + BN - 1) / BN), p.splits);
+  const Moe8Args none{};
+  if (a.out_bf16)
+    hipLaunchKernelGGL((tile8_kernel<BM, BN, NS, false, false>), grid, dim3(512), 0, st, a, p.kb_chunk,
+                       part, tiles_m, none);
+  else
+    hipLaunchKernelGGL((tile8_kernel<BM, BN, NS, true, false>), grid, dim3(512), 0, st, a, p.kb_chunk,
+                       part, tiles_m, none);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* workspace,
@@ -357,7 +590,10 @@ hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* wor
   if (a.m == 0) return hipSuccess;
   float* part = p.splits > 1 ? workspace : nullptr;
   hipError_t e;
-  if (p.mb == 4) e = run_linear8<4, 4>(a, p, part, st);
+  if (p.tile == 1) e = run_tile8<256, 256, 2>(a, p, part, st);
+  else if (p.tile == 2) e = run_tile8<128, 256, 3>(a, p, part, st);
+  else if (p.tile == 3) e = run_tile8<128, 128, 4>(a, p, part, st);
+  else if (p.mb == 4) e = run_linear8<4, 4>(a, p, part, st);
   else if (p.mb == 2) e = run_linear8<2, 4>(a, p, part, st);
   else e = run_linear8<1, 4>(a, p, part, st);
   if (e != hipSuccess || !part) return e;
@@ -369,13 +605,25 @@ hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* wor
 
 int moe8_tile_rows(int64_t entries, int n_experts) { return entries < 96ll * n_experts ? 128 : 256; }
 
-hipError_t launch_moe8(const Moe8Args& a, hipStream_t st) {
-  if (a.n == 0) return hipSuccess;
-  const long per = ((long)a.n * a.top_k + a.n_experts - 1) / a.n_experts;
-  const dim3 grid((a.n_out + 127) / 128, a.n_experts);
-  if (per <= 12) hipLaunchKernelGGL(moe8_kernel<1>, grid, dim3(256), 0, st, a);
-  else if (per <= 24) hipLaunchKernelGGL(moe8_kernel<2>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(moe8_kernel<4>, grid, dim3(256), 0, st, a);
+hipError_t launch_moe8(const Moe8Args& g, hipStream_t st) {
+  if (g.n == 0) return hipSuccess;
+  const int64_t entries = (int64_t)g.n * g.top_k;
+  const int64_t per = (entries + g.n_experts - 1) / g.n_experts;
+  if (per > 48) {
+    Linear8Args a{};
+    a.n_out = g.n_out; a.k = g.k; a.x = g.x; a.ldx = g.ldx; a.xs = g.xs; a.lds = g.lds;
+    a.w = g.w; a.ws = g.ws; a.out = g.out; a.ldo = g.n_out; a.out_bf16 = 1;
+    // as many tiles as lists of any lengths can fill
+    const int64_t tiles_m = std::min<int64_t>((entries + g.tile_rows - 1) / g.tile_rows + g.n_experts, entries);
+    const dim3 grid((unsigned)(tiles_m * (g.tile_rows / 128) * ((g.n_out + 255) / 256)));
+    hipLaunchKernelGGL((tile8_kernel<128, 256, 3, false, true>), grid, dim3(512), 0, st, a, g.k >> 7,
+                       nullptr, 0, g);
+    return hipGetLastError();
+  }
+  const dim3 grid((g.n_out + 127) / 128, g.n_experts);
+  if (per <= 12) hipLaunchKernelGGL(moe8_kernel<1>, grid, dim3(256), 0, st, g);
+  else if (per <= 24) hipLaunchKernelGGL(moe8_kernel<2>, grid, dim3(256), 0, st, g);
+  else hipLaunchKernelGGL(moe8_kernel<4>, grid, dim3(256), 0, st, g);
   return hipGetLastError();
 }
 

@@ -1543,8 +1543,9 @@ SEVO_API sevo_status sevo_linear_fp8(const sevo_linear_fp8_args* a, void* stream
   if (a->m < 0 || (a->out_type != SEVO_F32 && a->out_type != SEVO_BF16))
     return fail(SEVO_ERR_INVALID_ARGUMENT, "m %d, out_type %d", a->m, a->out_type);
   if (sevo_status s = check_fp8_product(a->n_out, a->k, a->ldx)) return s;
-  if (a->lds < a->m || a->lds >= 1 << 29)
-    return fail(SEVO_ERR_INVALID_ARGUMENT, "lds %lld outside [m, 2^29)", (long long)a->lds);
+  if (a->lds < a->m) return fail(SEVO_ERR_INVALID_ARGUMENT, "lds %lld < m", (long long)a->lds);
+  if (a->lds >= ((int64_t)1 << 31) / 4 / (a->k / 128))
+    return fail(SEVO_ERR_UNSUPPORTED, "x_scales of 2^31 bytes or more: fewer rows a call");
   if (a->ldo < a->n_out || a->ldo % 4)
     return fail(SEVO_ERR_INVALID_ARGUMENT, "ldo %lld must be a multiple of 4, at least n_out",
                 (long long)a->ldo);
@@ -1647,6 +1648,7 @@ SEVO_API sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void
   m.w = static_cast<const uint8_t*>(a->w); m.ws = a->w_scales;
   m.weights = a->weights;
   m.offsets = p + L.offsets; m.assign = p + L.assign; m.tile_off = p + L.tiles;
+  m.tile_rows = sevo::moe8_tile_rows((int64_t)a->n * a->top_k, a->n_experts);
   m.out = static_cast<sevo::bf16_t*>(a->out);
   hipError_t e = sevo::launch_moe8(m, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_moe_linear_fp8");
