@@ -258,7 +258,7 @@ struct Linear8Plan {
   int rb = 4, mb = 1;  // 16-row weight and activation blocks per workgroup
   int tile = 0;        // 0: the stream; else a shape of LDS tiles
 };
-Linear8Plan plan_linear8(int m, int n_out, int k);
+Linear8Plan plan_linear8(int m, int n_out, int k, int out_bf16);
 size_t linear8_workspace_bytes(int m, int n_out, const Linear8Plan& p);
 hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* workspace,
                           hipStream_t st);

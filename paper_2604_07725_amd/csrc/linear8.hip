@@ -50,11 +50,13 @@ struct Operand;
 template <>
 struct Operand<false> {
   i32x8 v;
+  Operand() = default;
   __device__ __forceinline__ explicit Operand(const Frag8& f) : v(f.v) {}
 };
 template <>
 struct Operand<true> {
   bf16x8v v[4];
+  Operand() = default;
   __device__ __forceinline__ explicit Operand(const Frag8& f) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = codes_to_bf16(f.u[i >> 1][2 * (i & 1)], f.u[i >> 1][2 * (i & 1) + 1]);
@@ -85,6 +87,21 @@ __device__ __forceinline__ void store4(void* out, size_t off, const f32x4& v, in
   else
     *reinterpret_cast<f32x4*>(static_cast<float*>(out) + off) = v;
 }
+
+// Direct global -> LDS load of N bytes per lane at voff (checked against the
+// records) + soff (wave-uniform, not checked); lane i's bytes land at lds + N i.
+template <int N>
+__device__ __forceinline__ void dma_s(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t soff,
+                                      uint8_t* lds) {
+  static_assert(N == 16 || N == 4, "bytes per lane");
+  const auto dst = (__attribute__((address_space(3))) void*)lds;
+  if constexpr (N == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, (int)voff, (int)soff, 0, 0);
+  else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 4, (int)voff, (int)soff, 0, 0);
+}
+
+// steps between two direct loads of tile8_kernel, by its activation tiles per wave
+template <int XT>
+constexpr int kSpread = XT == 8 ? 2 : 1;
 
 }  // namespace
 
@@ -325,20 +342,24 @@ __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
 // codes go straight from global memory to LDS (16 bytes a lane), as do the
 // block's scales; NS stage buffers keep NS - 1 stages in flight.
 //   * W pieces are the 1 KB halves of the packed fragments;
-//   * an X piece is eight whole 128-byte rows.  Lane i brings row i % 8, run
-//     i / 8 of an even piece and run (i / 8) ^ 1 of an odd one, so the 16 lanes of a
-//     fragment read (eight rows of each) cover all 64 banks.
+//   * an X piece is eight whole 128-byte rows.  Its place p of 8 rows x 16 bytes
+//     holds run p / 2 + 4 (p % 2), in odd pieces run p / 2 + 4 (1 - p % 2), so that
+//     lane l of a fragment read (two pieces) finds its run at bank 4 l modulo 64, as in
+//     one contiguous read (without: 4 more LDS cycles per read).
+// A workgroup takes tiles blockIdx.x, + gridDim.x, ...: the next tile's first
+// stages load while this one's results are stored.
 // Grouped (GR): the m-tiles are tiles of the experts' lists and a tile's rows are
 // gathered per lane.
 template <int BM, int BN, int NS, bool EXACT, bool GR>
 __global__ __launch_bounds__(512) void tile8_kernel(Linear8Args a, int kb_chunk,
                                                     float* __restrict__ part, int tiles_m, Moe8Args g) {
   constexpr int WN = BN / 64, WM = 8 / WN, XT = BM / WM / 16;
-  static_assert(WN * WM == 8 && XT * WM * 16 == BM, "wave grid");
+  static_assert(WN * WM == 8 && XT * WM * 16 == BM && XT % 2 == 0, "wave grid");
   constexpr int XD = BM / 64, D = XD + BN / 64;      // X pieces and pieces of a wave and stage
   constexpr int kScales = (BM + BN) * 128;           // byte offset of a stage's scales
   constexpr int STAGE = kScales + 8 * 256;
-  static_assert(NS * STAGE <= 160 * 1024, "LDS");
+  constexpr int kOutRow = 64 * 2 + 16;               // bytes of a staged bf16 output row of a wave
+  static_assert(NS * STAGE <= 160 * 1024 && 8 * 16 * kOutRow <= STAGE, "LDS");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[NS * STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -346,174 +367,291 @@ __global__ __launch_bounds__(512) void tile8_kernel(Linear8Args a, int kb_chunk,
   const int r = lane & 15, q = lane >> 4;
   const int KB = a.k >> 7;
   const int tiles_n = (a.n_out + BN - 1) / BN;
-
-  // tile order: a contiguous range of tiles per XCD, in groups of 1024 rows
-  if constexpr (GR) tiles_m = g.tile_off[g.n_experts] * (g.tile_rows / BM);
-  const int total = tiles_m * tiles_n;
-  int t = blockIdx.x;
-  if (GR && t >= total) return;  // uniform over the workgroup, before any barrier
-  {
-    const int per = total >> 3;
-    if (t < per * 8) t = (t & 7) * per + (t >> 3);
-  }
-  constexpr int GM = 1024 / BM;
-  const int first_m = t / (GM * tiles_n) * GM;
-  const int gsize = min(GM, tiles_m - first_m);
-  const int in_group = t - first_m * tiles_n;
-  const int tm = first_m + in_group % gsize, tn = in_group / gsize;
-  int m0 = tm * BM;
-  const int n0 = tn * BN;
-  int rows = a.m, ent0 = 0;
-  if constexpr (GR) {
-    const int sub = g.tile_rows / BM, tile = tm / sub;
-    int lo = 0, hi = g.n_experts;  // tile_off[lo] <= tile < tile_off[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (g.tile_off[mid] <= tile) lo = mid;
-      else hi = mid;
-    }
-    ent0 = g.offsets[lo];
-    rows = g.offsets[lo + 1] - ent0;
-    m0 = ((tile - g.tile_off[lo]) * sub + tm % sub) * BM;
-    if (m0 >= rows) return;  // uniform, before any barrier
-    a.w += (size_t)lo * a.n_out * a.k;
-    a.ws += (size_t)lo * ((a.n_out + 127) >> 7) * KB;
-  }
-  // the row of X that row i of the tile's matrix reads (rows past the end: the last)
-  auto x_row = [&](int i) {
-    i = min(i, rows - 1);
-    if constexpr (GR) {
-      const int asg = g.assign[ent0 + i];
-      return g.down ? asg : asg / g.top_k;
-    } else {
-      return i;
-    }
-  };
-
   const int st0 = GR ? 0 : blockIdx.y * kb_chunk;
   const int nst = GR ? KB : min(KB - st0, kb_chunk);
+  if constexpr (GR) tiles_m = g.tile_off[g.n_experts] * (g.tile_rows / BM);
+  const int total = tiles_m * tiles_n;
 
-  // ---- this wave's direct loads of a stage: D pieces and 64 scales.  Every
-  // offset is in range: rows are clamped, stages past the last are not issued.
-  struct Load {
-    __amdgpu_buffer_rsrc_t r;
-    uint32_t voff, soff, step;
-  };
-  auto rsrc = [](const void* p) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7FFFFFFF, 0x00020000);
-  };
-  Load ld[D], ls;
-#pragma unroll
-  for (int i = 0; i < D; ++i) {
-    const int f = wave + 8 * i;
-    Load& l = ld[i];
-    if (i < XD) {
-      const int run = (lane >> 3) ^ (f & 1);
-      const int base = GR ? 0 : min(m0 + 8 * f, rows - 1);
-      const int row = x_row(m0 + 8 * f + (lane & 7));
-      l.r = rsrc(a.x + (size_t)base * a.ldx);
-      l.voff = (uint32_t)((size_t)(row - base) * a.ldx) + 16 * run;
-      l.soff = st0 * 128u;
-      l.step = 128;
-    } else {
-      const int c = f - 8 * XD;  // 1 KB half c % 2 of fragment c / 2
-      const int sb = min((n0 >> 6) + (c >> 3), (a.n_out >> 6) - 1);
-      l.r = rsrc(a.w + (size_t)sb * KB * 8192);
-      l.voff = (c & 7) * 1024 + lane * 16;
-      l.soff = st0 * 8192u;
-      l.step = 8192;
+  // ---- one tile: its place, and this wave's direct loads of a stage (D pieces and
+  // 64 scales): three descriptors, offsets of the lane and of the piece and stage
+  // (scalar).  Every offset is in range (rows are clamped; 256 ldx and 256 k are
+  // below 2^31); past the last stage the descriptors have no records, so that the
+  // loop issues without a branch and nothing is read.
+  const uint8_t* xb;   // what the X, W and scale offsets count from
+  const uint8_t* wb;
+  const float* sb;
+  uint32_t x_voff[XD], w_soff[D - XD], s_voff, s_step;
+  int m0, n0, rows, ent0;
+  // (false: nothing in it)
+  auto set_tile = [&](int t) {
+    // a contiguous range of tiles per XCD, in groups of 1024 rows
+    const int per = total >> 3;
+    if (t < per * 8) t = (t & 7) * per + (t >> 3);
+    constexpr int GM = 1024 / BM;
+    const int first_m = t / (GM * tiles_n) * GM;
+    const int gsize = min(GM, tiles_m - first_m);
+    const int in_group = t - first_m * tiles_n;
+    const int tm = first_m + in_group % gsize;
+    n0 = in_group / gsize * BN;
+    m0 = tm * BM;
+    rows = a.m;
+    ent0 = 0;
+    const uint8_t* w = a.w;
+    const float* ws = a.ws;
+    if constexpr (GR) {
+      const int sub = g.tile_rows / BM, tile = tm / sub;
+      int lo = 0, hi = g.n_experts;  // tile_off[lo] <= tile < tile_off[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (g.tile_off[mid] <= tile) lo = mid;
+        else hi = mid;
+      }
+      ent0 = g.offsets[lo];
+      rows = g.offsets[lo + 1] - ent0;
+      m0 = ((tile - g.tile_off[lo]) * sub + tm % sub) * BM;
+      if (m0 >= rows) return false;
+      w += (size_t)lo * a.n_out * a.k;
+      ws += (size_t)lo * ((a.n_out + 127) >> 7) * KB;
     }
-  }
-  if (wave < XD) {  // 64 of the rows' scales
-    ls.r = rsrc(GR ? a.xs : a.xs + (size_t)st0 * a.lds);
-    ls.voff = 4u * x_row(m0 + 64 * wave + lane);
-    ls.soff = 0;
-    ls.step = (uint32_t)a.lds * 4;
-  } else {          // the weight blocks' scales (lane % 2: the tile's 128-column blocks)
-    const int nb = min((n0 >> 7) + (lane & 1), ((a.n_out + 127) >> 7) - 1);
-    ls.r = rsrc(a.ws);
-    ls.voff = 4u * nb * KB;
-    ls.soff = 4u * st0;
-    ls.step = 4;
-  }
-  auto issue = [&](int st) {
-    uint8_t* so = smem + (st % NS) * STAGE;
+    // the row of X that row i of the tile's matrix reads (rows past the end: the last)
+    auto x_row = [&](int i) {
+      i = min(i, rows - 1);
+      if constexpr (GR) {
+        const int asg = g.assign[ent0 + i];
+        return g.down ? asg : asg / g.top_k;
+      } else {
+        return i;
+      }
+    };
+    const int base = GR ? 0 : m0;
+    xb = a.x + (size_t)base * a.ldx;
+    wb = w + (size_t)(n0 >> 6) * KB * 8192;
 #pragma unroll
-    for (int i = 0; i < D; ++i)
-      dma16(ld[i].r, ld[i].voff + (ld[i].soff + st * ld[i].step), so + (wave + 8 * i) * 1024);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        ls.r, (__attribute__((address_space(3))) void*)(so + kScales + 256 * wave), 4,
-        (int)(ls.voff + (ls.soff + st * ls.step)), 0, 0, 0);
+    for (int i = 0; i < XD; ++i) {
+      const int f = wave + 8 * i;
+      const int run = (lane >> 4) + 4 * (((lane >> 3) ^ f) & 1);
+      x_voff[i] = (uint32_t)((size_t)(x_row(m0 + 8 * f + (lane & 7)) - base) * a.ldx) + 16 * run;
+    }
+#pragma unroll
+    for (int i = 0; i < D - XD; ++i) {
+      const int c = wave + 8 * i;  // 1 KB half c % 2 of fragment c / 2
+      w_soff[i] = (uint32_t)(min(c >> 3, ((a.n_out - n0) >> 6) - 1) * KB * 8192 + (c & 7) * 1024);
+    }
+    if (wave < XD) {  // 64 of the rows' scales
+      sb = GR ? a.xs : a.xs + (size_t)st0 * a.lds;
+      s_voff = 4u * x_row(m0 + 64 * wave + lane);
+      s_step = (uint32_t)a.lds * 4;
+    } else {          // the weight blocks' scales (lane % 2: the tile's 128-column blocks)
+      const int nb = min((n0 >> 7) + (lane & 1), ((a.n_out + 127) >> 7) - 1);
+      sb = ws + st0;
+      s_voff = 4u * nb * KB;
+      s_step = 4;
+    }
+    return true;
   };
-
-  f32x4 acc[XT][4];
+  // loads [i0, i1) of stage st (load D: the scales)
+  auto issue = [&](int st, int i0, int i1) {
+    uint8_t* so = smem + (st % NS) * STAGE;
+    const int records = st < nst ? 0x7FFFFFFF : 0;
+    auto rsrc = [&](const void* p) {
+      return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, records, 0x00020000);
+    };
 #pragma unroll
-  for (int i = 0; i < XT; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < D; ++i) {
+      if (i < i0 || i >= i1) continue;
+      uint8_t* dst = so + (wave + 8 * i) * 1024;
+      if (i < XD) dma_s<16>(rsrc(xb), x_voff[i], (st0 + st) * 128, dst);
+      else dma_s<16>(rsrc(wb), lane * 16, (st0 + st) * 8192 + w_soff[i - XD], dst);
+    }
+    if (i0 <= D && D < i1) dma_s<4>(rsrc(sb), s_voff, st * s_step, so + kScales + 256 * wave);
+  };
 
   // LDS byte offsets of this lane's runs, in a stage
-  const int x_off = wm * XT * 2048 + (r >> 3) * 1024 + (((q ^ (r >> 3)) * 8) + (r & 7)) * 16;
+  const int x_off0 = wm * XT * 2048 + (r >> 3) * 1024 + ((2 * q + (r >> 3)) * 8 + (r & 7)) * 16;
+  const int x_off1 = x_off0 ^ 128;
   const int w_off = BM * 128 + wn * 8192 + lane * 16;
   const int sx_off = kScales + (wm * XT * 16 + r) * 4;
   const int sw_off = kScales + 256 * 7 + (wn >> 1) * 4;
+  Frag8 wf[4], xf[2];
+  Operand<EXACT> wo[4], xo;
+  auto read_w = [&](const uint8_t* so, int j) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      wf[j].u[h] = *reinterpret_cast<const u32x4*>(so + w_off + 2048 * j + 1024 * h);
+  };
+  auto read_x = [&](const uint8_t* so, int i) {
+    xf[i & 1].u[0] = *reinterpret_cast<const u32x4*>(so + x_off0 + 2048 * i);
+    xf[i & 1].u[1] = *reinterpret_cast<const u32x4*>(so + x_off1 + 2048 * i);
+  };
+  auto read_sx = [&](const uint8_t* so, int i) {
+    return *reinterpret_cast<const float*>(so + sx_off + 64 * i);
+  };
+  auto read_sw = [&](const uint8_t* so) { return *reinterpret_cast<const float*>(so + sw_off); };
 
-  for (int st = 0; st < NS - 1 && st < nst; ++st) issue(st);
-  for (int kt = 0; kt < nst; ++kt) {
-    // stage kt has landed in every wave's part, and every wave has read stage kt - 1
-    if (NS > 2 && kt + NS - 2 < nst) wait_vmcnt<(NS - 2) * (D + 1)>();
-    else wait_vmcnt<0>();
-    wait_lgkm0();
+  // The loads of a stage are spread over its steps (a product each), one every EV
+  // steps from the meeting on: issued together they fill the address queue, and
+  // the waves wait for it instead of running products.
+  constexpr int EV = kSpread<XT>, kAfter = (4 + EV - 1) / EV;  // kAfter: in the last tile's steps
+  static_assert((D + 1) * EV <= 4 * XT, "a stage's loads fit its steps");
+  constexpr int kStores = 2 * XT;  // of a full bf16 tile, per wave
+
+  // the tile at t or the next one with rows; all of it uniform over the workgroup
+  int t = blockIdx.x;
+  auto next_tile = [&]() {
+    while (t < total && !set_tile(t)) t += gridDim.x;
+    return t < total;
+  };
+  if (!next_tile()) return;
+  for (int st = 0; st < NS - 1; ++st) issue(st, 0, D + 1);
+  bool stores_behind = false;  // exactly kStores stores were issued after those loads
+  for (;;) {
+    f32x4 acc[XT][4];
+#pragma unroll
+    for (int i = 0; i < XT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // Pipeline.  The weight fragments and the first activation tile of a stage are
+    // in registers when it begins.  Once its last activation tile is too, the
+    // waves meet: stage kt + 1 has landed, and the buffer of stage kt is free for
+    // the direct loads of stage kt + NS.  That tile's products run after the
+    // meeting, each weight fragment replaced by the next stage's as soon as it is
+    // done, so that neither the barrier nor the LDS latency leaves the matrix
+    // cores without work.  A product is added to its accumulator two products
+    // later; the last two of a stage in the next one.
+    if (stores_behind) wait_vmcnt<(NS - 2) * (D + 1) + kStores>();
+    else wait_vmcnt<(NS - 2) * (D + 1)>();
     lds_barrier();
-    if (kt + NS - 1 < nst) issue(kt + NS - 1);
-    const uint8_t* so = smem + (kt % NS) * STAGE;
-    Frag8 wf[4];
+    issue(NS - 1, 0, kAfter);
+    float sc[2], sw, sw_next;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) read_w(smem, j);
+    read_x(smem, 0);
+    sw = read_sw(smem);
+    sc[0] = read_sx(smem, 0) * sw;
+    sc[1] = 0.f;
+    f32x4 p[4];  // products on their way
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        wf[j].u[h] = *reinterpret_cast<const u32x4*>(so + w_off + 2048 * j + 1024 * h);
-    const float sw = *reinterpret_cast<const float*>(so + sw_off);
-    const Operand<EXACT> wo[4] = {Operand<EXACT>(wf[0]), Operand<EXACT>(wf[1]), Operand<EXACT>(wf[2]),
-                                  Operand<EXACT>(wf[3])};
+    for (int j = 0; j < 4; ++j) p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int kt = 0; kt < nst; ++kt) {
+      const uint8_t* so = smem + (kt % NS) * STAGE;
+      const uint8_t* sn = smem + ((kt + 1) % NS) * STAGE;
 #pragma unroll
-    for (int i = 0; i < XT; ++i) {
-      Frag8 xf;
+      for (int i = 0; i < XT; ++i) {
+        float s_read = 0.f;
+        if (i == XT - 1) {
+          wait_vmcnt<(NS - 2) * (D + 1)>();
+          wait_lgkm0();
+          lds_barrier();
+        }
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        xf.u[h] = *reinterpret_cast<const u32x4*>(so + x_off + 2048 * i + 512 * h);
-      const float s = *reinterpret_cast<const float*>(so + sx_off + 64 * i) * sw;
-      const Operand<EXACT> xo(xf);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) add_scaled(acc[i][j], block_product(wo[j], xo), s);
-    }
-  }
-
-  // ---- epilogue: lane holds row r and columns 4 q .. + 3 of each 16 x 16 tile
-#pragma unroll
-  for (int i = 0; i < XT; ++i) {
-    const int row = m0 + (wm * XT + i) * 16 + r;
-    if (row >= rows) continue;
-    float wt = 1.f;
-    size_t out_row = row;
-    if constexpr (GR) {
-      const int asg = g.assign[ent0 + row];
-      out_row = asg;
-      if (g.down) {
-        const int tok = asg / g.top_k;
-        out_row = (size_t)(asg - tok * g.top_k) * g.n + tok;
-        wt = g.weights[asg];
+        for (int j = 0; j < 4; ++j) {
+          if (i < XT - 1) {
+            if (j == 0) read_x(so, i + 1);
+            if (j == 1) s_read = read_sx(so, i + 1);
+          }
+          if (j == 0) xo = Operand<EXACT>(xf[i & 1]);
+          if (i == 0) wo[j] = Operand<EXACT>(wf[j]);
+          p[j] = block_product(wo[j], xo);
+          // two products back
+          if (j >= 2) add_scaled(acc[i][j - 2], p[j - 2], sc[i & 1]);
+          else add_scaled(acc[(i + XT - 1) % XT][j + 2], p[j + 2], sc[(i + 1) & 1]);
+          if (i == XT - 1) {
+            // (after the last stage these read a stale buffer that is never used)
+            read_w(sn, j);
+            if (j == 0) read_x(sn, 0);
+            if (j == 1) sw_next = read_sw(sn);
+            if (j == 1) s_read = read_sx(sn, 0);
+          }
+          const int step = (4 * i + j + 4) % (4 * XT);  // from the meeting on
+          if (step % EV == 0 && step / EV <= D)
+            issue(i == XT - 1 ? kt + NS : kt + NS - 1, step / EV, step / EV + 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (i == XT - 1) sw = sw_next;
+        sc[(i + 1) & 1] = s_read * sw;
       }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int col = n0 + wn * 64 + 16 * j + 4 * q;
-      if (col >= a.n_out) continue;
-      if (!GR && part)
-        *reinterpret_cast<f32x4*>(part + ((size_t)blockIdx.y * a.m + row) * a.n_out + col) = acc[i][j];
-      else
-        store4(a.out, out_row * a.ldo + col, GR ? acc[i][j] * wt : acc[i][j], a.out_bf16);
+    for (int j = 2; j < 4; ++j) add_scaled(acc[XT - 1][j], p[j], sc[1]);
+
+    // ---- the next tile's first stages, then this one's results
+    const int om0 = m0, on0 = n0, orows = rows, oent0 = ent0;
+    t += gridDim.x;
+    wait_vmcnt<0>();   // (the stages that the loop issued past the last, in zeros)
+    wait_lgkm0();
+    lds_barrier();     // every wave is done with the stage buffers
+    const bool more = next_tile();
+    if (more)
+      for (int st = 0; st < NS - 1; ++st) issue(st, 0, D + 1);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);  // the stores stay behind those loads
+    // output row of row i of the tile's matrix, and its routing weight
+    auto out_of = [&](int row, float& wt) -> size_t {
+      wt = 1.f;
+      if constexpr (GR) {
+        const int asg = g.assign[oent0 + row];
+        if (!g.down) return asg;
+        const int tok = asg / g.top_k;
+        wt = g.weights[asg];
+        return (size_t)(asg - tok * g.top_k) * g.n + tok;
+      } else {
+        return row;
+      }
+    };
+    if (!EXACT && !part) {
+      // bf16: sixteen rows at a time through the wave's share of the last stage
+      // buffer (which those loads leave alone), to leave as whole 128-byte runs
+      uint8_t* ot = smem + (NS - 1) * STAGE + wave * 16 * kOutRow;
+      const int col = on0 + wn * 64 + 8 * (lane & 7);
+#pragma unroll
+      for (int i = 0; i < XT; ++i) {
+        const int row0 = om0 + (wm * XT + i) * 16;
+        float wt = 1.f;
+        if constexpr (GR) {
+          if (row0 >= orows) break;
+          if (g.down) wt = g.weights[g.assign[oent0 + min(row0 + r, orows - 1)]];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 v = GR ? acc[i][j] * wt : acc[i][j];
+          *reinterpret_cast<uint2*>(ot + r * kOutRow + 32 * j + 8 * q) =
+              uint2{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
+        }
+        wait_lgkm0();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int lr = 8 * h + (lane >> 3), row = row0 + lr;
+          const u32x4 v = *reinterpret_cast<const u32x4*>(ot + lr * kOutRow + 16 * (lane & 7));
+          if (row < orows && col < a.n_out) {
+            float unused;
+            *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.out) + out_of(row, unused) * a.ldo + col) = v;
+          }
+        }
+        wait_lgkm0();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      stores_behind = !GR && om0 + BM <= orows && on0 + BN <= a.n_out;
+    } else {
+#pragma unroll
+      for (int i = 0; i < XT; ++i) {
+        const int row = om0 + (wm * XT + i) * 16 + r;
+        if (row >= orows) continue;
+        float wt;
+        const size_t out_row = out_of(row, wt);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int col = on0 + wn * 64 + 16 * j + 4 * q;
+          if (col >= a.n_out) continue;
+          if (part)
+            *reinterpret_cast<f32x4*>(part + ((size_t)blockIdx.y * a.m + row) * a.n_out + col) = acc[i][j];
+          else
+            store4(a.out, out_row * a.ldo + col, GR ? acc[i][j] * wt : acc[i][j], a.out_bf16);
+        }
+      }
     }
+    if (!more) break;
+    if (!stores_behind) wait_vmcnt<0>();
   }
 }
 
@@ -523,17 +661,18 @@ namespace {
 struct Tile {
   int bm, bn;
 };
+constexpr int kCUs = 256;  // one workgroup of LDS tiles each
 constexpr Tile kTiles[] = {{256, 256}, {128, 256}, {128, 128}};
 
 }  // namespace
 
-Linear8Plan plan_linear8(int m, int n_out, int k) {
+Linear8Plan plan_linear8(int m, int n_out, int k, int out_bf16) {
   Linear8Plan p;
   const int KB = k >> 7, nrb = n_out >> 4;
   int s = 1;
   if (m > 64) {
     p.tile = 3;
-    for (int i = 0; i < 3; ++i) {
+    for (int i = out_bf16 ? 0 : 1; i < 3; ++i) {
       const long tiles = (long)((m + kTiles[i].bm - 1) / kTiles[i].bm) * ((n_out + kTiles[i].bn - 1) / kTiles[i].bn);
       if (tiles >= 200) {
         p.tile = i + 1;
@@ -572,15 +711,20 @@ hipError_t run_linear8(const Linear8Args& a, const Linear8Plan& p, float* part, 
 template <int BM, int BN, int NS>
 hipError_t run_tile8(const Linear8Args& a, const Linear8Plan& p, float* part, hipStream_t st) {
   const int tiles_m = (a.m + BM - 1) / BM;
-  const dim3 grid(tiles_m * ((a.n_out + BN - 1) / BN), p.splits);
+  const int tiles = tiles_m * ((a.n_out + BN - 1) / BN);
+  const dim3 grid(std::min(tiles, std::max(1, kCUs / p.splits)), p.splits);
   const Moe8Args none{};
-  if (a.out_bf16)
+  if (a.out_bf16) {
     hipLaunchKernelGGL((tile8_kernel<BM, BN, NS, false, false>), grid, dim3(512), 0, st, a, p.kb_chunk,
                        part, tiles_m, none);
-  else
+    return hipGetLastError();
+  }
+  if constexpr (BM * BN < 256 * 256) {  // the converted weights have no room beside 256 x 256 sums
     hipLaunchKernelGGL((tile8_kernel<BM, BN, NS, true, false>), grid, dim3(512), 0, st, a, p.kb_chunk,
                        part, tiles_m, none);
-  return hipGetLastError();
+    return hipGetLastError();
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -615,7 +759,8 @@ hipError_t launch_moe8(const Moe8Args& g, hipStream_t st) {
     a.w = g.w; a.ws = g.ws; a.out = g.out; a.ldo = g.n_out; a.out_bf16 = 1;
     // as many tiles as lists of any lengths can fill
     const int64_t tiles_m = std::min<int64_t>((entries + g.tile_rows - 1) / g.tile_rows + g.n_experts, entries);
-    const dim3 grid((unsigned)(tiles_m * (g.tile_rows / 128) * ((g.n_out + 255) / 256)));
+    const int64_t tiles = tiles_m * (g.tile_rows / 128) * ((g.n_out + 255) / 256);
+    const dim3 grid((unsigned)std::min<int64_t>(tiles, kCUs));
     hipLaunchKernelGGL((tile8_kernel<128, 256, 3, false, true>), grid, dim3(512), 0, st, a, g.k >> 7,
                        nullptr, 0, g);
     return hipGetLastError();

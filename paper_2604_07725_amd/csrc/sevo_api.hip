@@ -1440,11 +1440,11 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 // shape rules shared by the products
 sevo_status check_fp8_product(int n_out, int k, int64_t ldx) {
   if (n_out < 1 || k < 1) return fail(SEVO_ERR_INVALID_ARGUMENT, "n_out %d, k %d", n_out, k);
-  if (n_out % 64 || k % 128 || k >= 1 << 24)
-    return fail(SEVO_ERR_UNSUPPORTED, "n_out %d must be a multiple of 64 and k %d of 128 below 2^24",
+  if (n_out % 64 || k % 128 || k >= 1 << 23)
+    return fail(SEVO_ERR_UNSUPPORTED, "n_out %d must be a multiple of 64 and k %d of 128 below 2^23",
                 n_out, k);
-  if (ldx < k || ldx % 16 || ldx >= 1 << 26)
-    return fail(SEVO_ERR_INVALID_ARGUMENT, "ldx %lld must be a multiple of 16 in [k, 2^26)",
+  if (ldx < k || ldx % 16 || ldx >= 1 << 23)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "ldx %lld must be a multiple of 16 in [k, 2^23)",
                 (long long)ldx);
   return SEVO_OK;
 }
@@ -1534,8 +1534,9 @@ SEVO_API sevo_status sevo_pack_weight_fp8(const void* src, void* dst, int64_t n_
 }
 
 SEVO_API size_t sevo_linear_fp8_workspace_bytes(int32_t m, int32_t n_out, int32_t k) {
-  if (m <= 0 || n_out <= 0 || k <= 0 || n_out % 64 || k % 128 || k >= 1 << 24) return 0;
-  return sevo::linear8_workspace_bytes(m, n_out, sevo::plan_linear8(m, n_out, k));
+  if (m <= 0 || n_out <= 0 || k <= 0 || n_out % 64 || k % 128 || k >= 1 << 23) return 0;
+  return std::max(sevo::linear8_workspace_bytes(m, n_out, sevo::plan_linear8(m, n_out, k, 0)),
+                  sevo::linear8_workspace_bytes(m, n_out, sevo::plan_linear8(m, n_out, k, 1)));
 }
 
 SEVO_API sevo_status sevo_linear_fp8(const sevo_linear_fp8_args* a, void* stream) {
@@ -1552,7 +1553,7 @@ SEVO_API sevo_status sevo_linear_fp8(const sevo_linear_fp8_args* a, void* stream
   if (a->m == 0) return SEVO_OK;
   if (bad_ptr(a->x) || !a->x_scales || bad_ptr(a->w) || !a->w_scales || bad_ptr(a->out))
     return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
-  const sevo::Linear8Plan p = sevo::plan_linear8(a->m, a->n_out, a->k);
+  const sevo::Linear8Plan p = sevo::plan_linear8(a->m, a->n_out, a->k, a->out_type == SEVO_BF16);
   const size_t need = sevo::linear8_workspace_bytes(a->m, a->n_out, p);
   if (need > 0) {
     if (bad_ptr(a->workspace)) return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned workspace");

@@ -81,9 +81,9 @@ def test_pack_weight_fp8_refuses(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(m=-1), sevo.INVALID_ARGUMENT), (dict(out_type=2), sevo.INVALID_ARGUMENT),
     (dict(n_out=0), sevo.INVALID_ARGUMENT), (dict(n_out=96), sevo.UNSUPPORTED),
-    (dict(k=192), sevo.UNSUPPORTED), (dict(k=1 << 24, ldx=1 << 24), sevo.UNSUPPORTED),
+    (dict(k=192), sevo.UNSUPPORTED), (dict(k=1 << 23, ldx=1 << 23), sevo.UNSUPPORTED),
     (dict(ldx=240), sevo.INVALID_ARGUMENT), (dict(ldx=264), sevo.INVALID_ARGUMENT),
-    (dict(ldx=1 << 26), sevo.INVALID_ARGUMENT), (dict(lds=1 << 28), sevo.UNSUPPORTED), (dict(lds=3), sevo.INVALID_ARGUMENT),
+    (dict(ldx=1 << 23), sevo.INVALID_ARGUMENT), (dict(lds=1 << 28), sevo.UNSUPPORTED), (dict(lds=3), sevo.INVALID_ARGUMENT),
     (dict(ldo=124), sevo.INVALID_ARGUMENT), (dict(ldo=130), sevo.INVALID_ARGUMENT),
     (dict(x=0), sevo.INVALID_ARGUMENT), (dict(x_scales=0), sevo.INVALID_ARGUMENT),
     (dict(w=F + 8), sevo.INVALID_ARGUMENT), (dict(w_scales=0), sevo.INVALID_ARGUMENT),
