@@ -99,10 +99,6 @@ __device__ __forceinline__ void dma_s(__amdgpu_buffer_rsrc_t r, uint32_t voff, u
   else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 4, (int)voff, (int)soff, 0, 0);
 }
 
-// steps between two direct loads of tile8_kernel, by its activation tiles per wave
-template <int XT>
-constexpr int kSpread = XT == 8 ? 2 : 1;
-
 }  // namespace
 
 // Few rows: a weight stream.  One workgroup per (RB 16-row weight blocks, K
@@ -337,29 +333,32 @@ __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
   }
 }
 
-// More rows: LDS tiles of BM x BN, eight waves in a grid of 8 / (BN / 64) x BN / 64,
+// More rows: LDS tiles of BM x BN, NW waves in a grid of NW / (BN / 64) x BN / 64,
 // each 16 XT rows x 64 columns.  A stage is one 128-column block: the X and W
 // codes go straight from global memory to LDS (16 bytes a lane), as do the
 // block's scales; NS stage buffers keep NS - 1 stages in flight.
 //   * W pieces are the 1 KB halves of the packed fragments;
-//   * an X piece is eight whole 128-byte rows.  Its place p of 8 rows x 16 bytes
-//     holds run p / 2 + 4 (p % 2), in odd pieces run p / 2 + 4 (1 - p % 2), so that
-//     lane l of a fragment read (two pieces) finds its run at bank 4 l modulo 64, as in
-//     one contiguous read (without: 4 more LDS cycles per read).
+//   * an X piece is eight whole 128-byte rows, eight consecutive lanes each (a
+//     lane per row in turn: 16 bytes per clock and CU instead of 57).  Place p of
+//     row r holds run p ^ (r / 2 % 8), so that each quarter of a fragment read covers
+//     all 64 banks.
 // A workgroup takes tiles blockIdx.x, + gridDim.x, ...: the next tile's first
 // stages load while this one's results are stored.
 // Grouped (GR): the m-tiles are tiles of the experts' lists and a tile's rows are
 // gathered per lane.
-template <int BM, int BN, int NS, bool EXACT, bool GR>
-__global__ __launch_bounds__(512) void tile8_kernel(Linear8Args a, int kb_chunk,
+template <int BM, int BN, int NW, int NS, bool EXACT, bool GR>
+__global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_chunk,
                                                     float* __restrict__ part, int tiles_m, Moe8Args g) {
-  constexpr int WN = BN / 64, WM = 8 / WN, XT = BM / WM / 16;
-  static_assert(WN * WM == 8 && XT * WM * 16 == BM && XT % 2 == 0, "wave grid");
-  constexpr int XD = BM / 64, D = XD + BN / 64;      // X pieces and pieces of a wave and stage
+  constexpr int WN = BN / 64, WM = NW / WN, XT = BM / WM / 16;
+  static_assert(WN * WM == NW && XT * WM * 16 == BM && XT % 2 == 0, "wave grid");
+  constexpr int XD = BM / 8 / NW, D = XD + BN / 8 / NW;  // X pieces and pieces of a wave and stage
+  static_assert(XD * 8 * NW == BM && D * 8 * NW == BM + BN, "whole pieces");
   constexpr int kScales = (BM + BN) * 128;           // byte offset of a stage's scales
-  constexpr int STAGE = kScales + 8 * 256;
+  constexpr int XS = (BM + 63) / 64;                 // waves that bring row scales, 64 each
+  static_assert(XS < NW, "a wave for the weight scales");
+  constexpr int STAGE = kScales + NW * 256;
   constexpr int kOutRow = 64 * 2 + 16;               // bytes of a staged bf16 output row of a wave
-  static_assert(NS * STAGE <= 160 * 1024 && 8 * 16 * kOutRow <= STAGE, "LDS");
+  static_assert(NS * STAGE <= 160 * 1024 && NW * 16 * kOutRow <= STAGE, "LDS");
   __shared__ __attribute__((aligned(1024))) uint8_t smem[NS * STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -428,16 +427,16 @@ __global__ __launch_bounds__(512) void tile8_kernel(Linear8Args a, int kb_chunk,
     wb = w + (size_t)(n0 >> 6) * KB * 8192;
 #pragma unroll
     for (int i = 0; i < XD; ++i) {
-      const int f = wave + 8 * i;
-      const int run = (lane >> 4) + 4 * (((lane >> 3) ^ f) & 1);
-      x_voff[i] = (uint32_t)((size_t)(x_row(m0 + 8 * f + (lane & 7)) - base) * a.ldx) + 16 * run;
+      const int f = wave + NW * i;
+      const int run = (lane & 7) ^ (4 * (f & 1) + (lane >> 4));
+      x_voff[i] = (uint32_t)((size_t)(x_row(m0 + 8 * f + (lane >> 3)) - base) * a.ldx) + 16 * run;
     }
 #pragma unroll
     for (int i = 0; i < D - XD; ++i) {
-      const int c = wave + 8 * i;  // 1 KB half c % 2 of fragment c / 2
+      const int c = wave + NW * i;  // 1 KB half c % 2 of fragment c / 2
       w_soff[i] = (uint32_t)(min(c >> 3, ((a.n_out - n0) >> 6) - 1) * KB * 8192 + (c & 7) * 1024);
     }
-    if (wave < XD) {  // 64 of the rows' scales
+    if (wave < XS) {  // 64 of the rows' scales
       sb = GR ? a.xs : a.xs + (size_t)st0 * a.lds;
       s_voff = 4u * x_row(m0 + 64 * wave + lane);
       s_step = (uint32_t)a.lds * 4;
@@ -459,7 +458,7 @@ __global__ __launch_bounds__(512) void tile8_kernel(Linear8Args a, int kb_chunk,
 #pragma unroll
     for (int i = 0; i < D; ++i) {
       if (i < i0 || i >= i1) continue;
-      uint8_t* dst = so + (wave + 8 * i) * 1024;
+      uint8_t* dst = so + (wave + NW * i) * 1024;
       if (i < XD) dma_s<16>(rsrc(xb), x_voff[i], (st0 + st) * 128, dst);
       else dma_s<16>(rsrc(wb), lane * 16, (st0 + st) * 8192 + w_soff[i - XD], dst);
     }
@@ -467,11 +466,11 @@ __global__ __launch_bounds__(512) void tile8_kernel(Linear8Args a, int kb_chunk,
   };
 
   // LDS byte offsets of this lane's runs, in a stage
-  const int x_off0 = wm * XT * 2048 + (r >> 3) * 1024 + ((2 * q + (r >> 3)) * 8 + (r & 7)) * 16;
-  const int x_off1 = x_off0 ^ 128;
+  const int x_off0 = wm * XT * 2048 + r * 128 + (q ^ (r >> 1)) * 16;
+  const int x_off1 = x_off0 ^ 64;
   const int w_off = BM * 128 + wn * 8192 + lane * 16;
   const int sx_off = kScales + (wm * XT * 16 + r) * 4;
-  const int sw_off = kScales + 256 * 7 + (wn >> 1) * 4;
+  const int sw_off = kScales + 256 * (NW - 1) + (wn >> 1) * 4;
   Frag8 wf[4], xf[2];
   Operand<EXACT> wo[4], xo;
   auto read_w = [&](const uint8_t* so, int j) {
@@ -488,11 +487,11 @@ __global__ __launch_bounds__(512) void tile8_kernel(Linear8Args a, int kb_chunk,
   };
   auto read_sw = [&](const uint8_t* so) { return *reinterpret_cast<const float*>(so + sw_off); };
 
-  // The loads of a stage are spread over its steps (a product each), one every EV
-  // steps from the meeting on: issued together they fill the address queue, and
-  // the waves wait for it instead of running products.
-  constexpr int EV = kSpread<XT>, kAfter = (4 + EV - 1) / EV;  // kAfter: in the last tile's steps
-  static_assert((D + 1) * EV <= 4 * XT, "a stage's loads fit its steps");
+  // The loads of a stage are spread over steps (a product each) from the meeting
+  // on, one a step where the steps suffice: issued together they fill the address
+  // queue, and the waves wait for it instead of running products.
+  constexpr int SP = D + 1 < 4 * XT ? D + 1 : 4 * XT;
+  constexpr int kAfter = 4 * (D + 1) / SP;  // those of the last tile's four steps
   constexpr int kStores = 2 * XT;  // of a full bf16 tile, per wave
 
   // the tile at t or the next one with rows; all of it uniform over the workgroup
@@ -563,8 +562,8 @@ __global__ __launch_bounds__(512) void tile8_kernel(Linear8Args a, int kb_chunk,
             if (j == 1) s_read = read_sx(sn, 0);
           }
           const int step = (4 * i + j + 4) % (4 * XT);  // from the meeting on
-          if (step % EV == 0 && step / EV <= D)
-            issue(i == XT - 1 ? kt + NS : kt + NS - 1, step / EV, step / EV + 1);
+          if (step < SP)
+            issue(i == XT - 1 ? kt + NS : kt + NS - 1, step * (D + 1) / SP, (step + 1) * (D + 1) / SP);
           __builtin_amdgcn_sched_barrier(0);
         }
         if (i == XT - 1) sw = sw_next;
@@ -708,19 +707,25 @@ hipError_t run_linear8(const Linear8Args& a, const Linear8Plan& p, float* part, 
   return hipGetLastError();
 }
 
-template <int BM, int BN, int NS>
+// workgroups of LDS tiles that a CU holds at once
+template <int BM, int BN, int NW, int NS>
+constexpr int per_cu() {
+  return NS * ((BM + BN) * 128 + NW * 256) <= 80 * 1024 ? 2 : 1;
+}
+
+template <int BM, int BN, int NW, int NS>
 hipError_t run_tile8(const Linear8Args& a, const Linear8Plan& p, float* part, hipStream_t st) {
   const int tiles_m = (a.m + BM - 1) / BM;
   const int tiles = tiles_m * ((a.n_out + BN - 1) / BN);
-  const dim3 grid(std::min(tiles, std::max(1, kCUs / p.splits)), p.splits);
+  const dim3 grid(std::min(tiles, std::max(1, kCUs * per_cu<BM, BN, NW, NS>() / p.splits)), p.splits);
   const Moe8Args none{};
   if (a.out_bf16) {
-    hipLaunchKernelGGL((tile8_kernel<BM, BN, NS, false, false>), grid, dim3(512), 0, st, a, p.kb_chunk,
+    hipLaunchKernelGGL((tile8_kernel<BM, BN, NW, NS, false, false>), grid, dim3(64 * NW), 0, st, a, p.kb_chunk,
                        part, tiles_m, none);
     return hipGetLastError();
   }
   if constexpr (BM * BN < 256 * 256) {  // the converted weights have no room beside 256 x 256 sums
-    hipLaunchKernelGGL((tile8_kernel<BM, BN, NS, true, false>), grid, dim3(512), 0, st, a, p.kb_chunk,
+    hipLaunchKernelGGL((tile8_kernel<BM, BN, NW, NS, true, false>), grid, dim3(64 * NW), 0, st, a, p.kb_chunk,
                        part, tiles_m, none);
     return hipGetLastError();
   }
@@ -734,11 +739,29 @@ hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* wor
   if (a.m == 0) return hipSuccess;
   float* part = p.splits > 1 ? workspace : nullptr;
   hipError_t e;
-  if (p.tile == 1) e = run_tile8<256, 256, 2>(a, p, part, st);
-  else if (p.tile == 2) e = run_tile8<128, 256, 3>(a, p, part, st);
-  else if (p.tile == 3) e = run_tile8<128, 128, 4>(a, p, part, st);
+  if (p.tile == 1) e = run_tile8<256, 256, 8, 2>(a, p, part, st);
+  else if (p.tile == 2) e = run_tile8<128, 256, 8, 3>(a, p, part, st);
+  else if (p.tile == 3) e = run_tile8<128, 128, 8, 4>(a, p, part, st);
+  else if (p.tile == 4) e = run_tile8<64, 256, 8, 3>(a, p, part, st);
+  else if (p.tile == 5) e = run_tile8<64, 128, 4, 3>(a, p, part, st);
+  else if (p.tile == 6) e = run_tile8<32, 256, 4, 2>(a, p, part, st);
+  else if (p.tile == 7) e = run_tile8<32, 128, 2, 3>(a, p, part, st);
+  else if (p.tile == 8) e = run_tile8<32, 256, 4, 4>(a, p, part, st);
+  else if (p.tile == 9) e = run_tile8<64, 128, 4, 6>(a, p, part, st);
+  else if (p.mb == 4 && p.rb == 1) e = run_linear8<4, 1>(a, p, part, st);
+  else if (p.mb == 4 && p.rb == 2) e = run_linear8<4, 2>(a, p, part, st);
+  else if (p.mb == 4 && p.rb == 3) e = run_linear8<4, 3>(a, p, part, st);
   else if (p.mb == 4) e = run_linear8<4, 4>(a, p, part, st);
+  else if (p.mb == 2 && p.rb == 1) e = run_linear8<2, 1>(a, p, part, st);
+  else if (p.mb == 2 && p.rb == 2) e = run_linear8<2, 2>(a, p, part, st);
+  else if (p.mb == 2 && p.rb == 3) e = run_linear8<2, 3>(a, p, part, st);
+  else if (p.mb == 2 && p.rb == 6) e = run_linear8<2, 6>(a, p, part, st);
   else if (p.mb == 2) e = run_linear8<2, 4>(a, p, part, st);
+  else if (p.rb == 1) e = run_linear8<1, 1>(a, p, part, st);
+  else if (p.rb == 2) e = run_linear8<1, 2>(a, p, part, st);
+  else if (p.rb == 3) e = run_linear8<1, 3>(a, p, part, st);
+  else if (p.rb == 6) e = run_linear8<1, 6>(a, p, part, st);
+  else if (p.rb == 8) e = run_linear8<1, 8>(a, p, part, st);
   else e = run_linear8<1, 4>(a, p, part, st);
   if (e != hipSuccess || !part) return e;
   const size_t blocks = ((size_t)a.m * a.n_out / 4 + 255) / 256;
@@ -761,7 +784,7 @@ hipError_t launch_moe8(const Moe8Args& g, hipStream_t st) {
     const int64_t tiles_m = std::min<int64_t>((entries + g.tile_rows - 1) / g.tile_rows + g.n_experts, entries);
     const int64_t tiles = tiles_m * (g.tile_rows / 128) * ((g.n_out + 255) / 256);
     const dim3 grid((unsigned)std::min<int64_t>(tiles, kCUs));
-    hipLaunchKernelGGL((tile8_kernel<128, 256, 3, false, true>), grid, dim3(512), 0, st, a, g.k >> 7,
+    hipLaunchKernelGGL((tile8_kernel<128, 256, 8, 3, false, true>), grid, dim3(512), 0, st, a, g.k >> 7,
                        nullptr, 0, g);
     return hipGetLastError();
   }

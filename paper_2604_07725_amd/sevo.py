@@ -637,8 +637,22 @@ def _ld(t):
 
 def _call(name, device, stream, *args):
     """The C call on the tensors' device, by default on its current stream."""
-    with torch.cuda.device(device):
-        _check(getattr(lib(), name)(*args, _stream(stream)))
+    i = device.index
+    if i is None:
+        raise ValueError(f"{name}: tensors on {device}, expected a GPU")
+    # the stream's handle alone: building a Stream object takes longer than the launch
+    s = torch._C._cuda_getCurrentRawStream(i) if stream is None else _stream(stream)
+    if torch.cuda.current_device() == i:
+        status = getattr(lib(), name)(*args, s)
+    else:
+        with torch.cuda.device(i):
+            status = getattr(lib(), name)(*args, s)
+    if status != OK:
+        _check(status)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16=None,
@@ -666,8 +680,8 @@ def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16
     a = AddRmsnormFp8Args(
         rows=rows, cols=cols, n_partials=S,
         partial_type=BF16 if S and partials.dtype == torch.bfloat16 else F32, eps=float(eps),
-        x=_p(x), partials=_p(partials) if S else None, gain=_p(gain), out=_p(out),
-        scales=_p(scales), out_bf16=_p(out_bf16))
+        x=_ptr(x), partials=_ptr(partials) if S else None, gain=_ptr(gain), out=_ptr(out),
+        scales=_ptr(scales), out_bf16=_ptr(out_bf16))
     _call("sevo_add_rmsnorm_fp8", dev, stream, C.byref(a))
     return out, scales
 
@@ -689,8 +703,8 @@ def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
         scales = torch.empty(k // SCALE_BLOCK, m, dtype=torch.float32, device=dev)
     _need("out", out, torch.float8_e4m3fn, (m, k), dev)
     _need("scales", scales, torch.float32, (k // SCALE_BLOCK, m), dev)
-    _call("sevo_quantize_fp8", dev, stream, _p(x), _ld(x), m, k, 1 if swiglu else 0, _p(out),
-          _p(scales))
+    _call("sevo_quantize_fp8", dev, stream, _ptr(x), _ld(x), m, k, 1 if swiglu else 0, _ptr(out),
+          _ptr(scales))
     return out, scales
 
 
@@ -706,7 +720,7 @@ def sevo_pack_weight_fp8(src, dst=None, stream=None):
         dst = torch.empty_like(src)
     _need("dst", dst, torch.float8_e4m3fn, src.shape, src.device)
     k = src.shape[-1]
-    _call("sevo_pack_weight_fp8", src.device, stream, _p(src), _p(dst), src.numel() // max(k, 1), k)
+    _call("sevo_pack_weight_fp8", src.device, stream, _ptr(src), _ptr(dst), src.numel() // max(k, 1), k)
     return dst
 
 
@@ -736,8 +750,8 @@ def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16
         need = sevo_linear_fp8_workspace_bytes(m, n_out, k)
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     a = LinearFp8Args(m=m, n_out=n_out, k=k, out_type=F32 if out.dtype == torch.float32 else BF16,
-                      ldx=_ld(x), lds=_ld(x_scales), ldo=_ld(out), x=_p(x), x_scales=_p(x_scales),
-                      w=_p(w), w_scales=_p(w_scales), out=_p(out), workspace=_p(workspace),
+                      ldx=_ld(x), lds=_ld(x_scales), ldo=_ld(out), x=_ptr(x), x_scales=_ptr(x_scales),
+                      w=_ptr(w), w_scales=_ptr(w_scales), out=_ptr(out), workspace=_ptr(workspace),
                       workspace_bytes=0 if workspace is None else workspace.numel())
     _call("sevo_linear_fp8", dev, stream, C.byref(a))
     return out
@@ -767,8 +781,8 @@ def sevo_moe_route(logits, top_k, score="softmax", bias=None, n_groups=1, top_gr
                      score=ROUTE_SIGMOID if score == "sigmoid" else ROUTE_SOFTMAX,
                      n_groups=int(n_groups), top_groups=int(top_groups),
                      group_best=int(group_best), renormalise=1 if renormalise else 0,
-                     scaling=float(scaling), ld=_ld(logits), logits=_p(logits), bias=_p(bias),
-                     out_experts=_p(out_experts), out_weights=_p(out_weights))
+                     scaling=float(scaling), ld=_ld(logits), logits=_ptr(logits), bias=_ptr(bias),
+                     out_experts=_ptr(out_experts), out_weights=_ptr(out_weights))
     _call("sevo_moe_route", dev, stream, C.byref(a))
     return out_experts, out_weights
 
@@ -793,8 +807,8 @@ def sevo_moe_lists(experts, n_experts, buffer=None, stream=None) -> MoeLists:
         buffer = torch.empty(sevo_moe_lists_bytes(n, top_k, n_experts), dtype=torch.uint8,
                              device=experts.device)
     _need("buffer", buffer, torch.uint8, None, experts.device)
-    _call("sevo_moe_lists", experts.device, stream, _p(experts), n, top_k, int(n_experts),
-          _p(buffer), buffer.numel())
+    _call("sevo_moe_lists", experts.device, stream, _ptr(experts), n, top_k, int(n_experts),
+          _ptr(buffer), buffer.numel())
     return MoeLists(n, top_k, int(n_experts), buffer)
 
 
@@ -823,9 +837,9 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
         out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
     _need("out", out, torch.bfloat16, shape, dev)
     a = MoeLinearFp8Args(n=n, top_k=top_k, n_experts=E, n_out=n_out, k=k, down=1 if down else 0,
-                         ldx=_ld(x), lds=_ld(x_scales), x=_p(x), x_scales=_p(x_scales), w=_p(w),
-                         w_scales=_p(w_scales), weights=_p(weights), lists=_p(lists.buffer),
-                         out=_p(out))
+                         ldx=_ld(x), lds=_ld(x_scales), x=_ptr(x), x_scales=_ptr(x_scales), w=_ptr(w),
+                         w_scales=_ptr(w_scales), weights=_ptr(weights), lists=_ptr(lists.buffer),
+                         out=_ptr(out))
     _call("sevo_moe_linear_fp8", dev, stream, C.byref(a))
     return out
 
