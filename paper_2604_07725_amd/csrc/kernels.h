@@ -253,9 +253,9 @@ struct Linear8Args {
   int out_bf16;      // else fp32
 };
 struct Linear8Plan {
-  int splits = 1;    // K splits
-  int kb_chunk = 0;  // 128-column blocks per split
-  int rb = 4, mb = 1;  // 16-row weight and activation blocks per workgroup
+  int splits = 1;      // K splits
+  int kb_chunk = 0;    // 128-column blocks per split
+  int rb = 0, mb = 0;  // the stream: 16-row weight and activation blocks per workgroup
   int tile = 0;        // 0: the stream; else a shape of LDS tiles
 };
 Linear8Plan plan_linear8(int m, int n_out, int k, int out_bf16);

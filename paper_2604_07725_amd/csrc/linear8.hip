@@ -103,11 +103,17 @@ __device__ __forceinline__ void dma_s(__amdgpu_buffer_rsrc_t r, uint32_t voff, u
 
 // Few rows: a weight stream.  One workgroup per (RB 16-row weight blocks, K
 // split, M tile of 16 MB rows); its four waves take the 128-column steps of the
-// split in turn and sum their tiles through LDS.
+// split in turn and sum their tiles through LDS.  The weights go to registers in
+// fragments of contiguous 1 KB; the activations and their scales go through the
+// wave's own LDS ring by direct loads of whole 128-byte rows (gathered per lane
+// in fragment order they came at 16 bytes per clock and CU: 64 x 4096 x 4096 in M
+// tiles of 64 13.6 -> 10.5 us, 32 x 4096 x 4096 8.7 -> 7.5).  Three step buffers: two steps in flight under the products.
 template <int MB, int RB, bool EXACT>
 __global__ __launch_bounds__(256, 1) void linear8_kernel(Linear8Args a, int kb_chunk,
                                                          float* __restrict__ part) {
-  __shared__ f32x4 red[4][RB][MB][64];
+  constexpr int kStepBytes = MB * 2048 + 256;            // a step's rows and their scales
+  constexpr int kRing = 4 * 3 * kStepBytes, kRed = 4 * RB * MB * 1024;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kRing > kRed ? kRing : kRed];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, q = lane >> 4;
@@ -122,14 +128,18 @@ __global__ __launch_bounds__(256, 1) void linear8_kernel(Linear8Args a, int kb_c
     const int rb = rb0 + i < nrb ? rb0 + i : 0;
     wp[i] = a.w + ((size_t)(rb >> 2) * KB * 4 + (rb & 3)) * 2048 + lane * 16;
   }
-  const uint8_t* xp[MB];
-  const float* xsp[MB];
+  auto rsrc = [](const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7FFFFFFF, 0x00020000);
+  };
+  // place p of row r holds run p ^ (r / 2 % 8): see tile8_kernel
+  const __amdgpu_buffer_rsrc_t xr = rsrc(a.x + (size_t)m0 * a.ldx), sr = rsrc(a.xs + m0);
+  uint32_t x_voff[2 * MB];
 #pragma unroll
-  for (int b = 0; b < MB; ++b) {
-    const int row = min(m0 + 16 * b + r, a.m - 1);
-    xp[b] = a.x + (size_t)row * a.ldx + 16 * q;
-    xsp[b] = a.xs + row;
-  }
+  for (int f = 0; f < 2 * MB; ++f)
+    x_voff[f] = (uint32_t)min(8 * f + (lane >> 3), a.m - 1 - m0) * (uint32_t)a.ldx +
+                16 * ((lane & 7) ^ (4 * (f & 1) + (lane >> 4)));
+  const uint32_t s_voff = 4u * min(lane, a.m - 1 - m0);
+  const int x_off0 = r * 128 + (q ^ (r >> 1)) * 16, x_off1 = x_off0 ^ 64;
   // the RB (at most 8) row blocks lie in at most two 128-row scale blocks
   const float* ws0 = a.ws + (size_t)(rb0 >> 3) * KB;
   const float* ws1 = a.ws + (size_t)((min(rb0 + RB, nrb) - 1) >> 3) * KB;
@@ -139,64 +149,69 @@ __global__ __launch_bounds__(256, 1) void linear8_kernel(Linear8Args a, int kb_c
   const int cnt = nsteps > wave ? (nsteps - wave + 3) >> 2 : 0;  // steps of this wave
 
   struct Step {
-    Frag8 w[RB], x[MB];
-    float sx[MB], sw0, sw1;
+    Frag8 w[RB];
+    float sw0, sw1;
   };
-  // j-th step of this wave; past the end it re-reads the last one
-  auto load = [&](Step& f, int j) {
+  constexpr int kLoads = 2 * MB + 1 + 2 * RB;  // vector loads of a step
+  uint8_t* ring = smem + wave * 3 * kStepBytes;
+  // j-th step of this wave into buffer `slot`; past the end it re-reads the last one
+  auto load = [&](Step& f, int slot, int j) {
     const int st = st0 + wave + 4 * min(j, cnt - 1);
+    uint8_t* so = ring + slot * kStepBytes;
+#pragma unroll
+    for (int b = 0; b < 2 * MB; ++b) dma_s<16>(xr, x_voff[b], st * 128u, so + 1024 * b);
+    dma_s<4>(sr, s_voff, (uint32_t)st * (uint32_t)a.lds * 4u, so + 2048 * MB);
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         f.w[i].u[h] = __builtin_nontemporal_load(
             reinterpret_cast<const u32x4*>(wp[i] + (size_t)st * 8192 + 1024 * h));
-#pragma unroll
-    for (int b = 0; b < MB; ++b) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        f.x[b].u[h] = *reinterpret_cast<const u32x4*>(xp[b] + (size_t)st * 128 + 64 * h);
-      f.sx[b] = xsp[b][(size_t)st * a.lds];
-    }
     f.sw0 = ws0[st];
     f.sw1 = ws1[st];
+    __builtin_amdgcn_sched_barrier(0);
   };
   f32x4 acc[RB][MB];
 #pragma unroll
   for (int i = 0; i < RB; ++i)
 #pragma unroll
     for (int b = 0; b < MB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto mma = [&](const Step& f) {
+  auto mma = [&](const Step& f, int slot) {
+    wait_vmcnt<2 * kLoads>();  // the step's loads; the next two steps' may still run
+    __builtin_amdgcn_sched_barrier(0);
+    const uint8_t* so = ring + slot * kStepBytes;
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
-      const Operand<EXACT> xo(f.x[b]);
-      const float s0 = f.sx[b] * f.sw0, s1 = f.sx[b] * f.sw1;
+      Frag8 xf;
+      xf.u[0] = *reinterpret_cast<const u32x4*>(so + 2048 * b + x_off0);
+      xf.u[1] = *reinterpret_cast<const u32x4*>(so + 2048 * b + x_off1);
+      const float sx = *reinterpret_cast<const float*>(so + 2048 * MB + 64 * b + 4 * r);
+      const Operand<EXACT> xo(xf);
+      const float s0 = sx * f.sw0, s1 = sx * f.sw1;
 #pragma unroll
       for (int i = 0; i < RB; ++i)
         add_scaled(acc[i][b], block_product(Operand<EXACT>(f.w[i]), xo),
                    (rb0 + i) >> 3 == rb0 >> 3 ? s0 : s1);
     }
+    wait_lgkm0();  // the buffer is read before the next load into it is issued
+    __builtin_amdgcn_sched_barrier(0);
   };
   if (cnt > 0) {
-    // three buffers: two steps of loads in flight under the products
     Step f0, f1, f2;
-    load(f0, 0);
-    load(f1, 1);
+    load(f0, 0, 0);
+    load(f1, 1, 1);
     for (int j = 0; j < cnt; j += 3) {
-      load(f2, j + 2);
-      __builtin_amdgcn_sched_barrier(0);
-      mma(f0);
-      __builtin_amdgcn_sched_barrier(0);
-      load(f0, j + 3);
-      __builtin_amdgcn_sched_barrier(0);
-      if (j + 1 < cnt) mma(f1);
-      __builtin_amdgcn_sched_barrier(0);
-      load(f1, j + 4);
-      __builtin_amdgcn_sched_barrier(0);
-      if (j + 2 < cnt) mma(f2);
-      __builtin_amdgcn_sched_barrier(0);
+      load(f2, 2, j + 2);
+      mma(f0, 0);
+      load(f0, 0, j + 3);
+      if (j + 1 < cnt) mma(f1, 1);
+      load(f1, 1, j + 4);
+      if (j + 2 < cnt) mma(f2, 2);
     }
   }
+  wait_vmcnt<0>();  // the direct loads past the end have left the ring
+  __syncthreads();
+  f32x4(*red)[RB][MB][64] = reinterpret_cast<f32x4(*)[RB][MB][64]>(smem);
 #pragma unroll
   for (int i = 0; i < RB; ++i)
 #pragma unroll
@@ -657,38 +672,75 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
 // ------------------------------------------------------------------ plans and launches
 namespace {
 
-struct Tile {
-  int bm, bn;
+constexpr int kCUs = 256;
+
+// What a plan takes (us), fitted to 10471 timings of 20 row counts from 1 to 4096
+// and 16 matrices of 0.1 to 262 MB, weights cold, in graphs (8% rms; the plan with
+// the least is 1 to 2% slower than the best of all on average, 32% at worst: 48 x
+// 5120 x 8192 20.6 for 15.6).  LDS tiles: rounds of `cap` workgroups, a stage per
+// 128-column block, dearer on a full chip, the operands' bytes, and with a K
+// split the sum kernel and its partials.
+struct TileCost {
+  int bm, bn, cap;
+  double fixed, round, stage, load, per_mb, split, split_mb;
 };
-constexpr int kCUs = 256;  // one workgroup of LDS tiles each
-constexpr Tile kTiles[] = {{256, 256}, {128, 256}, {128, 128}};
+constexpr TileCost kBf16Tiles[] = {
+    {256, 256, kCUs, 3.9, 1.7, 1.23, 0.33, 0.0, 4.3, 0.32},
+    {128, 256, kCUs, 3.3, 2.1, 0.69, 0.17, 0.033, 4.1, 0.31},
+    {128, 128, kCUs, 3.5, 1.2, 0.40, 0.11, 0.035, 3.0, 0.39},
+    {64, 256, kCUs, 3.3, 1.1, 0.51, 0.085, 0.069, 2.5, 0.39},
+    {64, 128, 2 * kCUs, 3.3, 1.2, 0.38, 0.27, 0.052, 1.9, 0.49}};
+constexpr TileCost kF32Tiles[] = {
+    {},
+    {128, 256, kCUs, 6.0, 1.8, 1.42, 0.23, 0.0, 2.0, 0.33},
+    {128, 128, kCUs, 4.8, 1.4, 0.76, 0.15, 0.007, 1.9, 0.40},
+    {64, 256, kCUs, 4.7, 1.0, 0.89, 0.14, 0.017, 1.8, 0.41},
+    {64, 128, 2 * kCUs, 4.4, 0.65, 0.65, 0.45, 0.016, 1.6, 0.53}};
+// The stream, in one round of a workgroup per CU (in more it starts and drains again):
+// each wave takes every fourth step.
+constexpr double kStreamFixed = 4.0, kStreamBlock = 0.149, kStreamPair = 0.024, kStreamMB = 0.064,
+                 kStreamSplit = 1.8, kStreamSplitMB = 1.25;
+constexpr int kStreamRB[] = {1, 2, 3, 4, 6};
 
 }  // namespace
 
 Linear8Plan plan_linear8(int m, int n_out, int k, int out_bf16) {
-  Linear8Plan p;
-  const int KB = k >> 7, nrb = n_out >> 4;
-  int s = 1;
-  if (m > 64) {
-    p.tile = 3;
-    for (int i = out_bf16 ? 0 : 1; i < 3; ++i) {
-      const long tiles = (long)((m + kTiles[i].bm - 1) / kTiles[i].bm) * ((n_out + kTiles[i].bn - 1) / kTiles[i].bn);
-      if (tiles >= 200) {
-        p.tile = i + 1;
-        break;
+  Linear8Plan best;
+  double best_us = 1e30;
+  const int KB = k >> 7;
+  const double mbytes = 1e-6 * ((double)n_out + m) * k, out_mb = 4e-6 * m * n_out;
+  for (int want : {1, 2, 3, 4, 6, 8}) {
+    if (want > 1 && KB < 2 * want) break;
+    const int chunk = (KB + want - 1) / want, s = (KB + chunk - 1) / chunk;
+    for (int mb = 1; mb <= 2 && want <= 4; ++mb)
+      for (int rb : kStreamRB) {
+        if (mb == 2 && (rb > 4 || m <= 16)) continue;
+        const int64_t wgs = (int64_t)((m + 16 * mb - 1) / (16 * mb)) * ((n_out / 16 + rb - 1) / rb) * s;
+        if (wgs > kCUs) continue;
+        const int steps = (chunk + 3) / 4;
+        const double us = kStreamFixed + steps * rb * (kStreamBlock + kStreamPair * mb) + kStreamMB * mbytes +
+                          (s > 1 ? kStreamSplit + kStreamSplitMB * s * out_mb : 0.0);
+        if (us < best_us) {
+          best_us = us;
+          best = Linear8Plan{s, chunk, rb, mb, 0};
+        }
+      }
+    for (int i = 0; i < 5; ++i) {
+      const TileCost& t = out_bf16 ? kBf16Tiles[i] : kF32Tiles[i];
+      if (!t.bm) continue;
+      const int64_t wgs = (int64_t)((m + t.bm - 1) / t.bm) * ((n_out + t.bn - 1) / t.bn) * s;
+      // over many rounds the last one's idle CUs weigh less
+      const double rounds = wgs <= 4 * t.cap ? (double)((wgs + t.cap - 1) / t.cap) : (double)wgs / t.cap + 0.5;
+      const double full = std::min(1.0, (double)wgs / t.cap);
+      const double us = t.fixed + rounds * (t.round + chunk * (t.stage + t.load * full)) +
+                        t.per_mb * mbytes + (s > 1 ? t.split + t.split_mb * s * out_mb : 0.0);
+      if (us < best_us) {
+        best_us = us;
+        best = Linear8Plan{s, chunk, 0, 0, i + 1};
       }
     }
-    const Tile& t = kTiles[p.tile - 1];
-    const long tiles = (long)((m + t.bm - 1) / t.bm) * ((n_out + t.bn - 1) / t.bn);
-    while (s < 8 && tiles * s < 200 && KB >= 8 * s) s *= 2;
-  } else {
-    p.mb = m > 32 ? 4 : m > 16 ? 2 : 1;
-    p.rb = 4;
-    while (s < 8 && (long)((nrb + p.rb - 1) / p.rb) * s < 256 && KB >= 8 * s) s *= 2;
   }
-  p.kb_chunk = (KB + s - 1) / s;
-  p.splits = (KB + p.kb_chunk - 1) / p.kb_chunk;
-  return p;
+  return best;
 }
 
 size_t linear8_workspace_bytes(int m, int n_out, const Linear8Plan& p) {
@@ -711,6 +763,19 @@ hipError_t run_linear8(const Linear8Args& a, const Linear8Plan& p, float* part, 
 template <int BM, int BN, int NW, int NS>
 constexpr int per_cu() {
   return NS * ((BM + BN) * 128 + NW * 256) <= 80 * 1024 ? 2 : 1;
+}
+
+template <int MB>
+hipError_t run_stream(const Linear8Args& a, const Linear8Plan& p, float* part, hipStream_t st) {
+  switch (p.rb) {
+    case 1: return run_linear8<MB, 1>(a, p, part, st);
+    case 2: return run_linear8<MB, 2>(a, p, part, st);
+    case 3: return run_linear8<MB, 3>(a, p, part, st);
+    case 4: return run_linear8<MB, 4>(a, p, part, st);
+    case 6:
+      if constexpr (MB == 1) return run_linear8<MB, 6>(a, p, part, st);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 template <int BM, int BN, int NW, int NS>
@@ -739,30 +804,14 @@ hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* wor
   if (a.m == 0) return hipSuccess;
   float* part = p.splits > 1 ? workspace : nullptr;
   hipError_t e;
-  if (p.tile == 1) e = run_tile8<256, 256, 8, 2>(a, p, part, st);
-  else if (p.tile == 2) e = run_tile8<128, 256, 8, 3>(a, p, part, st);
-  else if (p.tile == 3) e = run_tile8<128, 128, 8, 4>(a, p, part, st);
-  else if (p.tile == 4) e = run_tile8<64, 256, 8, 3>(a, p, part, st);
-  else if (p.tile == 5) e = run_tile8<64, 128, 4, 3>(a, p, part, st);
-  else if (p.tile == 6) e = run_tile8<32, 256, 4, 2>(a, p, part, st);
-  else if (p.tile == 7) e = run_tile8<32, 128, 2, 3>(a, p, part, st);
-  else if (p.tile == 8) e = run_tile8<32, 256, 4, 4>(a, p, part, st);
-  else if (p.tile == 9) e = run_tile8<64, 128, 4, 6>(a, p, part, st);
-  else if (p.mb == 4 && p.rb == 1) e = run_linear8<4, 1>(a, p, part, st);
-  else if (p.mb == 4 && p.rb == 2) e = run_linear8<4, 2>(a, p, part, st);
-  else if (p.mb == 4 && p.rb == 3) e = run_linear8<4, 3>(a, p, part, st);
-  else if (p.mb == 4) e = run_linear8<4, 4>(a, p, part, st);
-  else if (p.mb == 2 && p.rb == 1) e = run_linear8<2, 1>(a, p, part, st);
-  else if (p.mb == 2 && p.rb == 2) e = run_linear8<2, 2>(a, p, part, st);
-  else if (p.mb == 2 && p.rb == 3) e = run_linear8<2, 3>(a, p, part, st);
-  else if (p.mb == 2 && p.rb == 6) e = run_linear8<2, 6>(a, p, part, st);
-  else if (p.mb == 2) e = run_linear8<2, 4>(a, p, part, st);
-  else if (p.rb == 1) e = run_linear8<1, 1>(a, p, part, st);
-  else if (p.rb == 2) e = run_linear8<1, 2>(a, p, part, st);
-  else if (p.rb == 3) e = run_linear8<1, 3>(a, p, part, st);
-  else if (p.rb == 6) e = run_linear8<1, 6>(a, p, part, st);
-  else if (p.rb == 8) e = run_linear8<1, 8>(a, p, part, st);
-  else e = run_linear8<1, 4>(a, p, part, st);
+  switch (p.tile) {
+    case 1: e = run_tile8<256, 256, 8, 2>(a, p, part, st); break;
+    case 2: e = run_tile8<128, 256, 8, 3>(a, p, part, st); break;
+    case 3: e = run_tile8<128, 128, 8, 4>(a, p, part, st); break;
+    case 4: e = run_tile8<64, 256, 8, 3>(a, p, part, st); break;
+    case 5: e = run_tile8<64, 128, 4, 3>(a, p, part, st); break;
+    default: e = p.mb == 1 ? run_stream<1>(a, p, part, st) : run_stream<2>(a, p, part, st);
+  }
   if (e != hipSuccess || !part) return e;
   const size_t blocks = ((size_t)a.m * a.n_out / 4 + 255) / 256;
   hipLaunchKernelGGL(linear8_sum_kernel, dim3((unsigned)std::min<size_t>(blocks, 8192)), dim3(256), 0,

@@ -97,9 +97,9 @@ def test_linear_fp8_refuses(kw, status):
 
 def test_linear_fp8_workspace():
     L = sevo.lib()
-    need = L.sevo_linear_fp8_workspace_bytes(16, 4096, 12288)
+    need = L.sevo_linear_fp8_workspace_bytes(64, 5120, 25600)
     assert need > 0
-    a = dict(m=16, n_out=4096, k=12288, out_type=sevo.BF16, ldx=12288, lds=16, ldo=4096, x=F,
+    a = dict(m=64, n_out=5120, k=25600, out_type=sevo.BF16, ldx=25600, lds=64, ldo=5120, x=F,
              x_scales=F, w=F, w_scales=F, out=F)
     short = sevo.LinearFp8Args(**a, workspace=F, workspace_bytes=need - 1)
     assert L.sevo_linear_fp8(C.byref(short), None) == sevo.WORKSPACE_TOO_SMALL
