@@ -274,12 +274,8 @@ struct Moe8Args {
   const float* weights;  // [n][top_k] (down)
   const int32_t* offsets;   // [E + 1]
   const int32_t* assign;    // entries t top_k + slot, expert-major
-  const int32_t* tile_off;  // [E + 1] first tile (of tile_rows entries) of each expert
-  int tile_rows;
   bf16_t* out;
 };
-// entries per tile of tile_off
-int moe8_tile_rows(int64_t entries, int n_experts);
 hipError_t launch_moe8(const Moe8Args& a, hipStream_t st);
 
 // ---- moe_route.hip
@@ -293,5 +289,9 @@ struct MoeRouteArgs {
   float* out_weights;
 };
 hipError_t launch_moe_route8(const MoeRouteArgs& a, hipStream_t st);
+// the lists of launch_moe_plan (offsets [E + 1], assign [nk]); scratch of
+// moe_plan_scratch_bytes
+hipError_t launch_moe_lists(const int32_t* sel, int nk, int E, int32_t* offsets, int32_t* assign,
+                            int32_t* scratch, hipStream_t st);
 
 }  // namespace sevo

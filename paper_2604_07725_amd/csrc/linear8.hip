@@ -250,10 +250,11 @@ __global__ __launch_bounds__(256) void linear8_sum_kernel(const float* __restric
   }
 }
 
-// The same product grouped by expert.  A wave takes two 16-row weight blocks of
-// one expert over the whole k, a workgroup 128 rows (one row of weight scales); the
-// expert's entries come in tiles of 16 NB rows, gathered through its list.
-template <int NB>
+// The product grouped by expert for few entries an expert: a stream of the chosen
+// experts' weights.  A wave takes two 16-row weight blocks of one expert over the
+// whole k, a workgroup 128 rows (one row of weight scales); the expert's entries come
+// 16 at a time, gathered through its list (more than 16 read its weights again,
+// mostly from a cache).
 __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -267,24 +268,16 @@ __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
                       ((size_t)(rb0 >> 2) * KB * 4 + (rb0 & 3)) * 2048 + lane * 16;
   const float* wsp = a.ws + ((size_t)e * ((a.n_out + 127) >> 7) + (rb0 >> 3)) * KB;
   struct Step {
-    Frag8 w[2], x[NB];
-    float sx[NB], sw;
+    Frag8 w[2], x;
+    float sx, sw;
   };
-  for (int m0 = 0; m0 < ne; m0 += 16 * NB) {
-    const uint8_t* xp[NB];
-    const float* xsp[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int asg = a.assign[off + min(m0 + 16 * b + r, ne - 1)];
-      const int row = a.down ? asg : asg / a.top_k;
-      xp[b] = a.x + (size_t)row * a.ldx + 16 * q;
-      xsp[b] = a.xs + row;
-    }
-    f32x4 acc[2][NB];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int m0 = 0; m0 < ne; m0 += 16) {
+    const int asg = a.assign[off + min(m0 + r, ne - 1)];
+    const int tok = asg / a.top_k;
+    const int row = a.down ? asg : tok;
+    const uint8_t* xp = a.x + (size_t)row * a.ldx + 16 * q;
+    const float* xsp = a.xs + row;
+    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
     auto load = [&](Step& f, int j) {
       const int st = min(j, KB - 1);
 #pragma unroll
@@ -294,23 +287,16 @@ __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
           f.w[i].u[h] = __builtin_nontemporal_load(
               reinterpret_cast<const u32x4*>(wp + (size_t)st * 8192 + 2048 * i + 1024 * h));
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          f.x[b].u[h] = *reinterpret_cast<const u32x4*>(xp[b] + (size_t)st * 128 + 64 * h);
-        f.sx[b] = xsp[b][(size_t)st * a.lds];
-      }
+      for (int h = 0; h < 2; ++h)
+        f.x.u[h] = *reinterpret_cast<const u32x4*>(xp + (size_t)st * 128 + 64 * h);
+      f.sx = xsp[(size_t)st * a.lds];
       f.sw = wsp[st];
     };
     auto mma = [&](const Step& f) {
+      const Operand<false> xo(f.x);
+      const float s = f.sx * f.sw;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const Operand<false> xo(f.x[b]);
-        const float s = f.sx[b] * f.sw;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          add_scaled(acc[i][b], block_product(Operand<false>(f.w[i]), xo), s);
-      }
+      for (int i = 0; i < 2; ++i) add_scaled(acc[i], block_product(Operand<false>(f.w[i]), xo), s);
     };
     Step f0, f1, f2;
     load(f0, 0);
@@ -329,21 +315,12 @@ __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
       if (j + 2 < KB) mma(f2);
       __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int i = m0 + 16 * b + r;
-      if (i >= ne) continue;
-      const int asg = a.assign[off + i];
-      float wt = 1.f;
-      size_t row = asg;
-      if (a.down) {
-        const int t = asg / a.top_k;
-        row = (size_t)(asg - t * a.top_k) * a.n + t;
-        wt = a.weights[asg];
-      }
+    if (m0 + r < ne) {
+      const float wt = a.down ? a.weights[asg] : 1.f;
+      const size_t out = a.down ? (size_t)(asg - tok * a.top_k) * a.n + tok : (size_t)asg;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        store4(a.out, row * a.n_out + (rb0 + h) * 16 + 4 * q, acc[h][b] * wt, 1);
+        store4(a.out, out * a.n_out + (rb0 + h) * 16 + 4 * q, acc[h] * wt, 1);
     }
   }
 }
@@ -373,8 +350,9 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
   static_assert(XS < NW, "a wave for the weight scales");
   constexpr int STAGE = kScales + NW * 256;
   constexpr int kOutRow = 64 * 2 + 16;               // bytes of a staged bf16 output row of a wave
-  static_assert(NS * STAGE <= 160 * 1024 && NW * 16 * kOutRow <= STAGE, "LDS");
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[NS * STAGE];
+  constexpr int kTable = GR ? BM * 8 : 0;            // a tile's output rows and routing weights
+  static_assert(NS * STAGE + kTable <= 160 * 1024 && NW * 16 * kOutRow <= STAGE, "LDS");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[NS * STAGE + kTable];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
@@ -383,22 +361,35 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
   const int tiles_n = (a.n_out + BN - 1) / BN;
   const int st0 = GR ? 0 : blockIdx.y * kb_chunk;
   const int nst = GR ? KB : min(KB - st0, kb_chunk);
-  if constexpr (GR) tiles_m = g.tile_off[g.n_experts] * (g.tile_rows / BM);
+  // grouped: each lane keeps the first tile, first entry and entries of experts lane + 64 j
+  int e_tile[GR ? 4 : 1], e_first[GR ? 4 : 1], e_rows[GR ? 4 : 1];
+  if constexpr (GR) {
+    tiles_m = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int e = lane + 64 * j;
+      const bool in = e < g.n_experts;
+      e_first[j] = in ? g.offsets[e] : 0;
+      e_rows[j] = in ? g.offsets[e + 1] - e_first[j] : 0;
+      const int tiles = (e_rows[j] + BM - 1) / BM;
+      int incl = tiles;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(incl, o, kWave);
+        if (lane >= o) incl += y;
+      }
+      e_tile[j] = in ? tiles_m + incl - tiles : 0x7FFFFFFF;
+      tiles_m += __builtin_amdgcn_readlane(incl, 63);
+    }
+  }
   const int total = tiles_m * tiles_n;
 
-  // ---- one tile: its place, and this wave's direct loads of a stage (D pieces and
-  // 64 scales): three descriptors, offsets of the lane and of the piece and stage
-  // (scalar).  Every offset is in range (rows are clamped; 256 ldx and 256 k are
-  // below 2^31); past the last stage the descriptors have no records, so that the
-  // loop issues without a branch and nothing is read.
-  const uint8_t* xb;   // what the X, W and scale offsets count from
-  const uint8_t* wb;
-  const float* sb;
-  uint32_t x_voff[XD], w_soff[D - XD], s_voff, s_step;
-  int m0, n0, rows, ent0;
-  // (false: nothing in it)
-  auto set_tile = [&](int t) {
-    // a contiguous range of tiles per XCD, in groups of 1024 rows
+  // ---- the place of tile t: a contiguous range of tiles per XCD, in groups of 1024
+  // rows.  All of it uniform over the workgroup.
+  struct Place {
+    int m0, n0, rows, ent0, expert;
+  };
+  auto find = [&](int t) {
     const int per = total >> 3;
     if (t < per * 8) t = (t & 7) * per + (t >> 3);
     constexpr int GM = 1024 / BM;
@@ -406,62 +397,74 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     const int gsize = min(GM, tiles_m - first_m);
     const int in_group = t - first_m * tiles_n;
     const int tm = first_m + in_group % gsize;
-    n0 = in_group / gsize * BN;
-    m0 = tm * BM;
-    rows = a.m;
-    ent0 = 0;
-    const uint8_t* w = a.w;
-    const float* ws = a.ws;
+    Place p{tm * BM, in_group / gsize * BN, a.m, 0, 0};
     if constexpr (GR) {
-      const int sub = g.tile_rows / BM, tile = tm / sub;
-      int lo = 0, hi = g.n_experts;  // tile_off[lo] <= tile < tile_off[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (g.tile_off[mid] <= tile) lo = mid;
-        else hi = mid;
-      }
-      ent0 = g.offsets[lo];
-      rows = g.offsets[lo + 1] - ent0;
-      m0 = ((tile - g.tile_off[lo]) * sub + tm % sub) * BM;
-      if (m0 >= rows) return false;
-      w += (size_t)lo * a.n_out * a.k;
-      ws += (size_t)lo * ((a.n_out + 127) >> 7) * KB;
+      // the last expert whose first tile is at or before tm
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) n += __popcll(__ballot(e_tile[j] <= tm));
+      p.expert = n - 1;
+      auto of = [&](const int (&v)[4]) {
+        const int j = p.expert >> 6;
+        const int x = j == 0 ? v[0] : j == 1 ? v[1] : j == 2 ? v[2] : v[3];
+        return __builtin_amdgcn_readlane(x, p.expert & 63);
+      };
+      p.m0 = (tm - of(e_tile)) * BM;
+      p.ent0 = of(e_first);
+      p.rows = of(e_rows);
     }
-    // the row of X that row i of the tile's matrix reads (rows past the end: the last)
-    auto x_row = [&](int i) {
-      i = min(i, rows - 1);
-      if constexpr (GR) {
-        const int asg = g.assign[ent0 + i];
-        return g.down ? asg : asg / g.top_k;
-      } else {
-        return i;
-      }
-    };
-    const int base = GR ? 0 : m0;
+    return p;
+  };
+  // grouped: the entries of the rows that this lane loads (asg: of row threadIdx.x)
+  int idx[XD], asg = 0;
+  auto fetch = [&](const Place& p) {
+    if constexpr (GR) {
+#pragma unroll
+      for (int i = 0; i < XD; ++i)
+        idx[i] = g.assign[p.ent0 + min(p.m0 + 8 * (wave + NW * i) + (lane >> 3), p.rows - 1)];
+      if (wave < XS) asg = g.assign[p.ent0 + min(p.m0 + 64 * wave + lane, p.rows - 1)];
+    }
+  };
+
+  // ---- this wave's direct loads of a stage (D pieces and 64 scales): three
+  // descriptors, offsets of the lane and of the piece and stage (scalar).  Every
+  // offset is in range (rows are clamped; 256 ldx and 256 k are below 2^31); past
+  // the last stage the descriptors have no records, so that the loop issues without
+  // a branch and nothing is read.
+  const uint8_t* xb;   // what the X, W and scale offsets count from
+  const uint8_t* wb;
+  const float* sb;
+  uint32_t x_voff[XD], w_soff[D - XD], s_voff, s_step;
+  auto set_loads = [&](const Place& p) {
+    const int base = GR ? 0 : p.m0;
     xb = a.x + (size_t)base * a.ldx;
-    wb = w + (size_t)(n0 >> 6) * KB * 8192;
+    wb = a.w + (size_t)p.expert * a.n_out * a.k + (size_t)(p.n0 >> 6) * KB * 8192;
+    auto x_row = [&](int entry, int i) {  // row i of the tile's matrix (past the end: the last)
+      if constexpr (GR) return g.down ? entry : entry / g.top_k;
+      else return min(p.m0 + i, p.rows - 1);
+    };
 #pragma unroll
     for (int i = 0; i < XD; ++i) {
       const int f = wave + NW * i;
       const int run = (lane & 7) ^ (4 * (f & 1) + (lane >> 4));
-      x_voff[i] = (uint32_t)((size_t)(x_row(m0 + 8 * f + (lane >> 3)) - base) * a.ldx) + 16 * run;
+      x_voff[i] = (uint32_t)((size_t)(x_row(idx[i], 8 * f + (lane >> 3)) - base) * a.ldx) + 16 * run;
     }
 #pragma unroll
     for (int i = 0; i < D - XD; ++i) {
       const int c = wave + NW * i;  // 1 KB half c % 2 of fragment c / 2
-      w_soff[i] = (uint32_t)(min(c >> 3, ((a.n_out - n0) >> 6) - 1) * KB * 8192 + (c & 7) * 1024);
+      w_soff[i] = (uint32_t)(min(c >> 3, ((a.n_out - p.n0) >> 6) - 1) * KB * 8192 + (c & 7) * 1024);
     }
     if (wave < XS) {  // 64 of the rows' scales
-      sb = GR ? a.xs : a.xs + (size_t)st0 * a.lds;
-      s_voff = 4u * x_row(m0 + 64 * wave + lane);
+      sb = a.xs + (size_t)st0 * a.lds;
+      s_voff = 4u * x_row(asg, 64 * wave + lane);
       s_step = (uint32_t)a.lds * 4;
     } else {          // the weight blocks' scales (lane % 2: the tile's 128-column blocks)
-      const int nb = min((n0 >> 7) + (lane & 1), ((a.n_out + 127) >> 7) - 1);
-      sb = ws + st0;
+      const int nblocks = (a.n_out + 127) >> 7;
+      const int nb = min((p.n0 >> 7) + (lane & 1), nblocks - 1);
+      sb = a.ws + (size_t)p.expert * nblocks * KB + st0;
       s_voff = 4u * nb * KB;
       s_step = 4;
     }
-    return true;
   };
   // loads [i0, i1) of stage st (load D: the scales)
   auto issue = [&](int st, int i0, int i1) {
@@ -507,17 +510,14 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
   // queue, and the waves wait for it instead of running products.
   constexpr int SP = D + 1 < 4 * XT ? D + 1 : 4 * XT;
   constexpr int kAfter = 4 * (D + 1) / SP;  // those of the last tile's four steps
-  constexpr int kStores = 2 * XT;  // of a full bf16 tile, per wave
 
-  // the tile at t or the next one with rows; all of it uniform over the workgroup
   int t = blockIdx.x;
-  auto next_tile = [&]() {
-    while (t < total && !set_tile(t)) t += gridDim.x;
-    return t < total;
-  };
-  if (!next_tile()) return;
+  if (t >= total) return;  // uniform, before any barrier
+  Place at = find(t), next = at;
+  fetch(at);
+  set_loads(at);
   for (int st = 0; st < NS - 1; ++st) issue(st, 0, D + 1);
-  bool stores_behind = false;  // exactly kStores stores were issued after those loads
+  int stored = 0;  // 16-row blocks whose two stores each were issued behind those loads
   for (;;) {
     f32x4 acc[XT][4];
 #pragma unroll
@@ -532,10 +532,36 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     // done, so that neither the barrier nor the LDS latency leaves the matrix
     // cores without work.  A product is added to its accumulator two products
     // later; the last two of a stage in the next one.
-    if (stores_behind) wait_vmcnt<(NS - 2) * (D + 1) + kStores>();
+    if (stored == XT) wait_vmcnt<(NS - 2) * (D + 1) + 2 * XT>();
+    else if (stored > 0) wait_vmcnt<(NS - 2) * (D + 1) + 2>();
     else wait_vmcnt<(NS - 2) * (D + 1)>();
     lds_barrier();
-    issue(NS - 1, 0, kAfter);
+    // grouped: what the end of the tile needs is loaded under its products
+    t += gridDim.x;
+    const bool more = t < total;
+    const int asg_now = asg;
+    float wt_now = 1.f;
+    if constexpr (GR) {
+      if (g.down && wave < XS) wt_now = g.weights[asg_now];
+    }
+    if (more) {
+      next = find(t);
+      fetch(next);
+    }
+    const int wrow = wm * XT * 16;             // this wave's first row in the tile
+    const int left = at.rows - at.m0 - wrow;   // its rows with results
+    // a wave without any only loads (its SIMD's other wave then has the matrix core)
+    const int active = left > 0 ? nst : 0;
+    if (!active) {
+      issue(NS - 1, 0, D + 1);
+      for (int kt = 0; kt < nst; ++kt) {
+        wait_vmcnt<(NS - 2) * (D + 1)>();
+        lds_barrier();
+        issue(kt + NS, 0, D + 1);
+      }
+    } else {
+      issue(NS - 1, 0, kAfter);
+    }
     float sc[2], sw, sw_next;
 #pragma unroll
     for (int j = 0; j < 4; ++j) read_w(smem, j);
@@ -546,7 +572,7 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     f32x4 p[4];  // products on their way
 #pragma unroll
     for (int j = 0; j < 4; ++j) p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int kt = 0; kt < nst; ++kt) {
+    for (int kt = 0; kt < active; ++kt) {
       const uint8_t* so = smem + (kt % NS) * STAGE;
       const uint8_t* sn = smem + ((kt + 1) % NS) * STAGE;
 #pragma unroll
@@ -589,42 +615,37 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     for (int j = 2; j < 4; ++j) add_scaled(acc[XT - 1][j], p[j], sc[1]);
 
     // ---- the next tile's first stages, then this one's results
-    const int om0 = m0, on0 = n0, orows = rows, oent0 = ent0;
-    t += gridDim.x;
     wait_vmcnt<0>();   // (the stages that the loop issued past the last, in zeros)
     wait_lgkm0();
     lds_barrier();     // every wave is done with the stage buffers
-    const bool more = next_tile();
-    if (more)
+    if (more) {
+      set_loads(next);
       for (int st = 0; st < NS - 1; ++st) issue(st, 0, D + 1);
+    }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);  // the stores stay behind those loads
-    // output row of row i of the tile's matrix, and its routing weight
-    auto out_of = [&](int row, float& wt) -> size_t {
-      wt = 1.f;
-      if constexpr (GR) {
-        const int asg = g.assign[oent0 + row];
-        if (!g.down) return asg;
-        const int tok = asg / g.top_k;
-        wt = g.weights[asg];
-        return (size_t)(asg - tok * g.top_k) * g.n + tok;
-      } else {
-        return row;
+    int* t_row = reinterpret_cast<int*>(smem + NS * STAGE);  // grouped: output row, weight
+    float* t_wt = reinterpret_cast<float*>(smem + NS * STAGE) + BM;
+    if constexpr (GR) {
+      if (threadIdx.x < BM) {
+        const int tok = asg_now / g.top_k;
+        t_row[threadIdx.x] = g.down ? (asg_now - tok * g.top_k) * g.n + tok : asg_now;
+        t_wt[threadIdx.x] = wt_now;
       }
-    };
+      wait_lgkm0();
+      lds_barrier();
+    }
     if (!EXACT && !part) {
       // bf16: sixteen rows at a time through the wave's share of the last stage
-      // buffer (which those loads leave alone), to leave as whole 128-byte runs
+      // buffer (which those loads leave alone), to leave as whole 128-byte runs.
+      // Lanes past the last row store it again, so that every block is two stores.
       uint8_t* ot = smem + (NS - 1) * STAGE + wave * 16 * kOutRow;
-      const int col = on0 + wn * 64 + 8 * (lane & 7);
+      const int col0 = at.n0 + wn * 64;
+      stored = col0 < a.n_out ? max(0, min(XT, (left + 15) >> 4)) : 0;
 #pragma unroll
       for (int i = 0; i < XT; ++i) {
-        const int row0 = om0 + (wm * XT + i) * 16;
-        float wt = 1.f;
-        if constexpr (GR) {
-          if (row0 >= orows) break;
-          if (g.down) wt = g.weights[g.assign[oent0 + min(row0 + r, orows - 1)]];
-        }
+        if (i >= stored) continue;  // uniform over the wave
+        const float wt = GR ? t_wt[wrow + 16 * i + r] : 1.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const f32x4 v = GR ? acc[i][j] * wt : acc[i][j];
@@ -635,37 +656,32 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int lr = 8 * h + (lane >> 3), row = row0 + lr;
+          const int lr = min(8 * h + (lane >> 3), left - 16 * i - 1);
           const u32x4 v = *reinterpret_cast<const u32x4*>(ot + lr * kOutRow + 16 * (lane & 7));
-          if (row < orows && col < a.n_out) {
-            float unused;
-            *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.out) + out_of(row, unused) * a.ldo + col) = v;
-          }
+          const size_t row = GR ? (size_t)t_row[wrow + 16 * i + lr] : (size_t)(at.m0 + wrow + 16 * i + lr);
+          *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.out) + row * a.ldo + col0 + 8 * (lane & 7)) = v;
         }
         wait_lgkm0();
         __builtin_amdgcn_sched_barrier(0);
       }
-      stores_behind = !GR && om0 + BM <= orows && on0 + BN <= a.n_out;
     } else {
 #pragma unroll
       for (int i = 0; i < XT; ++i) {
-        const int row = om0 + (wm * XT + i) * 16 + r;
-        if (row >= orows) continue;
-        float wt;
-        const size_t out_row = out_of(row, wt);
+        if (16 * i + r >= left) continue;
+        const size_t row = at.m0 + wrow + 16 * i + r;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int col = on0 + wn * 64 + 16 * j + 4 * q;
+          const int col = at.n0 + wn * 64 + 16 * j + 4 * q;
           if (col >= a.n_out) continue;
           if (part)
             *reinterpret_cast<f32x4*>(part + ((size_t)blockIdx.y * a.m + row) * a.n_out + col) = acc[i][j];
           else
-            store4(a.out, out_row * a.ldo + col, GR ? acc[i][j] * wt : acc[i][j], a.out_bf16);
+            store4(a.out, row * a.ldo + col, acc[i][j], a.out_bf16);
         }
       }
     }
     if (!more) break;
-    if (!stores_behind) wait_vmcnt<0>();
+    at = next;
   }
 }
 
@@ -819,29 +835,48 @@ hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* wor
   return hipGetLastError();
 }
 
-int moe8_tile_rows(int64_t entries, int n_experts) { return entries < 96ll * n_experts ? 128 : 256; }
+// Rows of a tile by the entries an expert has on average, 0: the stream (30B-A3B
+// gate/up and down, us, stream / tiles of 32 / 64 / 128 / 256 rows: 4 entries 65 + 35 /
+// 75 + 39; 8 85 + 48 / 77 + 43; 16 - / 83 + 49 / 84 + 51; 32 - / 97 + 52 / 92 + 55 / 100 + 59;
+// 64 - / - / 107 + 65 / 105 + 65 / 117 + 69; 128 - / - / 147 + 96 / 126 + 76 / 141 + 89; 256
+// - / - / - / 181 + 130 / 178 + 126).
+constexpr int kStreamEntries = 6;
+
+namespace {
+
+template <int BM, int BN, int NW, int NS>
+hipError_t run_moe8(const Linear8Args& a, const Moe8Args& g, hipStream_t st) {
+  // as many tiles as lists of any lengths can fill
+  const int64_t entries = (int64_t)g.n * g.top_k;
+  const int64_t tiles_m = std::min<int64_t>((entries + BM - 1) / BM + g.n_experts, entries);
+  const int64_t tiles = tiles_m * ((g.n_out + BN - 1) / BN);
+  const dim3 grid((unsigned)std::min<int64_t>(tiles, kCUs * per_cu<BM, BN, NW, NS>()));
+  hipLaunchKernelGGL((tile8_kernel<BM, BN, NW, NS, false, true>), grid, dim3(64 * NW), 0, st, a, a.k >> 7,
+                     nullptr, 0, g);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+static int moe8_tile_rows(const Moe8Args& g) {
+  const int64_t per = ((int64_t)g.n * g.top_k + g.n_experts - 1) / g.n_experts;
+  return per <= kStreamEntries ? 0 : per <= 24 ? 32 : per <= 64 ? 64 : per <= 200 ? 128 : 256;
+}
 
 hipError_t launch_moe8(const Moe8Args& g, hipStream_t st) {
   if (g.n == 0) return hipSuccess;
-  const int64_t entries = (int64_t)g.n * g.top_k;
-  const int64_t per = (entries + g.n_experts - 1) / g.n_experts;
-  if (per > 48) {
-    Linear8Args a{};
-    a.n_out = g.n_out; a.k = g.k; a.x = g.x; a.ldx = g.ldx; a.xs = g.xs; a.lds = g.lds;
-    a.w = g.w; a.ws = g.ws; a.out = g.out; a.ldo = g.n_out; a.out_bf16 = 1;
-    // as many tiles as lists of any lengths can fill
-    const int64_t tiles_m = std::min<int64_t>((entries + g.tile_rows - 1) / g.tile_rows + g.n_experts, entries);
-    const int64_t tiles = tiles_m * (g.tile_rows / 128) * ((g.n_out + 255) / 256);
-    const dim3 grid((unsigned)std::min<int64_t>(tiles, kCUs));
-    hipLaunchKernelGGL((tile8_kernel<128, 256, 8, 3, false, true>), grid, dim3(512), 0, st, a, g.k >> 7,
-                       nullptr, 0, g);
-    return hipGetLastError();
+  Linear8Args a{};
+  a.n_out = g.n_out; a.k = g.k; a.x = g.x; a.ldx = g.ldx; a.xs = g.xs; a.lds = g.lds;
+  a.w = g.w; a.ws = g.ws; a.out = g.out; a.ldo = g.n_out; a.out_bf16 = 1;
+  switch (moe8_tile_rows(g)) {
+    case 0:
+      hipLaunchKernelGGL(moe8_kernel, dim3((g.n_out + 127) / 128, g.n_experts), dim3(256), 0, st, g);
+      return hipGetLastError();
+    case 32: return run_moe8<32, 256, 4, 2>(a, g, st);
+    case 64: return run_moe8<64, 128, 4, 3>(a, g, st);
+    case 128: return run_moe8<128, 256, 8, 3>(a, g, st);
+    default: return run_moe8<256, 256, 8, 2>(a, g, st);
   }
-  const dim3 grid((g.n_out + 127) / 128, g.n_experts);
-  if (per <= 12) hipLaunchKernelGGL(moe8_kernel<1>, grid, dim3(256), 0, st, g);
-  else if (per <= 24) hipLaunchKernelGGL(moe8_kernel<2>, grid, dim3(256), 0, st, g);
-  else hipLaunchKernelGGL(moe8_kernel<4>, grid, dim3(256), 0, st, g);
-  return hipGetLastError();
 }
 
 }  // namespace sevo

@@ -148,4 +148,100 @@ hipError_t launch_moe_route8(const MoeRouteArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Entry lists in one launch: workgroup e reads every entry twice, once to count
+// those of lower experts (its list's first place) and its own, once to write its
+// own in order: each thread holds eight consecutive entries of a chunk, and an
+// entry's rank is the matches of the lanes and waves before it.  No sums pass
+// between workgroups, and nothing depends on scheduling.
+template <int T>
+__global__ __launch_bounds__(T) void moe_lists_kernel(const int32_t* __restrict__ sel, int nk, int E,
+                                                      int32_t* __restrict__ offsets,
+                                                      int32_t* __restrict__ assign) {
+  constexpr int W = T / 64, P = 8;  // entries a thread holds
+  __shared__ int red[2][W];
+  const int e = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto load = [&](int c0, int (&v)[P]) {
+    const int i = c0 + P * tid;
+    if (i + P <= nk) {
+      *reinterpret_cast<u32x4*>(&v[0]) = *reinterpret_cast<const u32x4*>(sel + i);
+      *reinterpret_cast<u32x4*>(&v[4]) = *reinterpret_cast<const u32x4*>(sel + i + 4);
+    } else {
+#pragma unroll
+      for (int j = 0; j < P; ++j) v[j] = i + j < nk ? sel[i + j] : -1;
+    }
+  };
+  int lower = 0, own = 0;
+  for (int c0 = 0; c0 < nk; c0 += P * T) {
+    int v[P];
+    load(c0, v);
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      lower += (uint32_t)v[j] < (uint32_t)e;  // (a negative id is in no list)
+      own += v[j] == e;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    lower += __shfl_xor(lower, o, kWave);
+    own += __shfl_xor(own, o, kWave);
+  }
+  if (lane == 0) {
+    red[0][wave] = lower;
+    red[1][wave] = own;
+  }
+  __syncthreads();
+  int first = 0, count = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    first += red[0][w];
+    count += red[1][w];
+  }
+  if (tid == 0) {
+    offsets[e] = first;
+    if (e == E - 1) offsets[E] = first + count;
+  }
+  if (count == 0) return;  // uniform
+  __syncthreads();
+  int buf = 0;
+  for (int c0 = 0; c0 < nk; c0 += P * T, buf ^= 1) {
+    int v[P];
+    load(c0, v);
+    const uint64_t below = (1ull << lane) - 1;
+    int rank = 0, total = 0;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const uint64_t b = __ballot(v[j] == e);
+      rank += __popcll(b & below);
+      total += __popcll(b);
+    }
+    if (lane == 0) red[buf][wave] = total;
+    __syncthreads();  // (the other buffer's readers have passed the barrier before it is written)
+    int at = first + rank;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if (w < wave) at += red[buf][w];
+      first += red[buf][w];
+    }
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+      if (v[j] == e) assign[at++] = c0 + P * tid + j;
+  }
+}
+
+// From this many entries on, reading all of them in every workgroup costs more
+// than the three launches that count, scan and place.
+constexpr int kOneLaunchEntries = 65536;
+
+hipError_t launch_moe_lists(const int32_t* sel, int nk, int E, int32_t* offsets, int32_t* assign,
+                            int32_t* scratch, hipStream_t st) {
+  if (nk == 0) return hipSuccess;
+  if (nk > kOneLaunchEntries)
+    return launch_moe_plan(sel, nk, E, offsets, assign, st, nullptr, 256, scratch);
+  if (nk <= 2048)
+    hipLaunchKernelGGL(moe_lists_kernel<256>, dim3(E), dim3(256), 0, st, sel, nk, E, offsets, assign);
+  else
+    hipLaunchKernelGGL(moe_lists_kernel<1024>, dim3(E), dim3(1024), 0, st, sel, nk, E, offsets, assign);
+  return hipGetLastError();
+}
+
 }  // namespace sevo

@@ -1460,14 +1460,13 @@ sevo_status check_moe_shape(int n, int top_k, int n_experts) {
 
 // the parts of a lists buffer, in int32
 struct ListsLayout {
-  size_t offsets, tiles, assign, scratch, total;
+  size_t offsets, assign, scratch, total;
 };
 ListsLayout lists_layout(int n, int top_k, int n_experts) {
   const size_t nk = (size_t)n * top_k;
   ListsLayout L;
   L.offsets = 0;
-  L.tiles = round_up(n_experts + 1, 64);
-  L.assign = 2 * L.tiles;
+  L.assign = round_up(n_experts + 1, 64);
   L.scratch = L.assign + round_up(nk, 64);
   L.total = L.scratch + round_up(sevo::moe_plan_scratch_bytes((int)nk, n_experts) / 4, 64);
   return L;
@@ -1613,16 +1612,14 @@ SEVO_API sevo_status sevo_moe_lists(const int32_t* experts, int32_t n, int32_t t
                                     void* stream) {
   if (sevo_status s = check_moe_shape(n, top_k, n_experts)) return s;
   if (n == 0) return SEVO_OK;
-  if (!experts || bad_ptr(lists)) return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  if (bad_ptr(experts) || bad_ptr(lists)) return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
   const ListsLayout L = lists_layout(n, top_k, n_experts);
   if (lists_bytes < L.total * 4)
     return fail(SEVO_ERR_WORKSPACE_TOO_SMALL, "lists need %zu bytes, got %zu", L.total * 4,
                 lists_bytes);
   int32_t* p = static_cast<int32_t*>(lists);
-  hipError_t e = sevo::launch_moe_plan(experts, n * top_k, n_experts, p + L.offsets, p + L.assign,
-                                       static_cast<hipStream_t>(stream), p + L.tiles,
-                                       sevo::moe8_tile_rows((int64_t)n * top_k, n_experts),
-                                       p + L.scratch);
+  hipError_t e = sevo::launch_moe_lists(experts, n * top_k, n_experts, p + L.offsets, p + L.assign,
+                                        p + L.scratch, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_moe_lists");
 }
 
@@ -1648,8 +1645,7 @@ SEVO_API sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void
   m.xs = a->x_scales; m.lds = a->lds;
   m.w = static_cast<const uint8_t*>(a->w); m.ws = a->w_scales;
   m.weights = a->weights;
-  m.offsets = p + L.offsets; m.assign = p + L.assign; m.tile_off = p + L.tiles;
-  m.tile_rows = sevo::moe8_tile_rows((int64_t)a->n * a->top_k, a->n_experts);
+  m.offsets = p + L.offsets; m.assign = p + L.assign;
   m.out = static_cast<sevo::bf16_t*>(a->out);
   hipError_t e = sevo::launch_moe8(m, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_moe_linear_fp8");

@@ -130,12 +130,13 @@ def test_moe_route_refuses(kw, status):
 def test_moe_lists_refuses():
     L = sevo.lib()
     need = L.sevo_moe_lists_bytes(64, 8, 128)
-    assert need >= 4 * (2 * 129 + 64 * 8)
+    assert need >= 4 * (129 + 64 * 8)
     assert L.sevo_moe_lists_bytes(64, 8, 257) == 0 and L.sevo_moe_lists_bytes(0, 8, 128) == 0
     assert L.sevo_moe_lists_bytes(1 << 28, 16, 128) == 0
     call = L.sevo_moe_lists
     assert call(F, 64, 8, 128, F, need - 1, None) == sevo.WORKSPACE_TOO_SMALL
     assert call(0, 64, 8, 128, F, need, None) == sevo.INVALID_ARGUMENT
+    assert call(F + 4, 64, 8, 128, F, need, None) == sevo.INVALID_ARGUMENT
     assert call(F, 64, 8, 128, F + 4, need, None) == sevo.INVALID_ARGUMENT
     assert call(F, 64, 8, 257, F, need, None) == sevo.UNSUPPORTED
     assert call(F, 1 << 28, 16, 128, F, 1 << 40, None) == sevo.INVALID_ARGUMENT
