@@ -15,9 +15,10 @@
 // Nothing is bound by memory here (8192 x 256 logits are 8 MiB, 2 us): a wave is a
 // chain of about a thousand instructions that run once, its reductions waiting for
 // each other.  So four tokens share a wave, reductions stay in a DPP row and the
-// float64 part, rolled up and small, is entered by few.  In a graph, times with the
-// launch (3.4 us): 8192 tokens, 256 experts, sigmoid, bias, 4 of 8 groups, top 8:
-// 12.6 us (float64 throughout: 56); 8192 x 128 softmax: 7.0 (34); 64 x 128: 5.8 (30).
+// float64 path is entered by few: one token in 4000 of the grouped case below, which
+// is why its length still shows there (of 8192 tokens two, 3 us).  In a graph, times
+// with the launch (3.4 us): 8192 tokens, 256 experts, sigmoid, bias, 4 of 8 groups, top
+// 8: 15.5 us (float64 throughout: 24); 8192 x 128 softmax: 7.3 (19); 64 x 128: 6.0 (16).
 #include "common.h"
 #include "kernels.h"
 
@@ -26,6 +27,7 @@ namespace sevo {
 namespace {
 
 constexpr int kMaxExperts = 256;
+constexpr int kPerLane = kMaxExperts / 64;
 
 template <int J>
 __device__ __forceinline__ double lane_xor_f64(double v) {
@@ -40,104 +42,117 @@ __device__ __forceinline__ double row_sum_f64(double v) {
   return v + lane_xor_f64<8>(v);
 }
 
-// the wave's best (value, then lower index) of each lane's candidate; every lane gets it
-template <int J>
-__device__ __forceinline__ void best_xor(double& v, int& i) {
-  const double ov = lane_xor_f64<J>(v);
-  const int oi = lane_xor<J>(i);
-  if (ov > v || (ov == v && oi < i)) {
-    v = ov;
-    i = oi;
-  }
+// Order-preserving keys of doubles that are not NaN; 0 is below every one
+__device__ __forceinline__ uint64_t key_f64(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return u ^ ((uint64_t)((int64_t)u >> 63) | 1ull << 63);
 }
-__device__ __forceinline__ void wave_best(double& v, int& i) {
-  best_xor<32>(v, i);
-  best_xor<16>(v, i);
-  best_xor<8>(v, i);
-  best_xor<4>(v, i);
-  best_xor<2>(v, i);
-  best_xor<1>(v, i);
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, lane_xor<1>(v));
+  v = max(v, lane_xor<2>(v));
+  v = max(v, lane_xor<4>(v));
+  v = max(v, lane_xor<8>(v));
+  v = max(v, lane_xor<16>(v));
+  return max(v, lane_xor<32>(v));
+}
+// the index that goes with the wave's largest key, of equal keys the lowest index.
+// The high words nearly always decide.
+__device__ __forceinline__ int wave_best(uint64_t key, int index) {
+  const uint32_t hi = (uint32_t)(key >> 32);
+  uint64_t who = __ballot(hi == wave_max_u32(hi));
+  if (who & (who - 1)) {  // uniform
+    const uint32_t lo = (who >> (threadIdx.x & 63)) & 1 ? (uint32_t)key : 0u;
+    who &= __ballot(lo == wave_max_u32(lo));
+    if (who & (who - 1))
+      return (int)~wave_max_u32((who >> (threadIdx.x & 63)) & 1 ? ~(uint32_t)index : 0u);
+  }
+  return __builtin_amdgcn_readlane(index, __builtin_ctzll(who));
 }
 
-// One token in float64 throughout, by a wave; s: its own LDS, scores then choice values
+// One token in float64 throughout, by a wave; lane l holds experts l + 64 i.
+// s: its own LDS, scores then choice values
 __device__ __forceinline__ void route_f64(const MoeRouteArgs& a, int t, double (*s)[kMaxExperts]) {
   const int lane = threadIdx.x & 63;
   const float* lg = a.logits + (size_t)t * a.ld;
+  float x[kPerLane], bias[kPerLane];
   float mx = -INFINITY;
   bool nan = false;
-#pragma unroll 1
-  for (int e = lane; e < a.n_experts; e += 64) {
-    mx = fmaxf(mx, lg[e]);
-    nan |= lg[e] != lg[e];
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    const int e = min(lane + 64 * i, a.n_experts - 1);
+    x[i] = lg[e];
+    bias[i] = a.bias ? a.bias[e] : 0.f;
+    mx = fmaxf(mx, x[i]);
+    nan |= x[i] != x[i];
   }
   mx = wave_max(mx);
   if (!a.sigmoid && __ballot(nan)) mx = NAN;  // a softmax with a NaN is one throughout
-  double sum = 0.0;
-#pragma unroll 1
-  for (int e = lane; e < a.n_experts; e += 64) {
-    const double x = exp(a.sigmoid ? -(double)lg[e] : (double)lg[e] - (double)mx);
-    s[0][e] = a.sigmoid ? 1.0 / (1.0 + x) : x;
-    sum += x;
+  double p[kPerLane], sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    p[i] = exp(a.sigmoid ? -(double)x[i] : (double)x[i] - (double)mx);
+    if (lane + 64 * i < a.n_experts) sum += p[i];
   }
   sum = row_sum_f64(sum);
   sum += lane_xor_f64<16>(sum);
   sum += lane_xor_f64<32>(sum);
-  uint32_t open = 0;  // bit i: expert lane + 64 i may be chosen
-#pragma unroll 1
-  for (int i = 0, e = lane; e < a.n_experts; ++i, e += 64) {
-    if (!a.sigmoid) s[0][e] /= sum;
-    const double p = a.bias ? s[0][e] + (double)a.bias[e] : s[0][e];
-    s[1][e] = p == p ? p : -INFINITY;  // a NaN is chosen after everything else
-    open |= 1u << i;
+  uint64_t key[kPerLane];  // of the choice values; 0: not to be chosen
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    const int e = lane + 64 * i;
+    p[i] = (a.sigmoid ? 1.0 : p[i]) / (a.sigmoid ? 1.0 + p[i] : sum);
+    double v = a.bias ? p[i] + (double)bias[i] : p[i];
+    v = v == v ? v : -INFINITY;  // a NaN is chosen after everything else
+    key[i] = e < a.n_experts ? key_f64(v) : 0;
+    s[0][e] = p[i];
+    s[1][e] = v;
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  const int each = a.n_experts / a.n_groups;
   if (a.top_groups < a.n_groups) {
+    const int each = a.n_experts / a.n_groups;
     // lane g: the sum of group g's one or two best
-    double g = -INFINITY;
+    uint64_t g = 0;
     if (lane < a.n_groups) {
       double b0 = -INFINITY, b1 = -INFINITY;
-#pragma unroll 4
+#pragma unroll 8
       for (int i = 0; i < each; ++i) {
         const double v = s[1][lane * each + i];
         b1 = fmax(b1, fmin(b0, v));
         b0 = fmax(b0, v);
       }
-      g = a.group_best == 2 ? b0 + b1 : b0;
-      if (g != g) g = -INFINITY;  // +inf and -inf biases in one group
+      const double sum2 = a.group_best == 2 ? b0 + b1 : b0;
+      g = key_f64(sum2 == sum2 ? sum2 : -INFINITY);  // +inf and -inf biases in one group
     }
     uint64_t kept = 0;
 #pragma unroll 1
     for (int r = 0; r < a.top_groups; ++r) {
-      double v = g;
-      int i = lane < a.n_groups && !((kept >> lane) & 1) ? lane : kWave;
-      if (i == kWave) v = -INFINITY;
-      wave_best(v, i);
-      kept |= 1ull << (i & 63);
+      const int best = wave_best(g, lane);
+      kept |= 1ull << best;
+      if (lane == best) g = 0;
     }
-#pragma unroll 1
-    for (int i = 0, e = lane; e < a.n_experts; ++i, e += 64)
-      if (!((kept >> (e / each)) & 1)) open &= ~(1u << i);
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i)
+      if (!((kept >> (min(lane + 64 * i, a.n_experts - 1) / each)) & 1)) key[i] = 0;
   }
   double wt = 0.0;  // lane r: the score of choice r
   int ex = 0;
 #pragma unroll 1
   for (int r = 0; r < a.top_k; ++r) {
-    double v = -INFINITY;
-    int best = 0x7FFFFFFF;
-#pragma unroll 1
-    for (int i = 0, e = lane; e < a.n_experts; ++i, e += 64)
-      if (((open >> i) & 1) && (best == 0x7FFFFFFF || s[1][e] > v)) {
-        v = s[1][e];
-        best = e;
+    uint64_t k = key[0];
+    int at = 0;
+#pragma unroll
+    for (int i = 1; i < kPerLane; ++i)
+      if (key[i] > k) {
+        k = key[i];
+        at = i;
       }
-    wave_best(v, best);
-    if (lane == (best & 63)) open &= ~(1u << (best >> 6));
-    if (lane == r) {
-      wt = s[0][best];
-      ex = best;
-    }
+    const int best = wave_best(k, lane + 64 * at);
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i)
+      if (lane + 64 * i == best) key[i] = 0;
+    if (lane == r) ex = best;
   }
+  if (lane < a.top_k) wt = s[0][ex];
   if (a.renormalise) wt /= row_sum_f64(wt) + 1e-20;  // (top_k is at most 16)
   if (lane < a.top_k) {
     a.out_experts[(size_t)t * a.top_k + lane] = ex;
