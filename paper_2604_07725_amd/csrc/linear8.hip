@@ -642,9 +642,12 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
       uint8_t* ot = smem + (NS - 1) * STAGE + wave * 16 * kOutRow;
       const int col0 = at.n0 + wn * 64;
       stored = col0 < a.n_out ? max(0, min(XT, (left + 15) >> 4)) : 0;
-#pragma unroll
-      for (int i = 0; i < XT; ++i) {
-        if (i >= stored) continue;  // uniform over the wave
+      bf16_t* out = static_cast<bf16_t*>(a.out) + col0;
+      if (!GR) out += (size_t)(at.m0 + wrow) * a.ldo;
+      const auto orsrc = __builtin_amdgcn_make_buffer_rsrc(out, 0, 0x7FFFFFFF, 0x00020000);
+      const uint32_t o_voff = (uint32_t)((lane >> 3) * (int)a.ldo + 8 * (lane & 7)) * 2;
+      // LDS serves a wave's accesses in order: the fences only keep the compiler's
+      auto block = [&](int i, bool whole) {
         const float wt = GR ? t_wt[wrow + 16 * i + r] : 1.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -652,17 +655,28 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
           *reinterpret_cast<uint2*>(ot + r * kOutRow + 32 * j + 8 * q) =
               uint2{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
         }
-        wait_lgkm0();
-        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int lr = min(8 * h + (lane >> 3), left - 16 * i - 1);
+          int lr = 8 * h + (lane >> 3);
+          if (!whole) lr = min(lr, left - 16 * i - 1);
           const u32x4 v = *reinterpret_cast<const u32x4*>(ot + lr * kOutRow + 16 * (lane & 7));
-          const size_t row = GR ? (size_t)t_row[wrow + 16 * i + lr] : (size_t)(at.m0 + wrow + 16 * i + lr);
-          *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.out) + row * a.ldo + col0 + 8 * (lane & 7)) = v;
+          if (whole && !GR) {
+            __builtin_amdgcn_raw_buffer_store_b128(v, orsrc, o_voff, (16 * i + 8 * h) * (int)a.ldo * 2, 2);
+          } else {
+            const size_t row = GR ? (size_t)t_row[wrow + 16 * i + lr] : (size_t)(16 * i + lr);
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(out + row * a.ldo + 8 * (lane & 7)));
+          }
         }
-        wait_lgkm0();
-        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      };
+      if (left >= 16 * XT && stored == XT && (GR || a.ldo < 1 << 22)) {
+#pragma unroll
+        for (int i = 0; i < XT; ++i) block(i, true);
+      } else {
+#pragma unroll
+        for (int i = 0; i < XT; ++i)
+          if (i < stored) block(i, false);  // uniform over the wave
       }
     } else {
 #pragma unroll
