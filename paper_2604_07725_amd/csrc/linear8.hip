@@ -345,6 +345,11 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
   static_assert(WN * WM == NW && XT * WM * 16 == BM && XT % 2 == 0, "wave grid");
   constexpr int XD = BM / 8 / NW, D = XD + BN / 8 / NW;  // X pieces and pieces of a wave and stage
   static_assert(XD * 8 * NW == BM && D * 8 * NW == BM + BN, "whole pieces");
+  // Two meetings of the waves a stage where its activation tiles can be halved: see
+  // the pipeline below.  U0 and U1 are the loads that each makes room for.
+  constexpr bool TWO = NS == 2 && XT >= 4;
+  constexpr int XH = TWO ? XD / 2 : XD;
+  constexpr int U0 = TWO ? D - XD + XH : D + 1, U1 = D + 1 - U0;
   constexpr int kScales = (BM + BN) * 128;           // byte offset of a stage's scales
   constexpr int XS = (BM + 63) / 64;                 // waves that bring row scales, 64 each
   static_assert(XS < NW, "a wave for the weight scales");
@@ -415,13 +420,20 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     }
     return p;
   };
+  // Piece (8 rows) of this wave's load i of X; the first XH are of rows that the waves
+  // read before the middle of a stage.
+  auto piece = [&](int i) {
+    if constexpr (!TWO) return wave + NW * i;
+    const int h = wave + NW * (i % XH);
+    return h / XT * 2 * XT + h % XT + (i < XH ? 0 : XT);
+  };
   // grouped: the entries of the rows that this lane loads (asg: of row threadIdx.x)
   int idx[XD], asg = 0;
   auto fetch = [&](const Place& p) {
     if constexpr (GR) {
 #pragma unroll
       for (int i = 0; i < XD; ++i)
-        idx[i] = g.assign[p.ent0 + min(p.m0 + 8 * (wave + NW * i) + (lane >> 3), p.rows - 1)];
+        idx[i] = g.assign[p.ent0 + min(p.m0 + 8 * piece(i) + (lane >> 3), p.rows - 1)];
       if (wave < XS) asg = g.assign[p.ent0 + min(p.m0 + 64 * wave + lane, p.rows - 1)];
     }
   };
@@ -445,7 +457,7 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     };
 #pragma unroll
     for (int i = 0; i < XD; ++i) {
-      const int f = wave + NW * i;
+      const int f = piece(i);
       const int run = (lane & 7) ^ (4 * (f & 1) + (lane >> 4));
       x_voff[i] = (uint32_t)((size_t)(x_row(idx[i], 8 * f + (lane >> 3)) - base) * a.ldx) + 16 * run;
     }
@@ -466,21 +478,26 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
       s_step = 4;
     }
   };
-  // loads [i0, i1) of stage st (load D: the scales)
+  // loads [i0, i1) of stage st: the weights, the first XH of X, the scales, the rest of X
   auto issue = [&](int st, int i0, int i1) {
     uint8_t* so = smem + (st % NS) * STAGE;
     const int records = st < nst ? 0x7FFFFFFF : 0;
     auto rsrc = [&](const void* p) {
       return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, records, 0x00020000);
     };
+    constexpr int DW = D - XD;
 #pragma unroll
-    for (int i = 0; i < D; ++i) {
+    for (int i = 0; i <= D; ++i) {
       if (i < i0 || i >= i1) continue;
-      uint8_t* dst = so + (wave + NW * i) * 1024;
-      if (i < XD) dma_s<16>(rsrc(xb), x_voff[i], (st0 + st) * 128, dst);
-      else dma_s<16>(rsrc(wb), lane * 16, (st0 + st) * 8192 + w_soff[i - XD], dst);
+      if (i < DW) {
+        dma_s<16>(rsrc(wb), lane * 16, (st0 + st) * 8192 + w_soff[i], so + BM * 128 + (wave + NW * i) * 1024);
+      } else if (i == DW + XH) {
+        dma_s<4>(rsrc(sb), s_voff, st * s_step, so + kScales + 256 * wave);
+      } else {
+        const int x = i - DW - (i > DW + XH);
+        dma_s<16>(rsrc(xb), x_voff[x], (st0 + st) * 128, so + piece(x) * 1024);
+      }
     }
-    if (i0 <= D && D < i1) dma_s<4>(rsrc(sb), s_voff, st * s_step, so + kScales + 256 * wave);
   };
 
   // LDS byte offsets of this lane's runs, in a stage
@@ -505,11 +522,14 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
   };
   auto read_sw = [&](const uint8_t* so) { return *reinterpret_cast<const float*>(so + sw_off); };
 
-  // The loads of a stage are spread over steps (a product each) from the meeting
-  // on, one a step where the steps suffice: issued together they fill the address
-  // queue, and the waves wait for it instead of running products.
-  constexpr int SP = D + 1 < 4 * XT ? D + 1 : 4 * XT;
-  constexpr int kAfter = 4 * (D + 1) / SP;  // those of the last tile's four steps
+  // The loads are spread over steps (a product each) from the meeting on, one a step
+  // where the steps suffice: issued together they fill the address queue, and the
+  // waves wait for it instead of running products.
+  constexpr int kSteps = TWO ? 2 * XT : 4 * XT;          // from a meeting to the next one
+  constexpr int SP0 = U0 < kSteps ? U0 : kSteps;
+  constexpr int kAfter = TWO ? D + 1 : 4 * (D + 1) / SP0;  // those issued when a stage begins
+  static_assert(!TWO || U1 <= 4, "U1 within the four products after the meeting");
+  constexpr int kFlight = (NS - (TWO ? 1 : 2)) * (D + 1);  // loads younger than those waited for
 
   int t = blockIdx.x;
   if (t >= total) return;  // uniform, before any barrier
@@ -526,16 +546,37 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
       for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     // Pipeline.  The weight fragments and the first activation tile of a stage are
     // in registers when it begins.  Once its last activation tile is too, the
-    // waves meet: stage kt + 1 has landed, and the buffer of stage kt is free for
-    // the direct loads of stage kt + NS.  That tile's products run after the
+    // waves meet: what stage kt + 1 begins with has landed, and the buffer of stage kt
+    // is free for the direct loads of stage kt + NS.  That tile's products run after the
     // meeting, each weight fragment replaced by the next stage's as soon as it is
     // done, so that neither the barrier nor the LDS latency leaves the matrix
     // cores without work.  A product is added to its accumulator two products
     // later; the last two of a stage in the next one.
-    if (stored == XT) wait_vmcnt<(NS - 2) * (D + 1) + 2 * XT>();
-    else if (stored > 0) wait_vmcnt<(NS - 2) * (D + 1) + 2>();
-    else wait_vmcnt<(NS - 2) * (D + 1)>();
+    // TWO: the waves meet in the middle of the stage as well.  Its weights and the
+    // first half of its activations are in registers by then: their places are free for
+    // stage kt + NS half a stage earlier, and the second half is waited for here, half a
+    // stage later.  So a load has NS - 1/2 stages to arrive in, not NS - 1.
+    // The stores of the last tile stand between its loads and later ones: the waits for
+    // the loads before them count them, or they would wait for the stores too.
+    // Measured: 8192 x 25600 x 5120 906 -> 885 us, 8192 x 4096 x 12288 350 -> 335; with three
+    // stages a load has time enough and the second meeting only costs (512 x 8192 x 5120
+    // 29.3 -> 29.8).
+    constexpr int kFirst = (NS - 2) * (D + 1) + (TWO ? U1 - 1 : 0);
+    if (stored == XT) wait_vmcnt<kFirst + 2 * XT>();
+    else if (stored > 0) wait_vmcnt<kFirst + 2>();
+    else wait_vmcnt<kFirst>();
     lds_barrier();
+    auto meet_mid = [&](int kt) {
+      if (kt == 0 && stored == XT) wait_vmcnt<kFlight + 2 * XT>();
+      else wait_vmcnt<kFlight>();
+      wait_lgkm0();
+      lds_barrier();
+    };
+    auto meet_end = [&]() {
+      wait_vmcnt<kFlight - TWO>();
+      wait_lgkm0();
+      lds_barrier();
+    };
     // grouped: what the end of the tile needs is loaded under its products
     t += gridDim.x;
     const bool more = t < total;
@@ -555,9 +596,12 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     if (!active) {
       issue(NS - 1, 0, D + 1);
       for (int kt = 0; kt < nst; ++kt) {
-        wait_vmcnt<(NS - 2) * (D + 1)>();
-        lds_barrier();
-        issue(kt + NS, 0, D + 1);
+        if constexpr (TWO) {
+          meet_mid(kt);
+          issue(kt + NS, 0, U0);
+        }
+        meet_end();
+        issue(kt + NS, TWO ? U0 : 0, D + 1);
       }
     } else {
       issue(NS - 1, 0, kAfter);
@@ -578,11 +622,8 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
 #pragma unroll
       for (int i = 0; i < XT; ++i) {
         float s_read = 0.f;
-        if (i == XT - 1) {
-          wait_vmcnt<(NS - 2) * (D + 1)>();
-          wait_lgkm0();
-          lds_barrier();
-        }
+        if (TWO && i == XT / 2 - 1) meet_mid(kt);
+        if (i == XT - 1) meet_end();
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           if (i < XT - 1) {
@@ -602,9 +643,15 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
             if (j == 1) sw_next = read_sw(sn);
             if (j == 1) s_read = read_sx(sn, 0);
           }
-          const int step = (4 * i + j + 4) % (4 * XT);  // from the meeting on
-          if (step < SP)
-            issue(i == XT - 1 ? kt + NS : kt + NS - 1, step * (D + 1) / SP, (step + 1) * (D + 1) / SP);
+          if constexpr (TWO) {
+            const int step = 4 * (i - (XT / 2 - 1)) + j;  // from the middle on
+            if (step >= 0 && step < SP0) issue(kt + NS, step * U0 / SP0, (step + 1) * U0 / SP0);
+            if (i == XT - 1 && j < U1) issue(kt + NS, U0 + j, U0 + j + 1);
+          } else {
+            const int step = (4 * i + j + 4) % (4 * XT);  // from the meeting on
+            if (step < SP0)
+              issue(i == XT - 1 ? kt + NS : kt + NS - 1, step * (D + 1) / SP0, (step + 1) * (D + 1) / SP0);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
         if (i == XT - 1) sw = sw_next;
