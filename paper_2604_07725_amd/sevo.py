@@ -749,6 +749,8 @@ def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16
     if workspace is None:
         need = sevo_linear_fp8_workspace_bytes(m, n_out, k)
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    else:
+        _need("workspace", workspace, torch.uint8, None, dev)
     a = LinearFp8Args(m=m, n_out=n_out, k=k, out_type=F32 if out.dtype == torch.float32 else BF16,
                       ldx=_ld(x), lds=_ld(x_scales), ldo=_ld(out), x=_ptr(x), x_scales=_ptr(x_scales),
                       w=_ptr(w), w_scales=_ptr(w_scales), out=_ptr(out), workspace=_ptr(workspace),

@@ -520,3 +520,178 @@ def test_two_streams(sevo):
     torch.cuda.synchronize()
     for i in range(2):
         assert torch.equal(outs[i], want[i])
+
+
+# ------------------------------------------------------------------ other calls
+@pytest.mark.parametrize("m,n_out,k", [(2100, 8256, 384), (1500, 20544, 128), (700, 16448, 256),
+                                       (40, 16960, 256), (4700, 4160, 1024)])
+@pytest.mark.parametrize("dtype", [torch.float32, BF])
+def test_linear_fp8_more_tiles_than_cus(sevo, m, n_out, k, dtype):
+    """A workgroup takes several tiles: the next one's loads run under the stores of
+    the last, whole tiles and cut ones in turn."""
+    say(f"tiles {m} x {n_out} x {k} {dtype}")
+    g = gen(m + k)
+    xq, xs = quantised(normal((m, k), g))
+    wq, ws = weights((n_out, k), g)
+    out = torch.full((m + 1, n_out), 7.0, dtype=dtype, device="cuda")
+    y = sevo.sevo_linear_fp8(xq, xs, sevo.sevo_pack_weight_fp8(wq), ws, out=out[:m])
+    check_product(y, xq, xs, wq, ws)
+    assert (out[m] == 7.0).all()
+
+
+def test_linear_fp8_far_rows(sevo):
+    """Output rows 2^23 bytes and more apart, the last ones past 2^31 bytes."""
+    g = gen(5)
+    m, n_out, k, ld = 300, 320, 256, (1 << 22) + 4
+    xq, xs = quantised(normal((m, k), g))
+    wq, ws = weights((n_out, k), g)
+    out = torch.empty(m, ld, dtype=BF, device="cuda")[:, :n_out]
+    sevo.sevo_linear_fp8(xq, xs, sevo.sevo_pack_weight_fp8(wq), ws, out=out)
+    check_product(out.contiguous(), xq, xs, wq, ws)
+
+
+def check_experts(y, xq, xs, wq, ws, flat, top_k, wt, down):
+    """Rows [entries, n_out] of the experts' products against float64."""
+    X = values(xq, xs)
+    for e in range(wq.shape[0]):
+        i = torch.nonzero(flat == e).squeeze(1)
+        if not i.numel():
+            continue
+        W = weight_values(wq[e], ws[e])
+        Xe = X[i if down else i // top_k]
+        ref, mag = Xe @ W.t().contiguous(), Xe.abs() @ W.abs().t().contiguous()
+        if down:
+            p = wt.reshape(-1)[i].double().unsqueeze(1)
+            ref, mag = ref * p, mag * p
+        err = (y[i].double() - ref).abs()
+        assert (err <= ref.abs() * 2.0 ** -8 + mag * 2.0 ** -15).all(), f"expert {e} down {down}"
+
+
+@pytest.mark.parametrize("n,E,top_k,n_out,k", [
+    (20, 16, 2, 192, 256), (100, 16, 3, 320, 384), (250, 12, 2, 448, 256), (400, 8, 3, 192, 128),
+    (900, 6, 2, 576, 384), (9000, 16, 8, 192, 128), (3, 256, 16, 64, 128), (1, 2, 2, 128, 128)])
+def test_moe_linear_fp8_inside_buffers(sevo, n, E, top_k, n_out, k):
+    """Every tile height, n_out no multiple of 128, rows and scales inside larger
+    buffers, a token that has the same expert twice; 72000 entries (lists in more
+    than one launch)."""
+    say(f"experts in buffers n={n} E={E} top {top_k} {n_out} x {k}")
+    g = gen(n + E + k)
+    ex, wt = routing(n, E, top_k, g, "even")
+    if n > 10:
+        ex[5] = ex[5, 0]
+        ex[n - 1, 0] = 1 << 30
+    wq, ws = weights((E, n_out, k), g)
+    w = sevo.sevo_pack_weight_fp8(wq)
+    lists = sevo.sevo_moe_lists(ex, E, buffer=poisoned(sevo.sevo_moe_lists_bytes(n, top_k, E)))
+    flat = ex.reshape(-1)
+    for down in (False, True):
+        rows = n * top_k if down else n
+        xq, xs = quantised(normal((rows, k), g))
+        xb = torch.full((rows, k + 32), 0x7F, dtype=torch.uint8, device="cuda")
+        xb[:, 16:16 + k] = xq.view(torch.uint8)
+        sb = torch.full((k // 128, rows + 7), float("nan"), device="cuda")
+        sb[:, 2:2 + rows] = xs
+        out = torch.full((top_k, n, n_out) if down else (n * top_k, n_out), 7.0, dtype=BF, device="cuda")
+        y = sevo.sevo_moe_linear_fp8(xb.view(F8)[:, 16:16 + k], sb[:, 2:2 + rows], w, ws, lists,
+                                     weights=wt if down else None, out=out)
+        y = y.transpose(0, 1).reshape(n * top_k, n_out) if down else y
+        assert (y[flat >= E] == 7.0).all()
+        check_experts(y, xq, xs, wq, ws, flat, top_k, wt, down)
+
+
+@pytest.mark.parametrize("n,E,top_k,score,biased", [
+    (4099, 256, 16, "sigmoid", True), (2050, 128, 8, "softmax", False), (1027, 250, 11, "softmax", True)])
+def test_moe_route_near_ties(sevo, n, E, top_k, score, biased):
+    """Logits a few fp32 steps apart, where fp32 scores cannot tell which is larger."""
+    g = gen(E)
+    steps = torch.randint(0, 40, (n, E), device="cuda", generator=g).float()
+    logits = 0.7 + steps * 2.0 ** -23
+    logits[: n // 2] += normal((n // 2, 1), g)
+    bias = torch.randint(0, 3, (E,), device="cuda", generator=g).float() * 2.0 ** -22 if biased else None
+    ex, wt = sevo.sevo_moe_route(logits, top_k, score, bias, renormalise=True)
+    z = logits.double().cpu().numpy()
+    p = 1 / (1 + np.exp(-z)) if score == "sigmoid" else np.exp(z - z.max(1, keepdims=True))
+    if score == "softmax":
+        p = p / p.sum(1, keepdims=True)
+    c = p if bias is None else p + bias.double().cpu().numpy()
+    got = ex.cpu().numpy()
+    # exp in float64 is within a step of its value on either side: choices whose values
+    # are that near may stand either way, and are equal up to it
+    rank = np.sort(c, 1)[:, ::-1][:, :top_k]
+    mine = np.take_along_axis(c, got, 1)
+    assert np.abs(mine - rank).max() <= 8 * 2.0 ** -53
+    assert all(len(set(r)) == top_k for r in got)
+    w = np.take_along_axis(p, got, 1)
+    np.testing.assert_allclose(wt.cpu().numpy(), w / w.sum(1, keepdims=True), rtol=2.0 ** -23)
+
+
+def test_graphs(sevo):
+    """Two layers' chains captured in two graphs, replayed in turn with eager calls
+    between: every replay gives the eager bits."""
+    H, F, E, top, n = 512, 256, 32, 4, 96
+    g = gen(77)
+    wg, wd, wo = weights((E, 2 * F, H), g), weights((E, H, F), g), weights((H, 4 * H), g)
+    pg, pd, po = (sevo.sevo_pack_weight_fp8(w[0]) for w in (wg, wd, wo))
+    gain = normal((H,), g, 0.1, BF) + 1
+
+    def layer(s):
+        a, sa = sevo.sevo_quantize_fp8(s["attn"])
+        o = sevo.sevo_linear_fp8(a, sa, po, wo[1])
+        x = s["x"].clone()
+        q, qs = sevo.sevo_add_rmsnorm_fp8(x, o.unsqueeze(0), gain, 1e-6)
+        ex, wt = sevo.sevo_moe_route(s["logits"], top, "sigmoid", None, 4, 2, 1)
+        lists = sevo.sevo_moe_lists(ex, E)
+        gu = sevo.sevo_moe_linear_fp8(q, qs, pg, wg[1], lists)
+        d, ds = sevo.sevo_quantize_fp8(gu, swiglu=True)
+        part = sevo.sevo_moe_linear_fp8(d, ds, pd, wd[1], lists, weights=wt)
+        y, ys = sevo.sevo_add_rmsnorm_fp8(x, part, gain, 1e-6)
+        f = sevo.sevo_linear_fp8(a, sa, po, wo[1], out_dtype=torch.float32)
+        return x, y.view(torch.uint8), ys, ex, wt, f
+
+    def fill(s, seed):
+        h = gen(seed)
+        s["x"].copy_(normal((n, H), h))
+        s["attn"].copy_(normal((n, 4 * H), h, 1.0, BF))
+        s["logits"].copy_(normal((n, E), h, 1.5))
+
+    states, graphs, outs = [], [], []
+    for i in range(2):
+        s = {"x": torch.empty(n, H, device="cuda"), "attn": torch.empty(n, 4 * H, dtype=BF, device="cuda"),
+             "logits": torch.empty(n, E, device="cuda")}
+        fill(s, i)
+        layer(s)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = layer(s)
+        states.append(s), graphs.append(graph), outs.append(out)
+    for turn in range(4):
+        for i in range(2):
+            fill(states[i], 100 * turn + i)
+        want = [[t.clone() for t in layer(s)] for s in states]
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            for got, ref in zip(outs[i], want[i]):
+                assert torch.equal(got, ref), f"turn {turn}, graph {i}"
+
+
+def test_other_stream_order(sevo):
+    """A chain on a stream of its own, its inputs made there too, the current stream
+    busy with other work."""
+    g = gen(8)
+    n_out, k = 256, 1024
+    wq, ws = weights((n_out, k), g)
+    w = sevo.sevo_pack_weight_fp8(wq)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for m in (1, 30, 200):
+        with torch.cuda.stream(side):
+            x = normal((m, k), gen(m), 1.0, BF)
+            q, s = sevo.sevo_quantize_fp8(x)
+            y = sevo.sevo_linear_fp8(q, s, w, ws)
+        busy = torch.randn(2048, 2048, device="cuda") @ torch.randn(2048, 2048, device="cuda")
+        side.synchronize()
+        check_product(y, q, s, wq, ws)
+        assert torch.isfinite(busy).all()
