@@ -9,6 +9,7 @@ unloadable library raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import re
 
@@ -617,6 +618,8 @@ def sevo_moe_ffn(model: Model, layer: int, h_tiled, n: int, stream=None, partial
 def _need(name, t, dtype, shape=None, device=None, contiguous=True):
     """Raises ValueError unless t is a tensor of this type, shape and device, rows
     contiguous (``contiguous``: all of it)."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.device == device:
+        return  # the usual call, whose checks count beside a launch of 3 us
     types = dtype if isinstance(dtype, tuple) else (dtype,)
     if t.dtype not in types:
         raise ValueError(f"{name}: {t.dtype}, expected {' or '.join(map(str, types))}")
@@ -642,11 +645,12 @@ def _call(name, device, stream, *args):
         raise ValueError(f"{name}: tensors on {device}, expected a GPU")
     # the stream's handle alone: building a Stream object takes longer than the launch
     s = torch._C._cuda_getCurrentRawStream(i) if stream is None else _stream(stream)
-    if torch.cuda.current_device() == i:
-        status = getattr(lib(), name)(*args, s)
+    fn = getattr(_lib or lib(), name)
+    if torch._C._cuda_getDevice() == i:
+        status = fn(*args, s)
     else:
         with torch.cuda.device(i):
-            status = getattr(lib(), name)(*args, s)
+            status = fn(*args, s)
     if status != OK:
         _check(status)
 
@@ -663,25 +667,27 @@ def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16
     (bf16 [rows, cols]) receives the normed rows too."""
     rows, cols = x.shape
     dev = x.device
-    _need("x", x, torch.float32)
+    _need("x", x, torch.float32, (rows, cols), dev)
     _need("gain", gain, torch.bfloat16, (cols,), dev)
     S = 0
     if partials is not None and partials.shape[0] > 0:
         S = partials.shape[0]
-        _need("partials", partials, (torch.float32, torch.bfloat16), (S, rows, cols), dev)
+        _need("partials", partials, torch.bfloat16 if partials.dtype == torch.bfloat16 else
+              torch.float32, (S, rows, cols), dev)
     if out is None:
         out = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=dev)
+    else:
+        _need("out", out, torch.float8_e4m3fn, (rows, cols), dev)
     if scales is None:
         scales = torch.empty(cols // SCALE_BLOCK, rows, dtype=torch.float32, device=dev)
-    _need("out", out, torch.float8_e4m3fn, (rows, cols), dev)
-    _need("scales", scales, torch.float32, (cols // SCALE_BLOCK, rows), dev)
+    else:
+        _need("scales", scales, torch.float32, (cols // SCALE_BLOCK, rows), dev)
     if out_bf16 is not None:
         _need("out_bf16", out_bf16, torch.bfloat16, (rows, cols), dev)
     a = AddRmsnormFp8Args(
-        rows=rows, cols=cols, n_partials=S,
-        partial_type=BF16 if S and partials.dtype == torch.bfloat16 else F32, eps=float(eps),
-        x=_ptr(x), partials=_ptr(partials) if S else None, gain=_ptr(gain), out=_ptr(out),
-        scales=_ptr(scales), out_bf16=_ptr(out_bf16))
+        rows, cols, S, BF16 if S and partials.dtype == torch.bfloat16 else F32, float(eps), x.data_ptr(),
+        partials.data_ptr() if S else None, gain.data_ptr(), out.data_ptr(), scales.data_ptr(),
+        _ptr(out_bf16))
     _call("sevo_add_rmsnorm_fp8", dev, stream, C.byref(a))
     return out, scales
 
@@ -690,8 +696,8 @@ def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
     """bf16 rows [m, k] (row stride from the tensor) to codes float8_e4m3fn [m, k]
     and scales fp32 [k / 128, m]; with ``swiglu`` of silu(gate) * up, x [m, 2 k]
     holding the gate columns, then the up columns."""
-    _need("x", x, torch.bfloat16, contiguous=False)
     m, k = x.shape
+    _need("x", x, torch.bfloat16, (m, k), x.device, contiguous=False)
     if swiglu:
         if k % 2:
             raise ValueError("x: an odd number of gate and up columns")
@@ -699,12 +705,14 @@ def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
     dev = x.device
     if out is None:
         out = torch.empty(m, k, dtype=torch.float8_e4m3fn, device=dev)
+    else:
+        _need("out", out, torch.float8_e4m3fn, (m, k), dev)
     if scales is None:
         scales = torch.empty(k // SCALE_BLOCK, m, dtype=torch.float32, device=dev)
-    _need("out", out, torch.float8_e4m3fn, (m, k), dev)
-    _need("scales", scales, torch.float32, (k // SCALE_BLOCK, m), dev)
-    _call("sevo_quantize_fp8", dev, stream, _ptr(x), _ld(x), m, k, 1 if swiglu else 0, _ptr(out),
-          _ptr(scales))
+    else:
+        _need("scales", scales, torch.float32, (k // SCALE_BLOCK, m), dev)
+    _call("sevo_quantize_fp8", dev, stream, x.data_ptr(), _ld(x), m, k, 1 if swiglu else 0,
+          out.data_ptr(), scales.data_ptr())
     return out, scales
 
 
@@ -724,6 +732,7 @@ def sevo_pack_weight_fp8(src, dst=None, stream=None):
     return dst
 
 
+@functools.lru_cache(maxsize=1024)  # (a plan from the sizes alone)
 def sevo_linear_fp8_workspace_bytes(m, n_out, k) -> int:
     return int(lib().sevo_linear_fp8_workspace_bytes(m, n_out, k))
 
@@ -739,22 +748,22 @@ def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16
     m, k = x.shape
     n_out = w.shape[0]
     dev = x.device
-    _need("x", x, f8, contiguous=False)
+    _need("x", x, f8, (m, k), dev, contiguous=False)
     _need("x_scales", x_scales, torch.float32, (k // SCALE_BLOCK, m), dev, contiguous=False)
     _need("w", w, f8, (n_out, k), dev)
     _need("w_scales", w_scales, torch.float32, (-(-n_out // SCALE_BLOCK), k // SCALE_BLOCK), dev)
     if out is None:
         out = torch.empty(m, n_out, dtype=out_dtype, device=dev)
-    _need("out", out, (torch.float32, torch.bfloat16), (m, n_out), dev, contiguous=False)
+    _need("out", out, torch.bfloat16 if out.dtype == torch.bfloat16 else torch.float32, (m, n_out),
+          dev, contiguous=False)
     if workspace is None:
         need = sevo_linear_fp8_workspace_bytes(m, n_out, k)
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     else:
         _need("workspace", workspace, torch.uint8, None, dev)
-    a = LinearFp8Args(m=m, n_out=n_out, k=k, out_type=F32 if out.dtype == torch.float32 else BF16,
-                      ldx=_ld(x), lds=_ld(x_scales), ldo=_ld(out), x=_ptr(x), x_scales=_ptr(x_scales),
-                      w=_ptr(w), w_scales=_ptr(w_scales), out=_ptr(out), workspace=_ptr(workspace),
-                      workspace_bytes=0 if workspace is None else workspace.numel())
+    a = LinearFp8Args(m, n_out, k, F32 if out.dtype == torch.float32 else BF16, _ld(x), _ld(x_scales),
+                      _ld(out), x.data_ptr(), x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(),
+                      out.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel())
     _call("sevo_linear_fp8", dev, stream, C.byref(a))
     return out
 
@@ -768,23 +777,23 @@ def sevo_moe_route(logits, top_k, score="softmax", bias=None, n_groups=1, top_gr
     ``n_groups`` expert groups by the sum of their ``group_best`` best."""
     if score not in ("softmax", "sigmoid"):
         raise ValueError(f"score: {score!r}")
-    _need("logits", logits, torch.float32, contiguous=False)
     n, E = logits.shape
     dev = logits.device
+    _need("logits", logits, torch.float32, (n, E), dev, contiguous=False)
     if bias is not None:
         _need("bias", bias, torch.float32, (E,), dev)
     if out_experts is None:
         out_experts = torch.empty(n, top_k, dtype=torch.int32, device=dev)
+    else:
+        _need("out_experts", out_experts, torch.int32, (n, top_k), dev)
     if out_weights is None:
         out_weights = torch.empty(n, top_k, dtype=torch.float32, device=dev)
-    _need("out_experts", out_experts, torch.int32, (n, top_k), dev)
-    _need("out_weights", out_weights, torch.float32, (n, top_k), dev)
-    a = MoeRouteArgs(n=n, n_experts=E, top_k=int(top_k),
-                     score=ROUTE_SIGMOID if score == "sigmoid" else ROUTE_SOFTMAX,
-                     n_groups=int(n_groups), top_groups=int(top_groups),
-                     group_best=int(group_best), renormalise=1 if renormalise else 0,
-                     scaling=float(scaling), ld=_ld(logits), logits=_ptr(logits), bias=_ptr(bias),
-                     out_experts=_ptr(out_experts), out_weights=_ptr(out_weights))
+    else:
+        _need("out_weights", out_weights, torch.float32, (n, top_k), dev)
+    a = MoeRouteArgs(n, E, int(top_k), ROUTE_SIGMOID if score == "sigmoid" else ROUTE_SOFTMAX,
+                     int(n_groups), int(top_groups), int(group_best), 1 if renormalise else 0,
+                     float(scaling), _ld(logits),
+                     logits.data_ptr(), _ptr(bias), out_experts.data_ptr(), out_weights.data_ptr())
     _call("sevo_moe_route", dev, stream, C.byref(a))
     return out_experts, out_weights
 
@@ -803,12 +812,13 @@ def sevo_moe_lists_bytes(n, top_k, n_experts) -> int:
 def sevo_moe_lists(experts, n_experts, buffer=None, stream=None) -> MoeLists:
     """Entry lists of experts int32 [n, top_k] for ``sevo_moe_linear_fp8``.
     ``buffer``: a caller's uint8 buffer of sevo_moe_lists_bytes."""
-    _need("experts", experts, torch.int32)
     n, top_k = experts.shape
+    _need("experts", experts, torch.int32, (n, top_k), experts.device)
     if buffer is None:
         buffer = torch.empty(sevo_moe_lists_bytes(n, top_k, n_experts), dtype=torch.uint8,
                              device=experts.device)
-    _need("buffer", buffer, torch.uint8, None, experts.device)
+    else:
+        _need("buffer", buffer, torch.uint8, None, experts.device)
     _call("sevo_moe_lists", experts.device, stream, _ptr(experts), n, top_k, int(n_experts),
           _ptr(buffer), buffer.numel())
     return MoeLists(n, top_k, int(n_experts), buffer)
@@ -837,11 +847,11 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
     shape = (top_k, n, n_out) if down else (n * top_k, n_out)
     if out is None:
         out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
-    _need("out", out, torch.bfloat16, shape, dev)
-    a = MoeLinearFp8Args(n=n, top_k=top_k, n_experts=E, n_out=n_out, k=k, down=1 if down else 0,
-                         ldx=_ld(x), lds=_ld(x_scales), x=_ptr(x), x_scales=_ptr(x_scales), w=_ptr(w),
-                         w_scales=_ptr(w_scales), weights=_ptr(weights), lists=_ptr(lists.buffer),
-                         out=_ptr(out))
+    else:
+        _need("out", out, torch.bfloat16, shape, dev)
+    a = MoeLinearFp8Args(n, top_k, E, n_out, k, 1 if down else 0, _ld(x), _ld(x_scales), x.data_ptr(),
+                         x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(), _ptr(weights),
+                         lists.buffer.data_ptr(), out.data_ptr())
     _call("sevo_moe_linear_fp8", dev, stream, C.byref(a))
     return out
 
