@@ -408,38 +408,39 @@ hipError_t launch_moe_route8(const MoeRouteArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Entry lists in one launch: workgroup e reads every entry twice, once to count
-// those of lower experts (its list's first place) and its own, once to write its
-// own in order: each thread holds eight consecutive entries of a chunk, and an
-// entry's rank is the matches of the lanes and waves before it.  No sums pass
-// between workgroups, and nothing depends on scheduling.
-template <int T>
+// Entry lists in one launch: workgroup e reads every entry once and counts those of
+// lower experts (its list's first place) and its own; its own then go out in order.  A
+// wave holds 512 C consecutive entries in registers, a lane eight of each 512, and an
+// entry's rank is the matches of the waves, chunks and lanes before it: one barrier,
+// no sums between workgroups, and nothing depends on scheduling.
+template <int T, int C>
 __global__ __launch_bounds__(T) void moe_lists_kernel(const int32_t* __restrict__ sel, int nk, int E,
                                                       int32_t* __restrict__ offsets,
                                                       int32_t* __restrict__ assign) {
-  constexpr int W = T / 64, P = 8;  // entries a thread holds
+  constexpr int W = T / 64, P = 8;  // entries of a lane and chunk
   __shared__ int red[2][W];
-  const int e = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  auto load = [&](int c0, int (&v)[P]) {
-    const int i = c0 + P * tid;
+  const int e = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i0 = wave * 512 * C + P * lane;
+  int v[C][P];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int i = i0 + 512 * c;
     if (i + P <= nk) {
-      *reinterpret_cast<u32x4*>(&v[0]) = *reinterpret_cast<const u32x4*>(sel + i);
-      *reinterpret_cast<u32x4*>(&v[4]) = *reinterpret_cast<const u32x4*>(sel + i + 4);
+      *reinterpret_cast<u32x4*>(&v[c][0]) = *reinterpret_cast<const u32x4*>(sel + i);
+      *reinterpret_cast<u32x4*>(&v[c][4]) = *reinterpret_cast<const u32x4*>(sel + i + 4);
     } else {
 #pragma unroll
-      for (int j = 0; j < P; ++j) v[j] = i + j < nk ? sel[i + j] : -1;
-    }
-  };
-  int lower = 0, own = 0;
-  for (int c0 = 0; c0 < nk; c0 += P * T) {
-    int v[P];
-    load(c0, v);
-#pragma unroll
-    for (int j = 0; j < P; ++j) {
-      lower += (uint32_t)v[j] < (uint32_t)e;  // (a negative id is in no list)
-      own += v[j] == e;
+      for (int j = 0; j < P; ++j) v[c][j] = i + j < nk ? sel[i + j] : -1;
     }
   }
+  int lower = 0, own = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      lower += (uint32_t)v[c][j] < (uint32_t)e;  // (a negative id is in no list)
+      own += v[c][j] == e;
+    }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     lower += __shfl_xor(lower, o, kWave);
@@ -450,41 +451,33 @@ __global__ __launch_bounds__(T) void moe_lists_kernel(const int32_t* __restrict_
     red[1][wave] = own;
   }
   __syncthreads();
-  int first = 0, count = 0;
+  int first = 0, count = 0, at = 0;
 #pragma unroll
   for (int w = 0; w < W; ++w) {
+    if (w < wave) at += red[1][w];
     first += red[0][w];
     count += red[1][w];
   }
-  if (tid == 0) {
+  if (threadIdx.x == 0) {
     offsets[e] = first;
     if (e == E - 1) offsets[E] = first + count;
   }
-  if (count == 0) return;  // uniform
-  __syncthreads();
-  int buf = 0;
-  for (int c0 = 0; c0 < nk; c0 += P * T, buf ^= 1) {
-    int v[P];
-    load(c0, v);
-    const uint64_t below = (1ull << lane) - 1;
-    int rank = 0, total = 0;
+  at += first;
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    int rank = at, total = 0;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-      const uint64_t b = __ballot(v[j] == e);
+      const uint64_t b = __ballot(v[c][j] == e);
       rank += __popcll(b & below);
       total += __popcll(b);
     }
-    if (lane == 0) red[buf][wave] = total;
-    __syncthreads();  // (the other buffer's readers have passed the barrier before it is written)
-    int at = first + rank;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      if (w < wave) at += red[buf][w];
-      first += red[buf][w];
-    }
+    if (total == 0) continue;  // uniform over the wave
 #pragma unroll
     for (int j = 0; j < P; ++j)
-      if (v[j] == e) assign[at++] = c0 + P * tid + j;
+      if (v[c][j] == e) assign[rank++] = i0 + 512 * c + j;
+    at += total;
   }
 }
 
@@ -497,10 +490,13 @@ hipError_t launch_moe_lists(const int32_t* sel, int nk, int E, int32_t* offsets,
   if (nk == 0) return hipSuccess;
   if (nk > kOneLaunchEntries)
     return launch_moe_plan(sel, nk, E, offsets, assign, st, nullptr, 256, scratch);
-  if (nk <= 2048)
-    hipLaunchKernelGGL(moe_lists_kernel<256>, dim3(E), dim3(256), 0, st, sel, nk, E, offsets, assign);
-  else
-    hipLaunchKernelGGL(moe_lists_kernel<1024>, dim3(E), dim3(1024), 0, st, sel, nk, E, offsets, assign);
+  auto go = [&](auto kern, int threads) {
+    hipLaunchKernelGGL(kern, dim3(E), dim3(threads), 0, st, sel, nk, E, offsets, assign);
+  };
+  if (nk <= 2048) go(moe_lists_kernel<256, 1>, 256);
+  else if (nk <= 8192) go(moe_lists_kernel<1024, 1>, 1024);
+  else if (nk <= 32768) go(moe_lists_kernel<1024, 4>, 1024);
+  else go(moe_lists_kernel<1024, 8>, 1024);
   return hipGetLastError();
 }
 
