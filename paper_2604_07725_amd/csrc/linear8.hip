@@ -897,10 +897,11 @@ hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* wor
 }
 
 // Rows of a tile by the entries an expert has on average, 0: the stream (30B-A3B
-// gate/up and down, us, stream / tiles of 32 / 64 / 128 / 256 rows: 4 entries 65 + 35 /
-// 75 + 39; 8 85 + 48 / 77 + 43; 16 - / 83 + 49 / 84 + 51; 32 - / 97 + 52 / 92 + 55 / 100 + 59;
-// 64 - / - / 107 + 65 / 105 + 65 / 117 + 69; 128 - / - / 147 + 96 / 126 + 76 / 141 + 89; 256
-// - / - / - / 181 + 130 / 178 + 126).
+// gate/up + down, us, stream / tiles of 32 / 128 / 256 rows: 4 entries 65 + 35 / 73 + 40 /
+// 75 + 45 / 89 + 51; 8 82 + 48 / 75 + 44 / 78 + 47 / 88 + 51; 24 - / 80 + 49 / 82 + 50 / 87 + 56;
+// 32 - / 91 + 52 / 93 + 57 / 90 + 55; 64 - / 116 + 70 / 97 + 62 / 96 + 63; 128 - / - / 119 + 74 /
+// 125 + 82; 200 - / - / 149 + 103 / 153 + 99; 256 - / - / 173 + 122 / 166 + 111; 512 - / - / 288 +
+// 204 / 264 + 189).  64 rows were never the best by more than 2%.
 constexpr int kStreamEntries = 6;
 
 namespace {
@@ -921,7 +922,7 @@ hipError_t run_moe8(const Linear8Args& a, const Moe8Args& g, hipStream_t st) {
 
 static int moe8_tile_rows(const Moe8Args& g) {
   const int64_t per = ((int64_t)g.n * g.top_k + g.n_experts - 1) / g.n_experts;
-  return per <= kStreamEntries ? 0 : per <= 24 ? 32 : per <= 64 ? 64 : per <= 200 ? 128 : 256;
+  return per <= kStreamEntries ? 0 : per <= 40 ? 32 : per <= 200 ? 128 : 256;
 }
 
 hipError_t launch_moe8(const Moe8Args& g, hipStream_t st) {
@@ -934,7 +935,6 @@ hipError_t launch_moe8(const Moe8Args& g, hipStream_t st) {
       hipLaunchKernelGGL(moe8_kernel, dim3((g.n_out + 127) / 128, g.n_experts), dim3(256), 0, st, g);
       return hipGetLastError();
     case 32: return run_moe8<32, 256, 4, 2>(a, g, st);
-    case 64: return run_moe8<64, 128, 4, 3>(a, g, st);
     case 128: return run_moe8<128, 256, 8, 3>(a, g, st);
     default: return run_moe8<256, 256, 8, 2>(a, g, st);
   }
