@@ -13,6 +13,8 @@ namespace sevo {
 
 namespace {
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
 constexpr float kTop = 448.f;               // largest e4m3 value
 constexpr float kLeastScale = 0x1p-64f;     // of a block of zeros
 
@@ -27,7 +29,7 @@ __device__ __forceinline__ uint32_t row16_umax(uint32_t v) {
 // The 128 values of a block, eight in each of 16 neighbouring lanes, to codes
 // (returned, 8 bytes) and their scale.  Magnitudes are compared as integers:
 // the order of finite values, with infinities and NaNs above them.
-__device__ __forceinline__ uint2 block_codes(const float (&y)[8], float* scale) {
+__device__ __forceinline__ u32x2 block_codes(const float (&y)[8], float* scale) {
   uint32_t a = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(y[i]) & 0x7FFFFFFFu);
@@ -39,7 +41,7 @@ __device__ __forceinline__ uint2 block_codes(const float (&y)[8], float* scale) 
   lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inv, y[3] * inv, lo, true);
   int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4] * inv, y[5] * inv, 0, false);
   hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6] * inv, y[7] * inv, hi, true);
-  return uint2{(uint32_t)lo, (uint32_t)hi};
+  return u32x2{(uint32_t)lo, (uint32_t)hi};
 }
 
 __device__ __forceinline__ void unpack8(const u32x4& w, float (&v)[8]) {
@@ -55,7 +57,10 @@ __device__ __forceinline__ void unpack8(const u32x4& w, float (&v)[8]) {
 // Workgroup per row; thread t owns columns 8 (t + T g) .. + 8, g < NG, in
 // registers from the one read of x to the codes, so a block of 128 columns is 16
 // lanes of one wave.  T and NG follow from the columns alone: a row's bits do not
-// depend on the rows beside it.
+// depend on the rows beside it.  Bound by HBM from about 1000 rows on: in graphs,
+// 8192 x 2048 with eight bf16 partials 72.7 us (5.8 TB/s), 8192 x 4096 with one 55.2 (6.7
+// TB/s); 4 x 4096 3.5 us, of which the launch is 3.4.  Half the threads with twice the
+// columns each: 81.9, 55.0 and 4.0.
 template <int T, int NG, typename P>
 __global__ __launch_bounds__(T) void add_rmsnorm_fp8_kernel(AddNormFp8Args a) {
   __shared__ float red[T / 64];
@@ -109,8 +114,8 @@ __global__ __launch_bounds__(T) void add_rmsnorm_fp8_kernel(AddNormFp8Args a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = v[g][i] * inv * gn[i];
     float s;
-    const uint2 q = block_codes(y, &s);
-    *reinterpret_cast<uint2*>(a.out + (size_t)row * a.cols + c) = q;
+    const u32x2 q = block_codes(y, &s);
+    *reinterpret_cast<u32x2*>(a.out + (size_t)row * a.cols + c) = q;
     if ((threadIdx.x & 15) == 0) a.scales[(size_t)(c >> 7) * a.rows + row] = s;
     if (a.out_bf16) {
       u32x4 o;
@@ -142,8 +147,9 @@ hipError_t launch_add_rmsnorm_fp8(const AddNormFp8Args& a, hipStream_t st) {
 }
 
 // A wave takes four blocks (512 columns) of R consecutive rows, 16 lanes a
-// block.  Lane j of a block's 16 keeps row j's scale, so that the scales of 16
-// rows leave as one run of a [k/128][m] row.
+// block.  Lane j of a block's 16 keeps row j's scale, so that the scales of R
+// rows leave as one run of a [k/128][m] row.  Bound by HBM: 8192 x 12288 SwiGLU in a
+// graph 99 us, 5.1 TB/s.
 template <int R, bool SWIGLU>
 __global__ __launch_bounds__(256) void quantize_fp8_kernel(const bf16_t* __restrict__ x, int64_t ldx,
                                                            int m, int k, uint8_t* __restrict__ out,
@@ -169,7 +175,8 @@ __global__ __launch_bounds__(256) void quantize_fp8_kernel(const bf16_t* __restr
       for (int e = 0; e < 8; ++e) y[e] = y[e] / (1.f + __expf(-y[e])) * u[e];
     }
     float s;
-    *reinterpret_cast<uint2*>(out + (size_t)row * k + c) = block_codes(y, &s);
+    // past the caches (8192 x 4096 19.2 -> 18.3 us): the product that reads them comes later
+    __builtin_nontemporal_store(block_codes(y, &s), reinterpret_cast<u32x2*>(out + (size_t)row * k + c));
     if (j == i) keep = s;
   }
   if (j < R && r0 + j < m) scales[(size_t)(c >> 7) * m + r0 + j] = keep;
@@ -185,10 +192,14 @@ hipError_t launch_quantize_fp8(const bf16_t* x, int64_t ldx, int m, int k, int s
                        scales);
     return hipGetLastError();
   };
-  // a row per wave while that leaves few waves, else 16 for whole runs of scales
+  // A row per wave while that leaves the chip short of waves, else four, whose loads
+  // pass under each other and whose scales share a line (us in graphs, a row a wave / 2 /
+  // 4 / 8 / 16: 64 x 12288 SwiGLU 3.5 / 3.8 / 5.0 / 7.0 / 11.4; 1024 x 4096 4.6 / 4.6 / 4.9 / 6.3 /
+  // 9.5; 2048 x 4096, 16384 waves of a row, 6.6 / 6.4 / 6.4 / 7.1 / 10.2; 8192 x 12288 SwiGLU
+  // 108.5 / 103.4 / 99.1 / 104.7 / 110.7).
   if ((long)m * quads < 16384)
     return swiglu ? go(quantize_fp8_kernel<1, true>, 1) : go(quantize_fp8_kernel<1, false>, 1);
-  return swiglu ? go(quantize_fp8_kernel<16, true>, 16) : go(quantize_fp8_kernel<16, false>, 16);
+  return swiglu ? go(quantize_fp8_kernel<4, true>, 4) : go(quantize_fp8_kernel<4, false>, 4);
 }
 
 // Row-major codes [n][k] -> the packed layout, one thread per 16-byte run of dst.
