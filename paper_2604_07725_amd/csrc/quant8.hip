@@ -58,11 +58,12 @@ __device__ __forceinline__ void unpack8(const u32x4& w, float (&v)[8]) {
 // registers from the one read of x to the codes, so a block of 128 columns is 16
 // lanes of one wave.  T and NG follow from the columns alone: a row's bits do not
 // depend on the rows beside it.  Bound by HBM from about 1000 rows on: in graphs,
-// 8192 x 2048 with eight bf16 partials 72.7 us (5.8 TB/s), 8192 x 4096 with one 55.2 (6.7
+// 8192 x 2048 with eight bf16 partials 70 us (6.0 TB/s), 8192 x 4096 with one 54.9 (6.7
 // TB/s); 4 x 4096 3.5 us, of which the launch is 3.4.  Half the threads with twice the
-// columns each: 81.9, 55.0 and 4.0.
+// columns each: 82, 55.0 and 4.0 (for 73, 55.2 and 3.5).  Codes are stored past the caches
+// (8192 x 5120 with one partial 75.8 -> 67.7).
 template <int T, int NG, typename P>
-__global__ __launch_bounds__(T) void add_rmsnorm_fp8_kernel(AddNormFp8Args a) {
+__global__ __launch_bounds__(T) void add_rmsnorm_fp8_kernel(AddNormFp8Args a, int past_cache) {
   __shared__ float red[T / 64];
   const int row = xcd_row(blockIdx.x, gridDim.x);
   float* xr = a.x + (size_t)row * a.cols;
@@ -78,25 +79,34 @@ __global__ __launch_bounds__(T) void add_rmsnorm_fp8_kernel(AddNormFp8Args a) {
     *reinterpret_cast<f32x4*>(&v[g][4]) = *reinterpret_cast<const f32x4*>(xr + c + 4);
     if (a.n_partials > 0) {
       constexpr int kAtOnce = 4;  // partials loaded together, added in order
-      for (int s0 = 0; s0 < a.n_partials; s0 += kAtOnce) {
-        float p[kAtOnce][8];
+      auto add = [&](auto once) {
+        auto get = [&](const P* src) {
+          const u32x4* q = reinterpret_cast<const u32x4*>(src);
+          if constexpr (decltype(once)::value) return __builtin_nontemporal_load(q);
+          else return *q;
+        };
+        for (int s0 = 0; s0 < a.n_partials; s0 += kAtOnce) {
+          float p[kAtOnce][8];
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j)
-          if (s0 + j < a.n_partials) {
-            const P* src = pr + (s0 + j) * plane + c;
-            if constexpr (sizeof(P) == 2) {
-              unpack8(*reinterpret_cast<const u32x4*>(src), p[j]);
-            } else {
-              *reinterpret_cast<f32x4*>(&p[j][0]) = *reinterpret_cast<const f32x4*>(src);
-              *reinterpret_cast<f32x4*>(&p[j][4]) = *reinterpret_cast<const f32x4*>(src + 4);
+          for (int j = 0; j < kAtOnce; ++j)
+            if (s0 + j < a.n_partials) {
+              const P* src = pr + (s0 + j) * plane + c;
+              if constexpr (sizeof(P) == 2) {
+                unpack8(get(src), p[j]);
+              } else {
+                *reinterpret_cast<u32x4*>(&p[j][0]) = get(src);
+                *reinterpret_cast<u32x4*>(&p[j][4]) = get(src + 4);
+              }
             }
-          }
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j)
-          if (s0 + j < a.n_partials)
+          for (int j = 0; j < kAtOnce; ++j)
+            if (s0 + j < a.n_partials)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[g][i] += p[j][i];
-      }
+              for (int i = 0; i < 8; ++i) v[g][i] += p[j][i];
+        }
+      };
+      if (past_cache) add(std::true_type{});
+      else add(std::false_type{});
       *reinterpret_cast<f32x4*>(xr + c) = *reinterpret_cast<f32x4*>(&v[g][0]);
       *reinterpret_cast<f32x4*>(xr + c + 4) = *reinterpret_cast<f32x4*>(&v[g][4]);
     }
@@ -115,7 +125,7 @@ __global__ __launch_bounds__(T) void add_rmsnorm_fp8_kernel(AddNormFp8Args a) {
     for (int i = 0; i < 8; ++i) y[i] = v[g][i] * inv * gn[i];
     float s;
     const u32x2 q = block_codes(y, &s);
-    *reinterpret_cast<u32x2*>(a.out + (size_t)row * a.cols + c) = q;
+    __builtin_nontemporal_store(q, reinterpret_cast<u32x2*>(a.out + (size_t)row * a.cols + c));
     if ((threadIdx.x & 15) == 0) a.scales[(size_t)(c >> 7) * a.rows + row] = s;
     if (a.out_bf16) {
       u32x4 o;
@@ -128,12 +138,19 @@ __global__ __launch_bounds__(T) void add_rmsnorm_fp8_kernel(AddNormFp8Args a) {
 
 hipError_t launch_add_rmsnorm_fp8(const AddNormFp8Args& a, hipStream_t st) {
   if (a.rows == 0) return hipSuccess;
+  // Partials are read past the caches once a call's data cannot stay in the last-level
+  // one (256 MiB) anyway: there they would push out x, which the next norm reads (us,
+  // plain / past the caches: 235 MB, 8192 x 4096 and one partial, 54.9 / 59.4; 302 MB, two,
+  // 64.0 / 68.5; 352 MB, 8192 x 2048 and eight, 70.3 / 70.1 and with new partials each call
+  // 80.6 / 68.8; 436 MB 95.3 / 88.5; 705 MB 158 / 133).
+  const int past_cache =
+      (size_t)a.rows * a.cols * (5 + (size_t)a.n_partials * (a.partials_bf16 ? 2 : 4)) > (size_t)320 << 20;
   auto go = [&](auto t_tag, auto ng_tag) {
     constexpr int T = decltype(t_tag)::value, NG = decltype(ng_tag)::value;
     if (a.partials_bf16)
-      hipLaunchKernelGGL((add_rmsnorm_fp8_kernel<T, NG, bf16_t>), dim3(a.rows), dim3(T), 0, st, a);
+      hipLaunchKernelGGL((add_rmsnorm_fp8_kernel<T, NG, bf16_t>), dim3(a.rows), dim3(T), 0, st, a, past_cache);
     else
-      hipLaunchKernelGGL((add_rmsnorm_fp8_kernel<T, NG, float>), dim3(a.rows), dim3(T), 0, st, a);
+      hipLaunchKernelGGL((add_rmsnorm_fp8_kernel<T, NG, float>), dim3(a.rows), dim3(T), 0, st, a, past_cache);
     return hipGetLastError();
   };
   using std::integral_constant;

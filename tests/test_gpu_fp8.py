@@ -695,3 +695,23 @@ def test_other_stream_order(sevo):
         side.synchronize()
         check_product(y, q, s, wq, ws)
         assert torch.isfinite(busy).all()
+
+
+@pytest.mark.parametrize("rows,cols,S,ptype", [(8300, 2048, 8, BF), (4100, 4096, 5, torch.float32),
+                                               (9000, 4096, 3, BF)])
+def test_add_rmsnorm_fp8_larger_than_the_cache(sevo, rows, cols, S, ptype):
+    """More data than the last-level cache holds: the bits of calls on fewer rows."""
+    say(f"norm {rows} x {cols}, {S} partials {ptype}")
+    g = gen(S)
+    x = normal((rows, cols), g, 2.0)
+    parts = torch.randn(S, rows, cols, device="cuda", generator=g).to(ptype)
+    gain = normal((cols,), g, 0.1, BF) + 1
+    want = []
+    for r0 in range(0, rows, 1024):
+        xp = x[r0:r0 + 1024].clone()
+        q, s = sevo.sevo_add_rmsnorm_fp8(xp, parts[:, r0:r0 + 1024].contiguous(), gain, 1e-6)
+        want.append((xp, q.view(torch.uint8), s))
+    q, s = sevo.sevo_add_rmsnorm_fp8(x, parts, gain, 1e-6)
+    assert torch.equal(x, torch.cat([w[0] for w in want]))
+    assert torch.equal(q.view(torch.uint8), torch.cat([w[1] for w in want]))
+    assert torch.equal(s, torch.cat([w[2] for w in want], 1))
