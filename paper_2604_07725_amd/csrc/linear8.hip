@@ -90,12 +90,13 @@ __device__ __forceinline__ void store4(void* out, size_t off, const f32x4& v, in
 
 // Direct global -> LDS load of N bytes per lane at voff (checked against the
 // records) + soff (wave-uniform, not checked); lane i's bytes land at lds + N i.
-template <int N>
+// ONCE: data that nothing else reads, past the caches.
+template <int N, bool ONCE = false>
 __device__ __forceinline__ void dma_s(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t soff,
                                       uint8_t* lds) {
   static_assert(N == 16 || N == 4, "bytes per lane");
   const auto dst = (__attribute__((address_space(3))) void*)lds;
-  if constexpr (N == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, (int)voff, (int)soff, 0, 0);
+  if constexpr (N == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, (int)voff, (int)soff, 0, ONCE ? 2 : 0);
   else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 4, (int)voff, (int)soff, 0, 0);
 }
 
@@ -107,12 +108,17 @@ __device__ __forceinline__ void dma_s(__amdgpu_buffer_rsrc_t r, uint32_t voff, u
 // fragments of contiguous 1 KB; the activations and their scales go through the
 // wave's own LDS ring by direct loads of whole 128-byte rows (gathered per lane
 // in fragment order they came at 16 bytes per clock and CU: 64 x 4096 x 4096 in M
-// tiles of 64 13.6 -> 10.5 us, 32 x 4096 x 4096 8.7 -> 7.5).  Three step buffers: two steps in flight under the products.
+// tiles of 64 13.6 -> 10.5 us, 32 x 4096 x 4096 8.7 -> 7.5).  Two steps are in flight under
+// the products of a third (three or four: no faster, 16 x 6144 x 4096 7.6 / 7.6 / 8.2).
+// Measured in graphs, weights cold: 8 x 51200 x 5120 52.7 us (5.0 TB/s), 16 x 6144 x 4096 7.6
+// (3.3), of which 3.4 a launch; from 32 rows on the CU's path from L2 bounds it, on which
+// the activations come too: 64 x 4096 x 12288 19.2 (2.7).
 template <int MB, int RB, bool EXACT>
 __global__ __launch_bounds__(256, 1) void linear8_kernel(Linear8Args a, int kb_chunk,
                                                          float* __restrict__ part) {
   constexpr int kStepBytes = MB * 2048 + 256;            // a step's rows and their scales
-  constexpr int kRing = 4 * 3 * kStepBytes, kRed = 4 * RB * MB * 1024;
+  constexpr int ND = 3;  // step buffers
+  constexpr int kRing = 4 * ND * kStepBytes, kRed = 4 * RB * MB * 1024;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kRing > kRed ? kRing : kRed];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -126,13 +132,10 @@ __global__ __launch_bounds__(256, 1) void linear8_kernel(Linear8Args a, int kb_c
 #pragma unroll
   for (int i = 0; i < RB; ++i) {
     const int rb = rb0 + i < nrb ? rb0 + i : 0;
-    wp[i] = a.w + ((size_t)(rb >> 2) * KB * 4 + (rb & 3)) * 2048 + lane * 16;
+    wp[i] = a.w + ((size_t)(rb >> 2) * KB * 4 + (rb & 3)) * 2048;
   }
-  auto rsrc = [](const void* p) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7FFFFFFF, 0x00020000);
-  };
   // place p of row r holds run p ^ (r / 2 % 8): see tile8_kernel
-  const __amdgpu_buffer_rsrc_t xr = rsrc(a.x + (size_t)m0 * a.ldx), sr = rsrc(a.xs + m0);
+  const uint8_t* xb = a.x + (size_t)m0 * a.ldx;
   uint32_t x_voff[2 * MB];
 #pragma unroll
   for (int f = 0; f < 2 * MB; ++f)
@@ -153,20 +156,24 @@ __global__ __launch_bounds__(256, 1) void linear8_kernel(Linear8Args a, int kb_c
     float sw0, sw1;
   };
   constexpr int kLoads = 2 * MB + 1 + 2 * RB;  // vector loads of a step
-  uint8_t* ring = smem + wave * 3 * kStepBytes;
-  // j-th step of this wave into buffer `slot`; past the end it re-reads the last one
+  uint8_t* ring = smem + wave * ND * kStepBytes;
+  // j-th step of this wave into buffer `slot`; past the end the descriptors have no
+  // records, and nothing is read
   auto load = [&](Step& f, int slot, int j) {
     const int st = st0 + wave + 4 * min(j, cnt - 1);
+    const int records = j < cnt ? 0x7FFFFFFF : 0;
+    auto rsrc = [&](const void* p) {
+      return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, records, 0x00020000);
+    };
     uint8_t* so = ring + slot * kStepBytes;
 #pragma unroll
-    for (int b = 0; b < 2 * MB; ++b) dma_s<16>(xr, x_voff[b], st * 128u, so + 1024 * b);
-    dma_s<4>(sr, s_voff, (uint32_t)st * (uint32_t)a.lds * 4u, so + 2048 * MB);
+    for (int b = 0; b < 2 * MB; ++b) dma_s<16>(rsrc(xb), x_voff[b], st * 128u, so + 1024 * b);
+    dma_s<4>(rsrc(a.xs + m0), s_voff, (uint32_t)st * (uint32_t)a.lds * 4u, so + 2048 * MB);
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        f.w[i].u[h] = __builtin_nontemporal_load(
-            reinterpret_cast<const u32x4*>(wp[i] + (size_t)st * 8192 + 1024 * h));
+      for (int h = 0; h < 2; ++h)  // (read once: past the caches)
+        f.w[i].u[h] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(wp[i]), lane * 16 + 1024 * h, st * 8192, 2);
     f.sw0 = ws0[st];
     f.sw1 = ws1[st];
     __builtin_amdgcn_sched_barrier(0);
@@ -177,7 +184,7 @@ __global__ __launch_bounds__(256, 1) void linear8_kernel(Linear8Args a, int kb_c
 #pragma unroll
     for (int b = 0; b < MB; ++b) acc[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto mma = [&](const Step& f, int slot) {
-    wait_vmcnt<2 * kLoads>();  // the step's loads; the next two steps' may still run
+    wait_vmcnt<(ND - 1) * kLoads>();  // the step's loads; the next steps' may still run
     __builtin_amdgcn_sched_barrier(0);
     const uint8_t* so = ring + slot * kStepBytes;
 #pragma unroll
@@ -197,17 +204,16 @@ __global__ __launch_bounds__(256, 1) void linear8_kernel(Linear8Args a, int kb_c
     __builtin_amdgcn_sched_barrier(0);
   };
   if (cnt > 0) {
-    Step f0, f1, f2;
-    load(f0, 0, 0);
-    load(f1, 1, 1);
-    for (int j = 0; j < cnt; j += 3) {
-      load(f2, 2, j + 2);
-      mma(f0, 0);
-      load(f0, 0, j + 3);
-      if (j + 1 < cnt) mma(f1, 1);
-      load(f1, 1, j + 4);
-      if (j + 2 < cnt) mma(f2, 2);
-    }
+    Step f[ND];
+#pragma unroll
+    for (int b = 0; b < ND - 1; ++b) load(f[b], b, b);
+    for (int j = 0; j < cnt; j += ND)
+#pragma unroll
+      for (int b = 0; b < ND; ++b) {
+        constexpr int kBack = ND - 1;
+        load(f[(b + kBack) % ND], (b + kBack) % ND, j + b + kBack);
+        if (j + b < cnt) mma(f[b], b);
+      }
   }
   wait_vmcnt<0>();  // the direct loads past the end have left the ring
   __syncthreads();
@@ -255,6 +261,7 @@ __global__ __launch_bounds__(256) void linear8_sum_kernel(const float* __restric
 // whole k, a workgroup 128 rows (one row of weight scales); the expert's entries come
 // 16 at a time, gathered through its list (more than 16 read its weights again,
 // mostly from a cache).
+// 30B-A3B gate/up of 64 tokens, 8 of 128 experts each: 63 us, 6.3 TB/s.
 __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -490,7 +497,11 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     for (int i = 0; i <= D; ++i) {
       if (i < i0 || i >= i1) continue;
       if (i < DW) {
-        dma_s<16>(rsrc(wb), lane * 16, (st0 + st) * 8192 + w_soff[i], so + BM * 128 + (wave + NW * i) * 1024);
+        // (an expert with so few entries has one tile, and its weights are read once: 12
+        // entries an expert 81.5 + 51 -> 77.5 + 47 us; with tiles that share them it costs
+        // 5%)
+        dma_s<16, GR && BM == 32>(rsrc(wb), lane * 16, (st0 + st) * 8192 + w_soff[i],
+                                  so + BM * 128 + (wave + NW * i) * 1024);
       } else if (i == DW + XH) {
         dma_s<4>(rsrc(sb), s_voff, st * s_step, so + kScales + 256 * wave);
       } else {
@@ -897,12 +908,13 @@ hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* wor
 }
 
 // Rows of a tile by the entries an expert has on average, 0: the stream (30B-A3B
-// gate/up + down, us, stream / tiles of 32 / 128 / 256 rows: 4 entries 65 + 35 / 73 + 40 /
-// 75 + 45 / 89 + 51; 8 82 + 48 / 75 + 44 / 78 + 47 / 88 + 51; 24 - / 80 + 49 / 82 + 50 / 87 + 56;
-// 32 - / 91 + 52 / 93 + 57 / 90 + 55; 64 - / 116 + 70 / 97 + 62 / 96 + 63; 128 - / - / 119 + 74 /
-// 125 + 82; 200 - / - / 149 + 103 / 153 + 99; 256 - / - / 173 + 122 / 166 + 111; 512 - / - / 288 +
-// 204 / 264 + 189).  64 rows were never the best by more than 2%.
-constexpr int kStreamEntries = 6;
+// gate/up + down, us, stream / tiles of 32 / 128 / 256 rows: 1 entry 40 + 22 / 40 + 28 / 48 + 31;
+// 4 63 + 35 / 68 + 37 / 72 + 45 / 89 + 51; 5 71 + 38 / 70 + 39 / 74 + 45; 8 82 + 48 / 70 + 40 / 77 +
+// 46 / 88 + 51; 24 - / 79 + 47 / 81 + 50 / 87 + 56; 32 - / 92 + 53 / 93 + 57 / 90 + 55; 40 - / 98 +
+// 60 / 94 + 59; 64 - / 116 + 70 / 97 + 62 / 96 + 63; 128 - / - / 119 + 74 / 125 + 82; 200 - / - /
+// 149 + 103 / 153 + 99; 256 - / - / 173 + 122 / 166 + 111; 512 - / - / 288 + 204 / 264 + 189).  64
+// rows were never the best by more than 2%.
+constexpr int kStreamEntries = 4;
 
 namespace {
 
@@ -922,7 +934,7 @@ hipError_t run_moe8(const Linear8Args& a, const Moe8Args& g, hipStream_t st) {
 
 static int moe8_tile_rows(const Moe8Args& g) {
   const int64_t per = ((int64_t)g.n * g.top_k + g.n_experts - 1) / g.n_experts;
-  return per <= kStreamEntries ? 0 : per <= 40 ? 32 : per <= 200 ? 128 : 256;
+  return per <= kStreamEntries ? 0 : per <= 32 ? 32 : per <= 200 ? 128 : 256;
 }
 
 hipError_t launch_moe8(const Moe8Args& g, hipStream_t st) {
