@@ -588,7 +588,7 @@ size_t sevo_moe_workspace_bytes(const sevo_model* m, int32_t n);
  *   weights codes packed by sevo_pack_weight_fp8; scales fp32
  *           [ceil(n_out / 128)][k / 128], row-major: one for each 128 x 128 block.
  * Quantisation of a block y of 128 values: s = max(max |y| / 448, 2^-64), code =
- * y / s rounded to nearest even.  A block that holds a NaN or an infinity gets
+ * y / s (y times the fp32 reciprocal of s) rounded to nearest even.  A block that holds a NaN or an infinity gets
  * the scale NaN and NaN codes, and so does every product that reads it. */
 #define SEVO_F32 0
 #define SEVO_BF16 1
