@@ -447,7 +447,7 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
 
   // ---- this wave's direct loads of a stage (D pieces and 64 scales): three
   // descriptors, offsets of the lane and of the piece and stage (scalar).  Every
-  // offset is in range (rows are clamped; 256 ldx and 256 k are below 2^31); past
+  // offset of a row is in range (256 ldx and 256 k are below 2^31); past
   // the last stage the descriptors have no records, so that the loop issues without
   // a branch and nothing is read.
   const uint8_t* xb;   // what the X, W and scale offsets count from
@@ -458,7 +458,7 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     const int base = GR ? 0 : p.m0;
     xb = a.x + (size_t)base * a.ldx;
     wb = a.w + (size_t)p.expert * a.n_out * a.k + (size_t)(p.n0 >> 6) * KB * 8192;
-    auto x_row = [&](int entry, int i) {  // row i of the tile's matrix (past the end: the last)
+    auto x_row = [&](int entry, int i) {  // row i of the tile's matrix (scales past the end: the last)
       if constexpr (GR) return g.down ? entry : entry / g.top_k;
       else return min(p.m0 + i, p.rows - 1);
     };
@@ -466,7 +466,12 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     for (int i = 0; i < XD; ++i) {
       const int f = piece(i);
       const int run = (lane & 7) ^ (4 * (f & 1) + (lane >> 4));
-      x_voff[i] = (uint32_t)((size_t)(x_row(idx[i], 8 * f + (lane >> 3)) - base) * a.ldx) + 16 * run;
+      const int row = 8 * f + (lane >> 3);
+      // Rows past the end: every dword of the lane is past the records, nothing is read and
+      // zeros arrive (8192 tokens of 30B-A3B experts 262 + 189 us with the last row again in
+      // their place, 255 + 186 so).
+      x_voff[i] = p.m0 + row < p.rows ? (uint32_t)((size_t)(x_row(idx[i], row) - base) * a.ldx) + 16 * run
+                                      : 0x80000000u;
     }
 #pragma unroll
     for (int i = 0; i < D - XD; ++i) {
