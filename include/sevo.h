@@ -643,12 +643,13 @@ sevo_status sevo_pack_weight_fp8(const void* src, void* dst, int64_t n_out, int3
  * norm + RoPE + append and the sampler, which read fp32); SEVO_BF16: out bf16 (for
  * the partials of sevo_add_rmsnorm_fp8 and for sevo_quantize_fp8), the inner
  * sums within 2e-5 of the block's largest, by the faster 8-bit matrix instructions.
- *   x [m][k], row stride ldx bytes (>= k, a multiple of 16, below 2^23); x_scales row stride
- *   lds (>= m); w packed; out row stride ldo elements (>= n_out, a multiple of 4).
- * n_out % 64 == 0, k % 128 == 0; x_scales below 2^31 bytes.  The workspace
- * is scratch of sevo_linear_fp8_workspace_bytes (0: may be NULL): calls that may overlap in time each need
- * their own.  The same call gives the same bits; the bits of a row may depend on
- * m (its plan).  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */
+ *   x [m][k], row stride ldx bytes (>= k, a multiple of 16, below 2^23); x_scales
+ *   row stride lds (>= m); w packed; out row stride ldo elements (>= n_out, a
+ *   multiple of 4).
+ * n_out % 64 == 0, k % 128 == 0; x_scales below 2^31 bytes.  The workspace is
+ * scratch of sevo_linear_fp8_workspace_bytes (0: may be NULL); calls that may
+ * overlap in time each need their own.  The same call gives the same bits; the
+ * bits of a row may depend on m (its plan).  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */
 typedef struct {
   int32_t m, n_out, k, out_type;
   int64_t ldx, lds, ldo;
