@@ -767,32 +767,32 @@ namespace {
 
 constexpr int kCUs = 256;
 
-// What a plan takes (us), fitted to 10471 timings of 20 row counts from 1 to 4096
-// and 16 matrices of 0.1 to 262 MB, weights cold, in graphs (8% rms; the plan with
-// the least is 1 to 2% slower than the best of all on average, 32% at worst: 48 x
-// 5120 x 8192 20.6 for 15.6).  LDS tiles: rounds of `cap` workgroups, a stage per
-// 128-column block, dearer on a full chip, the operands' bytes, and with a K
-// split the sum kernel and its partials.
+// What a plan takes (us), fitted to the timings within twice the best of their product,
+// of 10471 of 20 row counts from 1 to 4096 and 16 matrices of 0.1 to 262 MB, weights cold,
+// in graphs (7 to 12% rms; the plan with the least is 1.3% slower than the best of all
+// on average, 23% at worst: 48 x 5120 x 8192 19.2 for 15.6).  LDS tiles: rounds of `cap`
+// workgroups, a stage per 128-column block, dearer on a full chip, the operands' bytes,
+// and with a K split the sum kernel and its partials.
 struct TileCost {
   int bm, bn, cap;
   double fixed, round, stage, load, per_mb, split, split_mb;
 };
 constexpr TileCost kBf16Tiles[] = {
-    {256, 256, kCUs, 3.9, 1.7, 1.23, 0.33, 0.0, 4.3, 0.32},
-    {128, 256, kCUs, 3.3, 2.1, 0.69, 0.17, 0.033, 4.1, 0.31},
-    {128, 128, kCUs, 3.5, 1.2, 0.40, 0.11, 0.035, 3.0, 0.39},
-    {64, 256, kCUs, 3.3, 1.1, 0.51, 0.085, 0.069, 2.5, 0.39},
-    {64, 128, 2 * kCUs, 3.3, 1.2, 0.38, 0.27, 0.052, 1.9, 0.49}};
+    {256, 256, kCUs, 3.53, 2.29, 1.11, 0.288, 0.0, 2.18, 0.378},
+    {128, 256, kCUs, 2.83, 2.53, 0.675, 0.176, 0.031, 4.08, 0.311},
+    {128, 128, kCUs, 3.89, 0.818, 0.377, 0.141, 0.031, 2.98, 0.376},
+    {64, 256, kCUs, 4.0, 0.807, 0.443, 0.141, 0.074, 2.16, 0.392},
+    {64, 128, 2 * kCUs, 3.89, 0.73, 0.342, 0.321, 0.05, 1.97, 0.463}};
 constexpr TileCost kF32Tiles[] = {
     {},
-    {128, 256, kCUs, 6.0, 1.8, 1.42, 0.23, 0.0, 2.0, 0.33},
-    {128, 128, kCUs, 4.8, 1.4, 0.76, 0.15, 0.007, 1.9, 0.40},
-    {64, 256, kCUs, 4.7, 1.0, 0.89, 0.14, 0.017, 1.8, 0.41},
-    {64, 128, 2 * kCUs, 4.4, 0.65, 0.65, 0.45, 0.016, 1.6, 0.53}};
+    {128, 256, kCUs, 6.79, 1.81, 1.26, 0.339, 0.0, 1.03, 0.329},
+    {128, 128, kCUs, 5.69, 0.651, 0.669, 0.224, 0.0, 1.45, 0.423},
+    {64, 256, kCUs, 6.1, 0.0, 0.756, 0.304, 0.0, 0.928, 0.468},
+    {64, 128, 2 * kCUs, 4.89, 0.273, 0.601, 0.504, 0.015, 1.53, 0.529}};
 // The stream, in one round of a workgroup per CU (in more it starts and drains again):
 // each wave takes every fourth step.
-constexpr double kStreamFixed = 4.0, kStreamBlock = 0.149, kStreamPair = 0.024, kStreamMB = 0.064,
-                 kStreamSplit = 1.8, kStreamSplitMB = 1.25;
+constexpr double kStreamFixed = 4.0, kStreamBlock = 0.119, kStreamPair = 0.037, kStreamMB = 0.060,
+                 kStreamSplit = 1.75, kStreamSplitMB = 0.85;
 constexpr int kStreamRB[] = {1, 2, 3, 4, 6};
 
 }  // namespace
