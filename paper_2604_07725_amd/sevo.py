@@ -615,34 +615,33 @@ def sevo_moe_ffn(model: Model, layer: int, h_tiled, n: int, stream=None, partial
 
 
 # ------------------------------------------------------------------ 8-bit layers
-def _need(name, t, dtype, shape=None, device=None, contiguous=True):
-    """Raises ValueError unless t is a tensor of this type, shape and device, rows
-    contiguous (``contiguous``: all of it)."""
-    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.device == device:
+def _need(name, t, dtype, shape, device, contiguous=True):
+    """Raises ValueError unless t is a tensor of this type, shape (None: any) and
+    device index, rows contiguous (``contiguous``: all of it)."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device:
         return  # the usual call, whose checks count beside a launch of 3 us
-    types = dtype if isinstance(dtype, tuple) else (dtype,)
-    if t.dtype not in types:
-        raise ValueError(f"{name}: {t.dtype}, expected {' or '.join(map(str, types))}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name}: on {t.device}, expected {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, expected {f'cuda:{device}' if device >= 0 else 'cpu'}")
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
     if not contiguous and t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
 
 
-def _ld(t):
+def _ld(t, rows, cols):
     """Row stride of a 2-d tensor (one row has none of its own)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    ld = t.stride()[0]
+    return ld if rows > 1 else max(ld, cols)
 
 
-def _call(name, device, stream, *args):
-    """The C call on the tensors' device, by default on its current stream."""
-    i = device.index
-    if i is None:
-        raise ValueError(f"{name}: tensors on {device}, expected a GPU")
+def _call(name, i, stream, *args):
+    """The C call on device i, by default on its current stream."""
+    if i < 0:
+        raise ValueError(f"{name}: tensors on the CPU, expected a GPU")
     # the stream's handle alone: building a Stream object takes longer than the launch
     s = torch._C._cuda_getCurrentRawStream(i) if stream is None else _stream(stream)
     fn = getattr(_lib or lib(), name)
@@ -666,29 +665,28 @@ def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16
     float8_e4m3fn [rows, cols] and scales fp32 [cols / 128, rows].  ``out_bf16``
     (bf16 [rows, cols]) receives the normed rows too."""
     rows, cols = x.shape
-    dev = x.device
-    _need("x", x, torch.float32, (rows, cols), dev)
-    _need("gain", gain, torch.bfloat16, (cols,), dev)
-    S = 0
-    if partials is not None and partials.shape[0] > 0:
-        S = partials.shape[0]
-        _need("partials", partials, torch.bfloat16 if partials.dtype == torch.bfloat16 else
-              torch.float32, (S, rows, cols), dev)
+    dev, i = x.device, x.get_device()
+    _need("x", x, torch.float32, (rows, cols), i)
+    _need("gain", gain, torch.bfloat16, (cols,), i)
+    S = 0 if partials is None else partials.shape[0]
+    bf16 = S > 0 and partials.dtype is torch.bfloat16
+    if S:
+        _need("partials", partials, torch.bfloat16 if bf16 else torch.float32, (S, rows, cols), i)
     if out is None:
         out = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=dev)
     else:
-        _need("out", out, torch.float8_e4m3fn, (rows, cols), dev)
+        _need("out", out, torch.float8_e4m3fn, (rows, cols), i)
     if scales is None:
         scales = torch.empty(cols // SCALE_BLOCK, rows, dtype=torch.float32, device=dev)
     else:
-        _need("scales", scales, torch.float32, (cols // SCALE_BLOCK, rows), dev)
+        _need("scales", scales, torch.float32, (cols // SCALE_BLOCK, rows), i)
     if out_bf16 is not None:
-        _need("out_bf16", out_bf16, torch.bfloat16, (rows, cols), dev)
+        _need("out_bf16", out_bf16, torch.bfloat16, (rows, cols), i)
     a = AddRmsnormFp8Args(
-        rows, cols, S, BF16 if S and partials.dtype == torch.bfloat16 else F32, float(eps), x.data_ptr(),
+        rows, cols, S, BF16 if bf16 else F32, float(eps), x.data_ptr(),
         partials.data_ptr() if S else None, gain.data_ptr(), out.data_ptr(), scales.data_ptr(),
-        _ptr(out_bf16))
-    _call("sevo_add_rmsnorm_fp8", dev, stream, C.byref(a))
+        None if out_bf16 is None else out_bf16.data_ptr())
+    _call("sevo_add_rmsnorm_fp8", i, stream, C.byref(a))
     return out, scales
 
 
@@ -697,21 +695,22 @@ def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
     and scales fp32 [k / 128, m]; with ``swiglu`` of silu(gate) * up, x [m, 2 k]
     holding the gate columns, then the up columns."""
     m, k = x.shape
-    _need("x", x, torch.bfloat16, (m, k), x.device, contiguous=False)
+    dev, i = x.device, x.get_device()
+    _need("x", x, torch.bfloat16, (m, k), i, contiguous=False)
+    ldx = _ld(x, m, k)
     if swiglu:
         if k % 2:
             raise ValueError("x: an odd number of gate and up columns")
         k //= 2
-    dev = x.device
     if out is None:
         out = torch.empty(m, k, dtype=torch.float8_e4m3fn, device=dev)
     else:
-        _need("out", out, torch.float8_e4m3fn, (m, k), dev)
+        _need("out", out, torch.float8_e4m3fn, (m, k), i)
     if scales is None:
         scales = torch.empty(k // SCALE_BLOCK, m, dtype=torch.float32, device=dev)
     else:
-        _need("scales", scales, torch.float32, (k // SCALE_BLOCK, m), dev)
-    _call("sevo_quantize_fp8", dev, stream, x.data_ptr(), _ld(x), m, k, 1 if swiglu else 0,
+        _need("scales", scales, torch.float32, (k // SCALE_BLOCK, m), i)
+    _call("sevo_quantize_fp8", i, stream, x.data_ptr(), ldx, m, k, 1 if swiglu else 0,
           out.data_ptr(), scales.data_ptr())
     return out, scales
 
@@ -721,14 +720,14 @@ def sevo_pack_weight_fp8(src, dst=None, stream=None):
     layer) -> a new tensor of the same shape in the packed 8-bit layout."""
     if src.dim() not in (2, 3):
         raise ValueError("src: [n_out, k] or [E, n_out, k]")
-    _need("src", src, torch.float8_e4m3fn)
+    _need("src", src, torch.float8_e4m3fn, None, src.get_device())
     if src.shape[-2] % 64:
         raise ValueError("src: n_out must be a multiple of 64")
     if dst is None:
         dst = torch.empty_like(src)
-    _need("dst", dst, torch.float8_e4m3fn, src.shape, src.device)
+    _need("dst", dst, torch.float8_e4m3fn, src.shape, src.get_device())
     k = src.shape[-1]
-    _call("sevo_pack_weight_fp8", src.device, stream, _ptr(src), _ptr(dst), src.numel() // max(k, 1), k)
+    _call("sevo_pack_weight_fp8", src.get_device(), stream, _ptr(src), _ptr(dst), src.numel() // max(k, 1), k)
     return dst
 
 
@@ -744,27 +743,34 @@ def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16
     scales [ceil(n_out / 128), k / 128].  Y bf16, or fp32 (``out_dtype``, or the
     type of ``out``, whose row stride is kept).  ``workspace``: a caller's uint8
     buffer of sevo_linear_fp8_workspace_bytes (else one is allocated)."""
-    f8 = torch.float8_e4m3fn
+    f8, f32t = torch.float8_e4m3fn, torch.float32
     m, k = x.shape
     n_out = w.shape[0]
-    dev = x.device
-    _need("x", x, f8, (m, k), dev, contiguous=False)
-    _need("x_scales", x_scales, torch.float32, (k // SCALE_BLOCK, m), dev, contiguous=False)
-    _need("w", w, f8, (n_out, k), dev)
-    _need("w_scales", w_scales, torch.float32, (-(-n_out // SCALE_BLOCK), k // SCALE_BLOCK), dev)
+    kb = k // SCALE_BLOCK
+    dev, i = x.device, x.get_device()
+    _need("x", x, f8, (m, k), i, contiguous=False)
+    _need("x_scales", x_scales, f32t, (kb, m), i, contiguous=False)
+    _need("w", w, f8, (n_out, k), i)
+    _need("w_scales", w_scales, f32t, (-(-n_out // SCALE_BLOCK), kb), i)
+    kind = out_dtype if out is None else out.dtype
+    if kind is not torch.bfloat16 and kind is not f32t:
+        raise ValueError(f"out: {kind}, expected torch.float32 or torch.bfloat16")
     if out is None:
-        out = torch.empty(m, n_out, dtype=out_dtype, device=dev)
-    _need("out", out, torch.bfloat16 if out.dtype == torch.bfloat16 else torch.float32, (m, n_out),
-          dev, contiguous=False)
-    if workspace is None:
-        need = sevo_linear_fp8_workspace_bytes(m, n_out, k)
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        out, ldo = torch.empty(m, n_out, dtype=kind, device=dev), n_out
     else:
-        _need("workspace", workspace, torch.uint8, None, dev)
-    a = LinearFp8Args(m, n_out, k, F32 if out.dtype == torch.float32 else BF16, _ld(x), _ld(x_scales),
-                      _ld(out), x.data_ptr(), x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(),
-                      out.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel())
-    _call("sevo_linear_fp8", dev, stream, C.byref(a))
+        _need("out", out, kind, (m, n_out), i, contiguous=False)
+        ldo = _ld(out, m, n_out)
+    if workspace is not None:
+        _need("workspace", workspace, torch.uint8, None, i)
+        need = workspace.numel()
+    else:
+        need = sevo_linear_fp8_workspace_bytes(m, n_out, k)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    a = LinearFp8Args(m, n_out, k, F32 if kind is f32t else BF16, _ld(x, m, k), _ld(x_scales, kb, m),
+                      ldo, x.data_ptr(), x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(),
+                      out.data_ptr(), None if workspace is None else workspace.data_ptr(), need)
+    _call("sevo_linear_fp8", i, stream, C.byref(a))
     return out
 
 
@@ -778,23 +784,23 @@ def sevo_moe_route(logits, top_k, score="softmax", bias=None, n_groups=1, top_gr
     if score not in ("softmax", "sigmoid"):
         raise ValueError(f"score: {score!r}")
     n, E = logits.shape
-    dev = logits.device
-    _need("logits", logits, torch.float32, (n, E), dev, contiguous=False)
+    dev, i = logits.device, logits.get_device()
+    _need("logits", logits, torch.float32, (n, E), i, contiguous=False)
     if bias is not None:
-        _need("bias", bias, torch.float32, (E,), dev)
+        _need("bias", bias, torch.float32, (E,), i)
     if out_experts is None:
         out_experts = torch.empty(n, top_k, dtype=torch.int32, device=dev)
     else:
-        _need("out_experts", out_experts, torch.int32, (n, top_k), dev)
+        _need("out_experts", out_experts, torch.int32, (n, top_k), i)
     if out_weights is None:
         out_weights = torch.empty(n, top_k, dtype=torch.float32, device=dev)
     else:
-        _need("out_weights", out_weights, torch.float32, (n, top_k), dev)
+        _need("out_weights", out_weights, torch.float32, (n, top_k), i)
     a = MoeRouteArgs(n, E, int(top_k), ROUTE_SIGMOID if score == "sigmoid" else ROUTE_SOFTMAX,
                      int(n_groups), int(top_groups), int(group_best), 1 if renormalise else 0,
-                     float(scaling), _ld(logits),
+                     float(scaling), _ld(logits, n, E),
                      logits.data_ptr(), _ptr(bias), out_experts.data_ptr(), out_weights.data_ptr())
-    _call("sevo_moe_route", dev, stream, C.byref(a))
+    _call("sevo_moe_route", i, stream, C.byref(a))
     return out_experts, out_weights
 
 
@@ -813,13 +819,14 @@ def sevo_moe_lists(experts, n_experts, buffer=None, stream=None) -> MoeLists:
     """Entry lists of experts int32 [n, top_k] for ``sevo_moe_linear_fp8``.
     ``buffer``: a caller's uint8 buffer of sevo_moe_lists_bytes."""
     n, top_k = experts.shape
-    _need("experts", experts, torch.int32, (n, top_k), experts.device)
+    i = experts.get_device()
+    _need("experts", experts, torch.int32, (n, top_k), i)
     if buffer is None:
         buffer = torch.empty(sevo_moe_lists_bytes(n, top_k, n_experts), dtype=torch.uint8,
                              device=experts.device)
     else:
-        _need("buffer", buffer, torch.uint8, None, experts.device)
-    _call("sevo_moe_lists", experts.device, stream, _ptr(experts), n, top_k, int(n_experts),
+        _need("buffer", buffer, torch.uint8, None, i)
+    _call("sevo_moe_lists", i, stream, _ptr(experts), n, top_k, int(n_experts),
           _ptr(buffer), buffer.numel())
     return MoeLists(n, top_k, int(n_experts), buffer)
 
@@ -835,24 +842,25 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
     down = weights is not None
     rows, k = x.shape
     n_out = w.shape[1]
-    dev = x.device
-    _need("x", x, f8, (n * top_k if down else n, k), contiguous=False)
-    _need("x_scales", x_scales, torch.float32, (k // SCALE_BLOCK, rows), dev, contiguous=False)
-    _need("w", w, f8, (E, n_out, k), dev)
+    dev, i = x.device, x.get_device()
+    _need("x", x, f8, (n * top_k if down else n, k), i, contiguous=False)
+    _need("x_scales", x_scales, torch.float32, (k // SCALE_BLOCK, rows), i, contiguous=False)
+    _need("w", w, f8, (E, n_out, k), i)
     _need("w_scales", w_scales, torch.float32,
-          (E, -(-n_out // SCALE_BLOCK), k // SCALE_BLOCK), dev)
-    _need("lists", lists.buffer, torch.uint8, None, dev)
+          (E, -(-n_out // SCALE_BLOCK), k // SCALE_BLOCK), i)
+    _need("lists", lists.buffer, torch.uint8, None, i)
     if down:
-        _need("weights", weights, torch.float32, (n, top_k), dev)
+        _need("weights", weights, torch.float32, (n, top_k), i)
     shape = (top_k, n, n_out) if down else (n * top_k, n_out)
     if out is None:
         out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
     else:
-        _need("out", out, torch.bfloat16, shape, dev)
-    a = MoeLinearFp8Args(n, top_k, E, n_out, k, 1 if down else 0, _ld(x), _ld(x_scales), x.data_ptr(),
+        _need("out", out, torch.bfloat16, shape, i)
+    a = MoeLinearFp8Args(n, top_k, E, n_out, k, 1 if down else 0, _ld(x, rows, k),
+                         _ld(x_scales, k // SCALE_BLOCK, rows), x.data_ptr(),
                          x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(), _ptr(weights),
                          lists.buffer.data_ptr(), out.data_ptr())
-    _call("sevo_moe_linear_fp8", dev, stream, C.byref(a))
+    _call("sevo_moe_linear_fp8", i, stream, C.byref(a))
     return out
 
 
