@@ -112,7 +112,9 @@ __device__ __forceinline__ void dma_s(__amdgpu_buffer_rsrc_t r, uint32_t voff, u
 // the products of a third (three or four: no faster, 16 x 6144 x 4096 7.6 / 7.6 / 8.2).
 // Measured in graphs, weights cold: 8 x 51200 x 5120 52.7 us (5.0 TB/s), 16 x 6144 x 4096 7.6
 // (3.3), of which 3.4 a launch; from 32 rows on the CU's path from L2 bounds it, on which
-// the activations come too: 64 x 4096 x 12288 19.2 (2.7).
+// the activations come too: 64 x 4096 x 12288 19.2 (2.7).  M tiles of 64 rows read the
+// weights half as often as those of 32: 64 x 10240 x 5120 to fp32 24.1 -> 20.4 (LDS tiles
+// before), 128 x 6144 x 4096 to fp32 19.9 -> 15.5, 203 x 4096 x 4096 16.2 -> 14.3.
 template <int MB, int RB, bool EXACT>
 __global__ __launch_bounds__(256, 1) void linear8_kernel(Linear8Args a, int kb_chunk,
                                                          float* __restrict__ part) {
@@ -768,9 +770,9 @@ namespace {
 constexpr int kCUs = 256;
 
 // What a plan takes (us), fitted to the timings within twice the best of their product,
-// of 10471 of 20 row counts from 1 to 4096 and 16 matrices of 0.1 to 262 MB, weights cold,
-// in graphs (7 to 12% rms; the plan with the least is 1.3% slower than the best of all
-// on average, 23% at worst: 48 x 5120 x 8192 19.2 for 15.6).  LDS tiles: rounds of `cap`
+// of 14916 of 24 row counts from 1 to 4096 and 16 matrices of 0.1 to 262 MB, weights cold,
+// in graphs (7 to 12% rms; the plan with the least is 1.4% slower than the best of all
+// on average, 23% at worst: 48 x 5120 x 25600 37.5 for 30.4).  LDS tiles: rounds of `cap`
 // workgroups, a stage per 128-column block, dearer on a full chip, the operands' bytes,
 // and with a K split the sum kernel and its partials.
 struct TileCost {
@@ -791,8 +793,8 @@ constexpr TileCost kF32Tiles[] = {
     {64, 128, 2 * kCUs, 4.89, 0.273, 0.601, 0.504, 0.015, 1.53, 0.529}};
 // The stream, in one round of a workgroup per CU (in more it starts and drains again):
 // each wave takes every fourth step.
-constexpr double kStreamFixed = 4.0, kStreamBlock = 0.119, kStreamPair = 0.037, kStreamMB = 0.060,
-                 kStreamSplit = 1.75, kStreamSplitMB = 0.85;
+constexpr double kStreamFixed = 4.15, kStreamBlock = 0.095, kStreamPair = 0.055, kStreamMB = 0.055,
+                 kStreamSplit = 1.7, kStreamSplitMB = 0.88;
 constexpr int kStreamRB[] = {1, 2, 3, 4, 6};
 
 }  // namespace
@@ -805,9 +807,9 @@ Linear8Plan plan_linear8(int m, int n_out, int k, int out_bf16) {
   for (int want : {1, 2, 3, 4, 6, 8}) {
     if (want > 1 && KB < 2 * want) break;
     const int chunk = (KB + want - 1) / want, s = (KB + chunk - 1) / chunk;
-    for (int mb = 1; mb <= 2 && want <= 4; ++mb)
+    for (int mb = 1; mb <= 4 && want <= 4; mb *= 2)
       for (int rb : kStreamRB) {
-        if (mb == 2 && (rb > 4 || m <= 16)) continue;
+        if (mb > 1 && (rb > 4 || m <= 8 * mb)) continue;
         const int64_t wgs = (int64_t)((m + 16 * mb - 1) / (16 * mb)) * ((n_out / 16 + rb - 1) / rb) * s;
         if (wgs > kCUs) continue;
         const int steps = (chunk + 3) / 4;
@@ -903,7 +905,10 @@ hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* wor
     case 3: e = run_tile8<128, 128, 8, 4>(a, p, part, st); break;
     case 4: e = run_tile8<64, 256, 8, 3>(a, p, part, st); break;
     case 5: e = run_tile8<64, 128, 4, 3>(a, p, part, st); break;
-    default: e = p.mb == 1 ? run_stream<1>(a, p, part, st) : run_stream<2>(a, p, part, st);
+    default:
+      e = p.mb == 1   ? run_stream<1>(a, p, part, st)
+          : p.mb == 2 ? run_stream<2>(a, p, part, st)
+                      : run_stream<4>(a, p, part, st);
   }
   if (e != hipSuccess || !part) return e;
   const size_t blocks = ((size_t)a.m * a.n_out / 4 + 255) / 256;

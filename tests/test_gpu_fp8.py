@@ -715,3 +715,19 @@ def test_add_rmsnorm_fp8_larger_than_the_cache(sevo, rows, cols, S, ptype):
     assert torch.equal(x, torch.cat([w[0] for w in want]))
     assert torch.equal(q.view(torch.uint8), torch.cat([w[1] for w in want]))
     assert torch.equal(s, torch.cat([w[2] for w in want], 1))
+
+
+@pytest.mark.parametrize("m,n_out,k", [(33, 5120, 25600), (64, 10240, 5120), (81, 8192, 2048), (128, 6144, 4096),
+                                       (192, 4096, 4096), (203, 2048, 768), (256, 512, 256)])
+@pytest.mark.parametrize("dtype", [torch.float32, BF])
+def test_linear_fp8_middle_rows(sevo, m, n_out, k, dtype):
+    """Row counts between a few and many, with one to four M tiles of 64 rows, the last
+    one cut."""
+    say(f"middle {m} x {n_out} x {k} {dtype}")
+    g = gen(m + n_out)
+    xq, xs = quantised(normal((m, k), g))
+    wq, ws = weights((n_out, k), g)
+    out = torch.full((m + 2, n_out), 7.0, dtype=dtype, device="cuda")
+    y = sevo.sevo_linear_fp8(xq, xs, sevo.sevo_pack_weight_fp8(wq), ws, out=out[:m])
+    check_product(y, xq, xs, wq, ws)
+    assert (out[m:] == 7.0).all()
