@@ -771,7 +771,7 @@ constexpr int kCUs = 256;
 
 // What a plan takes (us), fitted to the timings within twice the best of their product,
 // of 14916 of 24 row counts from 1 to 4096 and 16 matrices of 0.1 to 262 MB, weights cold,
-// in graphs (7 to 12% rms; the plan with the least is 1.4% slower than the best of all
+// in graphs (7 to 12% rms; the plan with the least is 1.1% slower than the best of all
 // on average, 23% at worst: 48 x 5120 x 25600 37.5 for 30.4).  LDS tiles: rounds of `cap`
 // workgroups, a stage per 128-column block, dearer on a full chip, the operands' bytes,
 // and with a K split the sum kernel and its partials.
@@ -792,9 +792,10 @@ constexpr TileCost kF32Tiles[] = {
     {64, 256, kCUs, 6.1, 0.0, 0.756, 0.304, 0.0, 0.928, 0.468},
     {64, 128, 2 * kCUs, 4.89, 0.273, 0.601, 0.504, 0.015, 1.53, 0.529}};
 // The stream, in one round of a workgroup per CU (in more it starts and drains again):
-// each wave takes every fourth step.
-constexpr double kStreamFixed = 4.15, kStreamBlock = 0.095, kStreamPair = 0.055, kStreamMB = 0.055,
-                 kStreamSplit = 1.7, kStreamSplitMB = 0.88;
+// each wave takes every fourth step, whose time is that of its loads, 2 KB for each block
+// of weight rows and of activation rows.
+constexpr double kStreamFixed = 3.93, kStreamW = 0.156, kStreamX = 0.126, kStreamMB = 0.028,
+                 kStreamSplit = 1.86, kStreamSplitMB = 1.04;
 constexpr int kStreamRB[] = {1, 2, 3, 4, 6};
 
 }  // namespace
@@ -813,7 +814,7 @@ Linear8Plan plan_linear8(int m, int n_out, int k, int out_bf16) {
         const int64_t wgs = (int64_t)((m + 16 * mb - 1) / (16 * mb)) * ((n_out / 16 + rb - 1) / rb) * s;
         if (wgs > kCUs) continue;
         const int steps = (chunk + 3) / 4;
-        const double us = kStreamFixed + steps * rb * (kStreamBlock + kStreamPair * mb) + kStreamMB * mbytes +
+        const double us = kStreamFixed + steps * (kStreamW * rb + kStreamX * mb) + kStreamMB * mbytes +
                           (s > 1 ? kStreamSplit + kStreamSplitMB * s * out_mb : 0.0);
         if (us < best_us) {
           best_us = us;
