@@ -617,9 +617,9 @@ def sevo_moe_ffn(model: Model, layer: int, h_tiled, n: int, stream=None, partial
 # ------------------------------------------------------------------ 8-bit layers
 def _need(name, t, dtype, shape, device, contiguous=True):
     """Raises ValueError unless t is a tensor of this type, shape (None: any) and
-    device index, rows contiguous (``contiguous``: all of it)."""
-    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device:
-        return  # the usual call, whose checks count beside a launch of 3 us
+    device index, rows contiguous (``contiguous``: all of it).  The callers ask for the
+    usual tensors in one condition first: a call of this for each takes as long as
+    a tenth of the launch."""
     if t.dtype != dtype:
         raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
     if shape is not None and tuple(t.shape) != tuple(shape):
@@ -666,11 +666,14 @@ def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16
     (bf16 [rows, cols]) receives the normed rows too."""
     rows, cols = x.shape
     dev, i = x.device, x.get_device()
-    _need("x", x, torch.float32, (rows, cols), i)
-    _need("gain", gain, torch.bfloat16, (cols,), i)
+    if not (x.dtype is torch.float32 and x.is_contiguous() and gain.dtype is torch.bfloat16 and
+            gain.shape == (cols,) and gain.is_contiguous() and gain.get_device() == i):
+        _need("x", x, torch.float32, (rows, cols), i)
+        _need("gain", gain, torch.bfloat16, (cols,), i)
     S = 0 if partials is None else partials.shape[0]
     bf16 = S > 0 and partials.dtype is torch.bfloat16
-    if S:
+    if S and not (bf16 and partials.shape == (S, rows, cols) and partials.is_contiguous() and
+                  partials.get_device() == i):
         _need("partials", partials, torch.bfloat16 if bf16 else torch.float32, (S, rows, cols), i)
     if out is None:
         out = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=dev)
@@ -696,7 +699,8 @@ def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
     holding the gate columns, then the up columns."""
     m, k = x.shape
     dev, i = x.device, x.get_device()
-    _need("x", x, torch.bfloat16, (m, k), i, contiguous=False)
+    if not (x.dtype is torch.bfloat16 and x.is_contiguous()):
+        _need("x", x, torch.bfloat16, (m, k), i, contiguous=False)
     ldx = _ld(x, m, k)
     if swiglu:
         if k % 2:
@@ -748,10 +752,16 @@ def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16
     n_out = w.shape[0]
     kb = k // SCALE_BLOCK
     dev, i = x.device, x.get_device()
-    _need("x", x, f8, (m, k), i, contiguous=False)
-    _need("x_scales", x_scales, f32t, (kb, m), i, contiguous=False)
-    _need("w", w, f8, (n_out, k), i)
-    _need("w_scales", w_scales, f32t, (-(-n_out // SCALE_BLOCK), kb), i)
+    if not (x.dtype is f8 and x.is_contiguous() and
+            x_scales.dtype is f32t and x_scales.shape == (kb, m) and x_scales.is_contiguous() and
+            w.dtype is f8 and w.shape == (n_out, k) and w.is_contiguous() and
+            w_scales.dtype is f32t and w_scales.shape == (-(-n_out // SCALE_BLOCK), kb) and
+            w_scales.is_contiguous() and
+            x_scales.get_device() == w.get_device() == w_scales.get_device() == i):
+        _need("x", x, f8, (m, k), i, contiguous=False)
+        _need("x_scales", x_scales, f32t, (kb, m), i, contiguous=False)
+        _need("w", w, f8, (n_out, k), i)
+        _need("w_scales", w_scales, f32t, (-(-n_out // SCALE_BLOCK), kb), i)
     kind = out_dtype if out is None else out.dtype
     if kind is not torch.bfloat16 and kind is not f32t:
         raise ValueError(f"out: {kind}, expected torch.float32 or torch.bfloat16")
@@ -785,7 +795,8 @@ def sevo_moe_route(logits, top_k, score="softmax", bias=None, n_groups=1, top_gr
         raise ValueError(f"score: {score!r}")
     n, E = logits.shape
     dev, i = logits.device, logits.get_device()
-    _need("logits", logits, torch.float32, (n, E), i, contiguous=False)
+    if not (logits.dtype is torch.float32 and logits.is_contiguous()):
+        _need("logits", logits, torch.float32, (n, E), i, contiguous=False)
     if bias is not None:
         _need("bias", bias, torch.float32, (E,), i)
     if out_experts is None:
