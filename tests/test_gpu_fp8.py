@@ -731,3 +731,39 @@ def test_linear_fp8_middle_rows(sevo, m, n_out, k, dtype):
     y = sevo.sevo_linear_fp8(xq, xs, sevo.sevo_pack_weight_fp8(wq), ws, out=out[:m])
     check_product(y, xq, xs, wq, ws)
     assert (out[m:] == 7.0).all()
+
+
+def test_mixed_calls_on_four_streams(sevo):
+    """Products of every kind, routings and quantisers at once, in changing company:
+    always the bits of the same call alone."""
+    g = gen(21)
+    jobs = []
+    for m, n_out, k, dtype in ((700, 4096, 1024, BF), (64, 4096, 4096, BF), (2100, 2048, 768, BF),
+                               (203, 5120, 2048, torch.float32), (16, 6144, 4096, torch.float32)):
+        q, s = quantised(normal((m, k), g))
+        wq, ws = weights((n_out, k), g)
+        w = sevo.sevo_pack_weight_fp8(wq)
+        jobs.append(lambda q=q, s=s, w=w, ws=ws, d=dtype: sevo.sevo_linear_fp8(q, s, w, ws, out_dtype=d))
+    for n, E, top, n_out, k in ((900, 16, 4, 512, 384), (64, 64, 8, 768, 512), (300, 16, 4, 512, 512)):
+        ex, _ = routing(n, E, top, g, "even")
+        wq, ws = weights((E, n_out, k), g)
+        w = sevo.sevo_pack_weight_fp8(wq)
+        q, s = quantised(normal((n, k), g))
+        jobs.append(lambda ex=ex, E=E, q=q, s=s, w=w, ws=ws:
+                    sevo.sevo_moe_linear_fp8(q, s, w, ws, sevo.sevo_moe_lists(ex, E)))
+    logits, rows = normal((3000, 256), g, 1.5), normal((2000, 4096), g, 1.0, BF)
+    jobs.append(lambda: sevo.sevo_moe_route(logits, 8, "sigmoid", None, 8, 4, 2)[1])
+    jobs.append(lambda: sevo.sevo_quantize_fp8(rows)[0].view(torch.uint8))
+    want = [f() for f in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    rng = np.random.default_rng(4)
+    for turn in range(12):
+        got = []
+        for stream in streams:
+            with torch.cuda.stream(stream):
+                for j in rng.integers(0, len(jobs), 5):
+                    got.append((j, jobs[j]()))
+        torch.cuda.synchronize()
+        for j, t in got:
+            assert torch.equal(t, want[j]), f"turn {turn}, call {j}"
