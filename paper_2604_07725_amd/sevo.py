@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import inspect
 import os
 import re
 
@@ -223,6 +224,47 @@ def _stream(stream):
     return vp(stream)
 
 
+def _tensors(values):
+    """The tensors among values, tuples of them and entry lists."""
+    for v in values:
+        if isinstance(v, torch.Tensor):
+            yield v
+        elif isinstance(v, tuple):
+            yield from _tensors(v)
+        elif isinstance(v, MoeLists):
+            yield v.buffer
+
+
+def _on_its_stream(fn):
+    """A call with ``stream`` (a torch.cuda.Stream or a raw handle) allocates and
+    fills on that stream too.  The allocator hands memory out in the order of the
+    stream it is asked on: a workspace that belonged to the current stream would be
+    given to the next call while this one's kernels still use it.  What is returned
+    is marked as used by the current stream as well, where the caller may read it;
+    inputs are the caller's to keep until the stream has read them."""
+    at = list(inspect.signature(fn).parameters).index("stream")
+
+    @functools.wraps(fn)
+    def call(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return fn(*args, **kw)
+        device = next((t.device for t in _tensors((*args, *kw.values()))), None)
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(getattr(stream, "value", stream) or 0, device=device)
+        elif device is not None and stream.device != device:
+            raise ValueError(f"stream: of {stream.device}, the tensors on {device}")
+        current = torch.cuda.current_stream(device)
+        with torch.cuda.stream(stream):
+            out = fn(*args, **kw)
+        if current.cuda_stream != stream.cuda_stream:
+            for t in _tensors((out,)):
+                t.record_stream(current)
+        return out
+
+    return call
+
+
 def _p(t):
     return None if t is None else vp(t.data_ptr())
 
@@ -243,6 +285,7 @@ def sevo_attn_workspace_bytes(n, n_q_heads, n_kv_heads, head_dim, max_pages, num
                                                num_splits))
 
 
+@_on_its_stream
 def sevo_attn_decode(q, kv_pool, page_table, seq_lens, out=None, scale=None,
                      num_splits=0, workspace=None, stream=None):
     """o = paged GQA decode attention.  q [n, hq, d] bf16; kv_pool in the paged
@@ -279,6 +322,7 @@ def sevo_attn_decode_noalloc(q, kv_pool, page_table, seq_lens, out, scale=None, 
 
 
 # ------------------------------------------------------------------ prefill
+@_on_its_stream
 def sevo_attn_prefill(q, kv_pool, page_table, seq_starts, max_seq_len, start_pos=None, out=None,
                       scale=None, stream=None):
     """Causal GQA prefill attention.  q [T, hq, d] bf16 (sequences back to back);
@@ -305,6 +349,7 @@ def sevo_sample_workspace_bytes(n: int, vocab: int) -> int:
     return int(lib().sevo_sample_workspace_bytes(n, vocab))
 
 
+@_on_its_stream
 def sevo_logprob_sample(logits, temperature, seed, cand_uid, positions, out_tokens=None,
                         out_logprobs=None, workspace=None, stream=None, vocab=None,
                         conf_topk=0, out_conf=None, conf_sum=None, top_k=0, top_p=1.0,
@@ -335,6 +380,7 @@ def sevo_logprob_sample(logits, temperature, seed, cand_uid, positions, out_toke
     return out_tokens, out_logprobs
 
 
+@_on_its_stream
 def sevo_group_confidence(conf_sum, token_counts, groups, out=None, stream=None):
     """GC [n_groups] from per-candidate confidence sums, token counts (int32)
     and groups int32 [n_groups, K] of candidate indices."""
@@ -347,6 +393,7 @@ def sevo_group_confidence(conf_sum, token_counts, groups, out=None, stream=None)
 
 
 # ------------------------------------------------------------------ sub-steps
+@_on_its_stream
 def sevo_embed(embed, tokens, x=None, stream=None):
     n = tokens.shape[0]
     hidden = embed.shape[1]
@@ -357,6 +404,7 @@ def sevo_embed(embed, tokens, x=None, stream=None):
     return x
 
 
+@_on_its_stream
 def sevo_rmsnorm(x, gain, eps, out=None, stream=None):
     rows, cols = x.shape
     if out is None:
@@ -365,6 +413,7 @@ def sevo_rmsnorm(x, gain, eps, out=None, stream=None):
     return out
 
 
+@_on_its_stream
 def sevo_add_rmsnorm(x, partials, gain, eps, out=None, stream=None):
     """x fp32 [rows, cols] += the partials fp32 [S, rows, cols] (in s order; None
     for none), in place; returns RMSNorm(x) * gain as bf16 in the tiled
@@ -389,6 +438,7 @@ def sevo_linear_plan(m, n_out, k, k_splits=0, mode=LINEAR_STORE):
     return tuple(int(v) for v in plan)
 
 
+@_on_its_stream
 def sevo_linear(x, w, mode=LINEAR_STORE, out=None, k_splits=0, workspace=None, stream=None,
                 m=None, x_tiled=False, out_tiled=False):
     """Y = x w^T (bf16 in, fp32 accumulate) with the STORE / ADD / SWIGLU epilogue.
@@ -419,6 +469,7 @@ def sevo_linear(x, w, mode=LINEAR_STORE, out=None, k_splits=0, workspace=None, s
     return out
 
 
+@_on_its_stream
 def sevo_pack_weight(src, kind=PACK_PLAIN, dst=None, stream=None):
     """Row-major bf16 [n_out, k] -> a new tensor of the same shape in the packed layout."""
     n_out, k = src.shape
@@ -428,6 +479,7 @@ def sevo_pack_weight(src, kind=PACK_PLAIN, dst=None, stream=None):
     return dst
 
 
+@_on_its_stream
 def sevo_pack_kv(k_pool, v_pool, kv_pool=None, stream=None):
     """Plain K and V pools bf16 [pages, hkv, 16, d] -> the fused pool [pages, hkv, 2, 16 d]."""
     pages, hkv, slots, d = k_pool.shape
@@ -438,6 +490,7 @@ def sevo_pack_kv(k_pool, v_pool, kv_pool=None, stream=None):
     return kv_pool
 
 
+@_on_its_stream
 def sevo_qk_norm_rope_append(model, layer, qkv, positions, page_table, kv_pool, q_out=None,
                              stream=None):
     n = qkv.shape[0]
@@ -575,6 +628,7 @@ class StepBuffers:
         return self.out_tokens, self.out_logprobs
 
 
+@_on_its_stream
 def sevo_decode_step(model: Model, tokens, positions, page_table, kv_pools, cand_uid,
                      seed, temperature=1.0, num_splits=0, keep_logits=False, stream=None,
                      conf_topk=0, conf_sum=None, top_k=0, top_p=1.0, min_p=0.0,
@@ -594,6 +648,7 @@ def sevo_decode_step(model: Model, tokens, positions, page_table, kv_pools, cand
 
 
 # ------------------------------------------------------------------ mixture of experts
+@_on_its_stream
 def sevo_moe_ffn(model: Model, layer: int, h_tiled, n: int, stream=None, partials=None):
     """The MoE FFN of one layer on normed inputs in the tiled activation layout
     (n rows).  Returns (experts int32 [n, k], weights fp32 [n, k],
@@ -658,6 +713,7 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+@_on_its_stream
 def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16=None,
                          stream=None):
     """x fp32 [rows, cols] += the partials [S, rows, cols] (fp32 or bf16, in s
@@ -693,6 +749,7 @@ def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16
     return out, scales
 
 
+@_on_its_stream
 def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
     """bf16 rows [m, k] (row stride from the tensor) to codes float8_e4m3fn [m, k]
     and scales fp32 [k / 128, m]; with ``swiglu`` of silu(gate) * up, x [m, 2 k]
@@ -719,6 +776,7 @@ def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
     return out, scales
 
 
+@_on_its_stream
 def sevo_pack_weight_fp8(src, dst=None, stream=None):
     """Row-major codes float8_e4m3fn [n_out, k] (or [E, n_out, k], the experts of a
     layer) -> a new tensor of the same shape in the packed 8-bit layout."""
@@ -740,6 +798,7 @@ def sevo_linear_fp8_workspace_bytes(m, n_out, k) -> int:
     return int(lib().sevo_linear_fp8_workspace_bytes(m, n_out, k))
 
 
+@_on_its_stream
 def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16, workspace=None,
                     stream=None):
     """Y = X W^T of 8-bit operands: x codes [m, k] (row stride from the tensor) with
@@ -784,6 +843,7 @@ def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16
     return out
 
 
+@_on_its_stream
 def sevo_moe_route(logits, top_k, score="softmax", bias=None, n_groups=1, top_groups=1,
                    group_best=1, renormalise=True, scaling=1.0, out_experts=None,
                    out_weights=None, stream=None):
@@ -826,6 +886,7 @@ def sevo_moe_lists_bytes(n, top_k, n_experts) -> int:
     return int(lib().sevo_moe_lists_bytes(n, top_k, n_experts))
 
 
+@_on_its_stream
 def sevo_moe_lists(experts, n_experts, buffer=None, stream=None) -> MoeLists:
     """Entry lists of experts int32 [n, top_k] for ``sevo_moe_linear_fp8``.
     ``buffer``: a caller's uint8 buffer of sevo_moe_lists_bytes."""
@@ -842,6 +903,7 @@ def sevo_moe_lists(experts, n_experts, buffer=None, stream=None) -> MoeLists:
     return MoeLists(n, top_k, int(n_experts), buffer)
 
 
+@_on_its_stream
 def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None, out=None,
                         stream=None):
     """The experts' products of a routing, bf16.  Without ``weights``: gate/up, x
@@ -876,6 +938,7 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
 
 
 # ------------------------------------------------------------------ read probe
+@_on_its_stream
 def sevo_hbm_read_probe(buf, page_order=None, grid=32768, sink=None, stream=None):
     """Read every byte of the device tensor ``buf`` once (sequentially, or as
     8 KB pages in the int32 order ``page_order``); returns the sink tensor."""
