@@ -24,7 +24,7 @@ def test_stream_arguments(sevo):
     """Chains on two explicit streams, nothing given and temporaries dropped at once:
     always the bits of the same chain alone, in memory of the chain's stream."""
     g = gen(31)
-    m, n_out, k = 64, 1024, 8192
+    m, n_out, k = 64, 1024, 12288
     assert sevo.sevo_linear_fp8_workspace_bytes(m, n_out, k) > 0     # K splits: a workspace of the call's own
     wq, ws = weights((n_out, k), g)
     w = sevo.sevo_pack_weight_fp8(wq)
