@@ -193,13 +193,16 @@ __device__ __forceinline__ float value_of(uint32_t k) {
 // its product), the sum of a softmax, the reciprocal and the products by 5e-7.
 // Without a bias that is relative: two scores at |x| under 25 by 1e-5 together, and
 // under e^-25 by less than 1e-15.  With one, |x| e^-|x| < 0.4 bounds it absolutely:
-// 6e-7 for each score and the rounding of the bias's sum, twice that for the sum of
-// a group's two.  A key adds 2^-19 of its value.
+// 6e-7 for each score, and the bias's sum rounds by 2^-24 of itself.  A group's sum of
+// two is off by both of its members' errors and 2^-24 of itself: as its members can
+// cancel (a large bias of either sign), by 1.2e-6 and 2^-23 of their magnitudes.
+// A key adds 2^-19 of its value.
 struct Apart {
   float off, key_off, base;
   __device__ __forceinline__ explicit Apart(bool bias)
-      : off(bias ? 3e-6f : 1e-5f), key_off(bias ? 6e-6f : 1.3e-5f), base(bias ? 1.f : 1e-10f) {}
-  __device__ __forceinline__ bool scores(float a, float b) const { return a - b > off * (base + fabsf(a)); }
+      : off(bias ? 1.5e-6f : 5e-6f), key_off(bias ? 6e-6f : 1.3e-5f), base(bias ? 1.f : 1e-10f) {}
+  // how far a group's value can be off, its members' magnitudes adding to mag
+  __device__ __forceinline__ float group(float mag) const { return off * (base + mag); }
   __device__ __forceinline__ bool key(float a, float b) const { return a - b > key_off * (base + fabsf(a)); }
 };
 
@@ -293,16 +296,18 @@ __global__ __launch_bounds__(256) void moe_route8_kernel(MoeRouteArgs a, int np,
       if (seg > 2) top2_xor<2>(a0, a1);
       if (seg > 4) top2_xor<4>(a0, a1);
       const float g = a.group_best == 2 ? a0 + a1 : a0;
-      // a group's rank: how many are as large or larger, and the next one below
+      // a group's rank: how many are as large or larger
       int larger = 0;
-      float next = -INFINITY;
-      for (int o = seg; o < 16; o += seg) {
-        const float other = __shfl(g, (lane & 48) | ((l16 + o) & 15), kWave);
-        larger += other >= g;
-        next = fmaxf(next, other < g ? other : -INFINITY);
-      }
+      for (int o = seg; o < 16; o += seg)
+        larger += __shfl(g, (lane & 48) | ((l16 + o) & 15), kWave) >= g;
       bad |= larger < a.top_groups && !(fabsf(g) < 1e30f);
-      bad |= larger == a.top_groups - 1 && !apart.scores(g, next);
+      // the least that a group kept can be against the most that one left out can
+      const float err = apart.group(fabsf(a0) + (a.group_best == 2 ? fabsf(a1) : 0.f));
+      const float least = row_reduce(larger < a.top_groups ? g - err : INFINITY,
+                                     [](float x, float y) { return fminf(x, y); });
+      const float most = row_reduce(larger >= a.top_groups && g > -INFINITY ? g + err : -INFINITY,
+                                    [](float x, float y) { return fmaxf(x, y); });
+      bad |= !(least > most);
       // fewer kept than asked for: equal values stood at the border
       const uint64_t kept = __ballot(larger < a.top_groups && (l16 & (seg - 1)) == 0);
       bad |= __popc((uint32_t)(kept >> (lane & 48)) & 0xFFFFu) != a.top_groups;

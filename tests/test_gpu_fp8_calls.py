@@ -51,3 +51,50 @@ def test_stream_arguments(sevo):
         for y, z in got[i]:
             assert torch.equal(y, want[i][0]) and torch.equal(z, want[i][1])
         assert stream_of(got[i][-1][0]) == streams[i].cuda_stream
+
+
+# ------------------------------------------------------------------ routing
+def route64(logits, top_k, score, bias, groups, top_groups, best):
+    """(experts, weights) by the definition in float64 (numpy, all tokens at once)."""
+    z = logits.astype(np.float64)
+    n, E = z.shape
+    if score == "sigmoid":
+        p = 1 / (1 + np.exp(-z))
+    else:
+        p = np.exp(z - z.max(1, keepdims=True))
+        p = p / p.sum(1, keepdims=True)
+    c = p if bias is None else p + bias.astype(np.float64)
+    gs = -np.sort(-c.reshape(n, groups, E // groups), axis=2)[:, :, :best].sum(2)
+    kept = np.argsort(-gs, axis=1, kind="stable")[:, :top_groups]
+    keep = np.zeros((n, groups), bool)
+    np.put_along_axis(keep, kept, True, 1)
+    c = np.where(np.repeat(keep, E // groups, 1), c, -np.inf)
+    ex = np.argsort(-c, axis=1, kind="stable")[:, :top_k]
+    w = np.take_along_axis(p, ex, 1)
+    return ex, w / (w.sum(1, keepdims=True) + 1e-20)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("size", [3.0, 300.0, 1e4, 1e6, 1e9])
+def test_moe_route_large_biases(sevo, score, size):
+    """Each group has one expert with a large bias and the rest with its negative:
+    the sum of its two best is as small as the scores, and the float32 sum is off by
+    the rounding of the biases.  Beside them one group that is switched off by a
+    large negative bias.  The three experts with the large bias of the groups kept
+    stand apart from all others, so that the groups alone decide."""
+    n, E, groups, top_groups, top_k = 3000, 128, 8, 3, 3
+    rng = np.random.default_rng(int(size))
+    # scores near each other: groups a few float32 steps of the bias apart, and less
+    spread = 1.0 if size < 10 else min(1.0, size * (2e-6 if score == "sigmoid" else 5e-5))
+    z = (0.3 + rng.normal(0, spread, (n, E))).astype(np.float32)
+    bias = np.full(E, -size, np.float32)
+    # (each in another place of its lane's eight: no two of them have the same key)
+    bias[np.arange(groups) * (E // groups) + [0, 9, 2, 11, 4, 13, 6, 15]] = size
+    bias[-E // groups:] = -3 * size
+    ex, wt = sevo.sevo_moe_route(torch.from_numpy(z).cuda(), top_k, score, torch.from_numpy(bias).cuda(),
+                                 groups, top_groups, 2, True, 1.0)
+    rex, rwt = route64(z, top_k, score, bias, groups, top_groups, 2)
+    wrong = int((np.sort(ex.cpu().numpy() * groups // E, 1) != np.sort(rex * groups // E, 1)).any(1).sum())
+    assert wrong == 0, f"{wrong} of {n} tokens in other groups"
+    np.testing.assert_array_equal(ex.cpu().numpy(), rex)
+    np.testing.assert_allclose(wt.cpu().numpy(), rwt, rtol=2.0 ** -23)
