@@ -42,7 +42,9 @@ __device__ __forceinline__ double row_sum_f64(double v) {
   return v + lane_xor_f64<8>(v);
 }
 
-// Order-preserving keys of doubles that are not NaN; 0 is below every one
+// Order-preserving keys of doubles that are not NaN; kNanKey is below every one, and 0
+// below that
+constexpr uint64_t kNanKey = 1;
 __device__ __forceinline__ uint64_t key_f64(double v) {
   const uint64_t u = __builtin_bit_cast(uint64_t, v);
   return u ^ ((uint64_t)((int64_t)u >> 63) | 1ull << 63);
@@ -101,11 +103,11 @@ __device__ __forceinline__ void route_f64(const MoeRouteArgs& a, int t, double (
   for (int i = 0; i < kPerLane; ++i) {
     const int e = lane + 64 * i;
     p[i] = (a.sigmoid ? 1.0 : p[i]) / (a.sigmoid ? 1.0 + p[i] : sum);
-    double v = a.bias ? p[i] + (double)bias[i] : p[i];
-    v = v == v ? v : -INFINITY;  // a NaN is chosen after everything else
-    key[i] = e < a.n_experts ? key_f64(v) : 0;
+    const double v = a.bias ? p[i] + (double)bias[i] : p[i];
+    // a NaN is chosen after everything else, -inf too, and adds -inf to its group
+    key[i] = e >= a.n_experts ? 0 : v == v ? key_f64(v) : kNanKey;
     s[0][e] = p[i];
-    s[1][e] = v;
+    s[1][e] = v == v ? v : -INFINITY;
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   if (a.top_groups < a.n_groups) {
@@ -121,7 +123,7 @@ __device__ __forceinline__ void route_f64(const MoeRouteArgs& a, int t, double (
         b0 = fmax(b0, v);
       }
       const double sum2 = a.group_best == 2 ? b0 + b1 : b0;
-      g = key_f64(sum2 == sum2 ? sum2 : -INFINITY);  // +inf and -inf biases in one group
+      g = sum2 == sum2 ? key_f64(sum2) : kNanKey;  // (+inf and -inf biases in one group)
     }
     uint64_t kept = 0;
 #pragma unroll 1

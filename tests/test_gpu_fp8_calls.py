@@ -98,3 +98,19 @@ def test_moe_route_large_biases(sevo, score, size):
     assert wrong == 0, f"{wrong} of {n} tokens in other groups"
     np.testing.assert_array_equal(ex.cpu().numpy(), rex)
     np.testing.assert_allclose(wt.cpu().numpy(), rwt, rtol=2.0 ** -23)
+
+
+def test_moe_route_nan_is_last(sevo):
+    """A NaN is chosen after every other value, experts that a bias of -inf has
+    switched off among them; a group without a value after those with one."""
+    nan, inf = float("nan"), float("inf")
+    z = torch.tensor([[nan, 0.0, 2.0, 1.0, 0.5, nan, 0.25, -1.0]], device="cuda")
+    bias = torch.tensor([0, 0, 0, -inf, 0, 0, 0, 0], device="cuda")
+    for top_k, want in ((5, [2, 4, 6, 1, 7]), (6, [2, 4, 6, 1, 7, 3]), (8, [2, 4, 6, 1, 7, 3, 0, 5])):
+        ex, wt = sevo.sevo_moe_route(z, top_k, "sigmoid", bias, renormalise=False)
+        assert ex[0].tolist() == want, ex[0].tolist()
+        assert torch.isnan(wt[0, 6:]).all() and torch.isfinite(wt[0, :6]).all()
+    # groups of two: 0's sum is +inf - inf, 1's -inf, 2's and 3's finite
+    bias = torch.tensor([inf, -inf, -inf, 0, 0, 0, 0, 0], device="cuda")
+    ex, _ = sevo.sevo_moe_route(torch.zeros(1, 8, device="cuda"), 6, "sigmoid", bias, 4, 3, 2, False)
+    assert sorted(ex[0].tolist()) == [2, 3, 4, 5, 6, 7]
