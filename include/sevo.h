@@ -697,7 +697,7 @@ sevo_status sevo_moe_route(const sevo_moe_route_args* a, void* stream);
 /* The entry lists of a routing, which the grouped products read: entry t top_k +
  * j (token t, slot j) goes to the list of experts[t][j], each list in entry
  * order.  An id outside [0, n_experts) joins no list: products leave its output
- * rows as they were.  experts int32 [n][top_k]; lists: a caller's buffer of
+ * rows as they were, or zero them (clear_unlisted).  experts int32 [n][top_k]; lists: a caller's buffer of
  * sevo_moe_lists_bytes, its contents private.  n top_k <= 2^30, n_experts 1..256,
  * top_k 1..16.  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */
 sevo_status sevo_moe_lists(const int32_t* experts, int32_t n, int32_t top_k, int32_t n_experts,
@@ -714,6 +714,8 @@ size_t sevo_moe_lists_bytes(int32_t n, int32_t top_k, int32_t n_experts);
  *   w [n_experts][n_out][k], each packed; w_scales [n_experts]
  *   [ceil(n_out / 128)][k / 128]; weights fp32 [n][top_k] (down only); lists of
  *   sevo_moe_lists for the same n, top_k and n_experts.
+ * clear_unlisted 1: the output rows of entries in no list are set to zero (so that the
+ * planes can be added); 0: they are left as they were.
  * ldx, lds as in sevo_linear_fp8; n_out % 64 == 0, k % 128 == 0; x and x_scales
  * each below 2^31 bytes (UNSUPPORTED beyond: fewer tokens a call).
  * Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP. */
@@ -727,6 +729,7 @@ typedef struct {
   const float* weights;
   const void* lists;
   void* out;
+  int32_t clear_unlisted;
 } sevo_moe_linear_fp8_args;
 
 sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void* stream);

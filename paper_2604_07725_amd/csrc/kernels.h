@@ -123,6 +123,10 @@ hipError_t launch_moe_plan(const int32_t* sel, int nk, int E, int32_t* offsets, 
                            hipStream_t st, int32_t* tile_off = nullptr, int tile_rows = 256,
                            int32_t* scratch = nullptr);
 size_t moe_plan_scratch_bytes(int nk, int E);
+// after a plan in launches of its own (scratch given, more than 4096 entries): the
+// entries without an expert, in order, to assign[offsets[E] .. nk)
+hipError_t launch_moe_plan_rest(const int32_t* sel, int nk, int E, const int32_t* offsets,
+                                int32_t* assign, const int32_t* scratch, hipStream_t st);
 // gate/up + SwiGLU into act, then down into part
 hipError_t launch_moe_experts(const MoeExpertArgs& a, hipStream_t st);
 
@@ -273,8 +277,9 @@ struct Moe8Args {
   const float* ws;       // [E][ceil(n_out / 128)][k / 128]
   const float* weights;  // [n][top_k] (down)
   const int32_t* offsets;   // [E + 1]
-  const int32_t* assign;    // entries t top_k + slot, expert-major
+  const int32_t* assign;    // entries t top_k + slot, expert-major, behind them those without one
   bf16_t* out;
+  int clear;                // the output rows of entries without an expert are zeroed
 };
 hipError_t launch_moe8(const Moe8Args& a, hipStream_t st);
 
@@ -289,8 +294,8 @@ struct MoeRouteArgs {
   float* out_weights;
 };
 hipError_t launch_moe_route8(const MoeRouteArgs& a, hipStream_t st);
-// the lists of launch_moe_plan (offsets [E + 1], assign [nk]); scratch of
-// moe_plan_scratch_bytes
+// the lists of launch_moe_plan (offsets [E + 1], assign [nk]), behind them in assign the
+// entries without an expert; scratch of moe_plan_scratch_bytes
 hipError_t launch_moe_lists(const int32_t* sel, int nk, int E, int32_t* offsets, int32_t* assign,
                             int32_t* scratch, hipStream_t st);
 

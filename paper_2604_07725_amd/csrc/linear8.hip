@@ -258,6 +258,18 @@ __global__ __launch_bounds__(256) void linear8_sum_kernel(const float* __restric
   }
 }
 
+// Zeros the output rows of the entries without an expert, which stand behind the lists:
+// every parts-th one, from the part-th on, by a whole workgroup.
+__device__ __forceinline__ void clear_unlisted(const Moe8Args& a, int part, int parts) {
+  const int nk = a.n * a.top_k;
+  for (int i = a.offsets[a.n_experts] + part; i < nk; i += parts) {
+    const int asg = a.assign[i], tok = asg / a.top_k;
+    const size_t row = a.down ? (size_t)(asg - tok * a.top_k) * a.n + tok : (size_t)asg;
+    for (int c = 8 * threadIdx.x; c < a.n_out; c += 8 * blockDim.x)
+      *reinterpret_cast<u32x4*>(a.out + row * a.n_out + c) = u32x4{0, 0, 0, 0};
+  }
+}
+
 // The product grouped by expert for few entries an expert: a stream of the chosen
 // experts' weights.  A wave takes two 16-row weight blocks of one expert over the
 // whole k, a workgroup 128 rows (one row of weight scales); the expert's entries come
@@ -269,6 +281,7 @@ __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, q = lane >> 4;
   const int e = blockIdx.y;
+  if (a.clear) clear_unlisted(a, blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
   const int off = a.offsets[e], ne = a.offsets[e + 1] - off;
   const int KB = a.k >> 7, nrb = a.n_out >> 4;
   const int rb0 = blockIdx.x * 8 + 2 * wave;
@@ -382,6 +395,7 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
   // grouped: each lane keeps the first tile, first entry and entries of experts lane + 64 j
   int e_tile[GR ? 4 : 1], e_first[GR ? 4 : 1], e_rows[GR ? 4 : 1];
   if constexpr (GR) {
+    if (g.clear) clear_unlisted(g, blockIdx.x, gridDim.x);
     tiles_m = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

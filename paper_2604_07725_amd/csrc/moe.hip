@@ -329,6 +329,38 @@ __global__ __launch_bounds__(kPlanThreads) void moe_plan_place_kernel(
   }
 }
 
+// The entries without an expert, in order, behind the lists: assign[offsets[E] ..
+// nk).  A chunk's first one has as many before it as the chunks before have entries
+// in no list; cbase as the scan left it.
+__global__ __launch_bounds__(kPlanThreads) void moe_plan_rest_kernel(
+    const int32_t* __restrict__ sel, int nk, int E, const int32_t* __restrict__ cbase,
+    const int32_t* __restrict__ offsets, int32_t* __restrict__ assign) {
+  constexpr int W = kPlanThreads / 64;
+  __shared__ int listed[W], rest[W];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r = blockIdx.x * kPlanThreads + tid;
+  int before = tid < E ? cbase[(size_t)blockIdx.x * E + tid] - offsets[tid] : 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, kWave);
+  const bool own = r < nk && (uint32_t)sel[r] >= (uint32_t)E;
+  const uint64_t mask = __ballot(own);
+  if (lane == 0) {
+    listed[wave] = before;
+    rest[wave] = __popcll(mask);
+  }
+  __syncthreads();
+  int at = offsets[E] + blockIdx.x * kPlanThreads + __popcll(mask & ((1ull << lane) - 1));
+  for (int w = 0; w < W; ++w) at += (w < wave ? rest[w] : 0) - listed[w];
+  if (own) assign[at] = r;
+}
+
+hipError_t launch_moe_plan_rest(const int32_t* sel, int nk, int E, const int32_t* offsets,
+                                int32_t* assign, const int32_t* scratch, hipStream_t st) {
+  hipLaunchKernelGGL(moe_plan_rest_kernel, dim3((nk + kPlanThreads - 1) / kPlanThreads),
+                     dim3(kPlanThreads), 0, st, sel, nk, E, scratch, offsets, assign);
+  return hipGetLastError();
+}
+
 size_t moe_plan_scratch_bytes(int nk, int E) {
   return (size_t)((nk + kPlanThreads - 1) / kPlanThreads) * E * 4;
 }

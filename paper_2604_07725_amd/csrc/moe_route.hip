@@ -416,7 +416,8 @@ hipError_t launch_moe_route8(const MoeRouteArgs& a, hipStream_t st) {
 }
 
 // Entry lists in one launch: workgroup e reads every entry once and counts those of
-// lower experts (its list's first place) and its own; its own then go out in order.  A
+// lower experts (its list's first place) and its own; its own then go out in order.
+// Workgroup E does the same for the entries without an expert, behind the lists.  A
 // wave holds 512 C consecutive entries in registers, a lane eight of each 512, and an
 // entry's rank is the matches of the waves, chunks and lanes before it: one barrier,
 // no sums between workgroups, and nothing depends on scheduling.
@@ -440,6 +441,13 @@ __global__ __launch_bounds__(T) void moe_lists_kernel(const int32_t* __restrict_
       for (int j = 0; j < P; ++j) v[c][j] = i + j < nk ? sel[i + j] : -1;
     }
   }
+  if (e == E) {  // uniform
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int j = 0; j < P; ++j)
+        if ((uint32_t)v[c][j] >= (uint32_t)E && i0 + 512 * c + j < nk) v[c][j] = E;
+  }
   int lower = 0, own = 0;
 #pragma unroll
   for (int c = 0; c < C; ++c)
@@ -458,17 +466,13 @@ __global__ __launch_bounds__(T) void moe_lists_kernel(const int32_t* __restrict_
     red[1][wave] = own;
   }
   __syncthreads();
-  int first = 0, count = 0, at = 0;
+  int first = 0, at = 0;
 #pragma unroll
   for (int w = 0; w < W; ++w) {
     if (w < wave) at += red[1][w];
     first += red[0][w];
-    count += red[1][w];
   }
-  if (threadIdx.x == 0) {
-    offsets[e] = first;
-    if (e == E - 1) offsets[E] = first + count;
-  }
+  if (threadIdx.x == 0) offsets[e] = first;
   at += first;
   const uint64_t below = (1ull << lane) - 1;
 #pragma unroll
@@ -489,16 +493,19 @@ __global__ __launch_bounds__(T) void moe_lists_kernel(const int32_t* __restrict_
 }
 
 // From this many entries on, reading all of them in every workgroup costs more
-// than the three launches that count, scan and place.
+// than the launches that count, scan and place.
 constexpr int kOneLaunchEntries = 65536;
 
 hipError_t launch_moe_lists(const int32_t* sel, int nk, int E, int32_t* offsets, int32_t* assign,
                             int32_t* scratch, hipStream_t st) {
   if (nk == 0) return hipSuccess;
-  if (nk > kOneLaunchEntries)
-    return launch_moe_plan(sel, nk, E, offsets, assign, st, nullptr, 256, scratch);
+  if (nk > kOneLaunchEntries) {
+    if (hipError_t e = launch_moe_plan(sel, nk, E, offsets, assign, st, nullptr, 256, scratch); e != hipSuccess)
+      return e;
+    return launch_moe_plan_rest(sel, nk, E, offsets, assign, scratch, st);
+  }
   auto go = [&](auto kern, int threads) {
-    hipLaunchKernelGGL(kern, dim3(E), dim3(threads), 0, st, sel, nk, E, offsets, assign);
+    hipLaunchKernelGGL(kern, dim3(E + 1), dim3(threads), 0, st, sel, nk, E, offsets, assign);
   };
   if (nk <= 2048) go(moe_lists_kernel<256, 1>, 256);
   else if (nk <= 8192) go(moe_lists_kernel<1024, 1>, 1024);

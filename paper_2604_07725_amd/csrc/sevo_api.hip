@@ -1626,7 +1626,8 @@ SEVO_API sevo_status sevo_moe_lists(const int32_t* experts, int32_t n, int32_t t
 SEVO_API sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void* stream) {
   if (!a) return fail(SEVO_ERR_INVALID_ARGUMENT, "null args");
   if (sevo_status s = check_moe_shape(a->n, a->top_k, a->n_experts)) return s;
-  if (a->down != 0 && a->down != 1) return fail(SEVO_ERR_INVALID_ARGUMENT, "down %d", a->down);
+  if ((a->down != 0 && a->down != 1) || (a->clear_unlisted != 0 && a->clear_unlisted != 1))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "down %d, clear_unlisted %d", a->down, a->clear_unlisted);
   if (sevo_status s = check_fp8_product(a->n_out, a->k, a->ldx)) return s;
   const int64_t rows = a->down ? (int64_t)a->n * a->top_k : a->n;
   if (a->lds < rows) return fail(SEVO_ERR_INVALID_ARGUMENT, "lds %lld < rows", (long long)a->lds);
@@ -1647,6 +1648,7 @@ SEVO_API sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void
   m.weights = a->weights;
   m.offsets = p + L.offsets; m.assign = p + L.assign;
   m.out = static_cast<sevo::bf16_t*>(a->out);
+  m.clear = a->clear_unlisted;
   hipError_t e = sevo::launch_moe8(m, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_moe_linear_fp8");
 }

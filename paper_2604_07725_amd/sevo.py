@@ -132,7 +132,8 @@ class MoeRouteArgs(C.Structure):
 class MoeLinearFp8Args(C.Structure):
     _fields_ = [("n", i32), ("top_k", i32), ("n_experts", i32), ("n_out", i32), ("k", i32),
                 ("down", i32), ("ldx", i64), ("lds", i64), ("x", vp), ("x_scales", vp),
-                ("w", vp), ("w_scales", vp), ("weights", vp), ("lists", vp), ("out", vp)]
+                ("w", vp), ("w_scales", vp), ("weights", vp), ("lists", vp), ("out", vp),
+                ("clear_unlisted", i32)]
 
 
 _SIGS = {
@@ -909,7 +910,8 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
     """The experts' products of a routing, bf16.  Without ``weights``: gate/up, x
     codes [n, k], returns [n * top_k, n_out].  With ``weights`` fp32 [n, top_k]:
     down, x codes [n * top_k, k], returns the weighted partials [top_k, n, n_out].
-    w packed codes [E, n_out, k], w_scales [E, ceil(n_out / 128), k / 128]."""
+    w packed codes [E, n_out, k], w_scales [E, ceil(n_out / 128), k / 128].  The rows
+    of entries whose expert id is outside [0, E) are zero, or with ``out`` as they were."""
     f8 = torch.float8_e4m3fn
     n, top_k, E = lists.n, lists.top_k, lists.n_experts
     down = weights is not None
@@ -925,14 +927,15 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
     if down:
         _need("weights", weights, torch.float32, (n, top_k), i)
     shape = (top_k, n, n_out) if down else (n * top_k, n_out)
-    if out is None:
+    clear = out is None
+    if clear:
         out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
     else:
         _need("out", out, torch.bfloat16, shape, i)
     a = MoeLinearFp8Args(n, top_k, E, n_out, k, 1 if down else 0, _ld(x, rows, k),
                          _ld(x_scales, k // SCALE_BLOCK, rows), x.data_ptr(),
                          x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(), _ptr(weights),
-                         lists.buffer.data_ptr(), out.data_ptr())
+                         lists.buffer.data_ptr(), out.data_ptr(), 1 if clear else 0)
     _call("sevo_moe_linear_fp8", i, stream, C.byref(a))
     return out
 

@@ -114,3 +114,45 @@ def test_moe_route_nan_is_last(sevo):
     bias = torch.tensor([inf, -inf, -inf, 0, 0, 0, 0, 0], device="cuda")
     ex, _ = sevo.sevo_moe_route(torch.zeros(1, 8, device="cuda"), 6, "sigmoid", bias, 4, 3, 2, False)
     assert sorted(ex[0].tolist()) == [2, 3, 4, 5, 6, 7]
+
+
+# ------------------------------------------------------------------ experts
+@pytest.mark.parametrize("n,E,top_k,n_out,k", [
+    (3, 8, 2, 192, 128), (40, 64, 4, 64, 256), (300, 16, 4, 320, 256), (900, 16, 4, 4160, 128),
+    (9000, 16, 8, 192, 128)])
+@pytest.mark.parametrize("share", [0.0, 0.3, 1.0])
+def test_moe_linear_fp8_unlisted_rows(sevo, n, E, top_k, n_out, k, share):
+    """Entries without an expert, as a rank that holds some of the experts has them:
+    without ``out`` their rows are zero in memory that was not, all other rows as they
+    are with it, and the next norm can add the planes."""
+    say(f"unlisted n={n} E={E} top {top_k} {n_out} x {k} share {share}")
+    g = gen(n + E)
+    ex = torch.randint(0, E, (n, top_k), device="cuda", dtype=torch.int32, generator=g)
+    drop = torch.rand((n, top_k), device="cuda", generator=g) < share
+    bad = torch.tensor([-1, E, -2 ** 31, 2 ** 31 - 1], device="cuda", dtype=torch.int32)
+    ex = torch.where(drop, bad[torch.randint(0, 4, (n, top_k), device="cuda", generator=g)], ex)
+    wt = torch.rand((n, top_k), device="cuda", generator=g)
+    wq, ws = weights((E, n_out, k), g)
+    w = sevo.sevo_pack_weight_fp8(wq)
+    lists = sevo.sevo_moe_lists(ex, E)
+    for down in (False, True):
+        xq, xs = quantised(normal((n * top_k if down else n, k), g))
+        kw = dict(weights=wt) if down else {}
+        shape = (top_k, n, n_out) if down else (n * top_k, n_out)
+        given = torch.full(shape, float("nan"), dtype=BF, device="cuda")
+        sevo.sevo_moe_linear_fp8(xq, xs, w, ws, lists, out=given, **kw)
+        rows = drop.t() if down else drop.reshape(-1)
+        assert torch.isnan(given[rows]).all() and torch.isfinite(given[~rows]).all()
+        dirty = torch.full(shape, float("nan"), dtype=BF, device="cuda")
+        at = dirty.data_ptr()
+        del dirty
+        y = sevo.sevo_moe_linear_fp8(xq, xs, w, ws, lists, **kw)
+        say(f"  the same memory: {y.data_ptr() == at}")
+        assert (y[rows] == 0).all() and torch.equal(y[~rows], given[~rows])
+    parts = torch.nn.functional.pad(y, (0, -n_out % 128)).contiguous()
+    x = normal((n, parts.shape[2]), g)
+    want = x.clone()
+    for p in parts:
+        want = want + p.float()
+    sevo.sevo_add_rmsnorm_fp8(x, parts, torch.ones(parts.shape[2], dtype=BF, device="cuda"), 1e-6)
+    assert torch.equal(x, want)
