@@ -883,6 +883,7 @@ class MoeLists:
         self.n, self.top_k, self.n_experts, self.buffer = n, top_k, n_experts, buffer
 
 
+@functools.lru_cache(maxsize=1024)
 def sevo_moe_lists_bytes(n, top_k, n_experts) -> int:
     return int(lib().sevo_moe_lists_bytes(n, top_k, n_experts))
 
@@ -924,6 +925,8 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
     _need("w_scales", w_scales, torch.float32,
           (E, -(-n_out // SCALE_BLOCK), k // SCALE_BLOCK), i)
     _need("lists", lists.buffer, torch.uint8, None, i)
+    if lists.buffer.numel() < sevo_moe_lists_bytes(n, top_k, E):
+        raise ValueError("lists: a buffer smaller than the lists of these sizes")
     if down:
         _need("weights", weights, torch.float32, (n, top_k), i)
     shape = (top_k, n, n_out) if down else (n * top_k, n_out)

@@ -3,7 +3,7 @@ tests/test_abi_fp8.py."""
 import ctypes as C
 
 import pytest
-
+import torch
 
 from paper_2604_07725_amd import sevo
 
@@ -18,3 +18,17 @@ def test_moe_linear_fp8_refuses(kw, status):
              x_scales=F, w=F, w_scales=F, lists=F, out=F)
     a.update(kw)
     assert sevo.lib().sevo_moe_linear_fp8(C.byref(sevo.MoeLinearFp8Args(**a)), None) == status
+
+
+def test_lists_of_other_sizes_are_refused():
+    """Lists in a buffer too small for their sizes are refused before the kernels
+    follow them out of it."""
+    f8 = torch.float8_e4m3fn
+    x, xs = torch.zeros(64, 256).to(f8), torch.zeros(2, 64)
+    w, ws = torch.zeros(3, 64, 256).to(f8), torch.zeros(3, 1, 2)
+    need = sevo.sevo_moe_lists_bytes(64, 2, 3)
+    for size in (0, 256, need - 1):
+        with pytest.raises(ValueError, match="lists"):
+            sevo.sevo_moe_linear_fp8(x, xs, w, ws, sevo.MoeLists(64, 2, 3, torch.zeros(size, dtype=torch.uint8)))
+    with pytest.raises(ValueError, match="GPU"):      # the size will do
+        sevo.sevo_moe_linear_fp8(x, xs, w, ws, sevo.MoeLists(64, 2, 3, torch.zeros(need, dtype=torch.uint8)))

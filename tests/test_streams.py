@@ -93,7 +93,8 @@ def watched(monkeypatch):
                         lambda t, s: seen.marked.append((t.data_ptr(), s.cuda_stream)), raising=False)
     monkeypatch.setattr(sevo, "lib", Library)
     monkeypatch.setattr(sevo, "_call", lambda name, i, stream, *a: seen.launched.append(stream))
-    monkeypatch.setattr(sevo, "sevo_linear_fp8_workspace_bytes", lambda *a: 4096)
+    for name in ("sevo_linear_fp8_workspace_bytes", "sevo_moe_lists_bytes"):   # (they keep their answers)
+        monkeypatch.setattr(sevo, name, lambda *a: 4096)
     for name in ("empty", "zeros", "empty_like"):
         monkeypatch.setattr(torch, name, recording(getattr(torch, name)))
     return seen
