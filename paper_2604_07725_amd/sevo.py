@@ -689,9 +689,9 @@ def _need(name, t, dtype, shape, device, contiguous=True):
 
 
 def _ld(t, rows, cols):
-    """Row stride of a 2-d tensor (one row has none of its own)."""
-    ld = t.stride()[0]
-    return ld if rows > 1 else max(ld, cols)
+    """Row stride of a 2-d tensor.  One row has none: the stride that its tensor says,
+    that of the buffer it is from, need not be one that the library takes."""
+    return t.stride()[0] if rows > 1 else cols
 
 
 def _call(name, i, stream, *args):

@@ -32,3 +32,14 @@ def test_lists_of_other_sizes_are_refused():
             sevo.sevo_moe_linear_fp8(x, xs, w, ws, sevo.MoeLists(64, 2, 3, torch.zeros(size, dtype=torch.uint8)))
     with pytest.raises(ValueError, match="GPU"):      # the size will do
         sevo.sevo_moe_linear_fp8(x, xs, w, ws, sevo.MoeLists(64, 2, 3, torch.zeros(need, dtype=torch.uint8)))
+
+
+def test_one_row_of_any_buffer():
+    """One token out of a buffer whose rows are no multiple of 16 bytes apart, or far
+    apart: the stride between rows that are not there is not refused."""
+    f8, bf = torch.float8_e4m3fn, torch.bfloat16
+    x = torch.zeros(3, 264).to(f8)[:1, :256]
+    assert sevo._ld(x, 1, 256) == 256
+    assert sevo._ld(torch.zeros(256, 1).t(), 1, 256) == 256
+    assert sevo._ld(torch.zeros(3, 264)[:, :256], 3, 256) == 264
+    assert sevo._ld(torch.zeros(1, 1 << 24, dtype=bf)[:, :512], 1, 512) == 512

@@ -156,3 +156,30 @@ def test_moe_linear_fp8_unlisted_rows(sevo, n, E, top_k, n_out, k, share):
         want = want + p.float()
     sevo.sevo_add_rmsnorm_fp8(x, parts, torch.ones(parts.shape[2], dtype=BF, device="cuda"), 1e-6)
     assert torch.equal(x, want)
+
+
+# ------------------------------------------------------------------ one row
+def test_one_row_of_any_buffer(sevo):
+    """One token out of buffers whose rows are an odd number of bytes apart."""
+    g = gen(12)
+    n_out, k, E = 192, 256, 4
+    wq, ws = weights((E, n_out, k), g)
+    w = sevo.sevo_pack_weight_fp8(wq)
+    xq, xs = quantised(normal((1, k), g))
+    x = torch.zeros(3, k + 8, device="cuda").to(F8)
+    x[:1, :k] = xq
+    out = torch.full((3, n_out + 1), 7.0, dtype=BF, device="cuda")
+    sevo.sevo_linear_fp8(x[:1, :k], xs, w[0], ws[0], out=out[:1, :n_out])
+    check_product(out[:1, :n_out], xq, xs, wq[0], ws[0])
+    assert (out[1:] == 7.0).all() and (out[0, n_out:] == 7.0).all()
+    y = sevo.sevo_moe_linear_fp8(x[:1, :k], xs, w, ws,
+                                 sevo.sevo_moe_lists(torch.tensor([[2, 1]], device="cuda", dtype=torch.int32), E))
+    for j, e in enumerate((2, 1)):
+        check_product(y[j:j + 1], xq, xs, wq[e], ws[e])
+    rows = normal((3, 2 * k + 3), g, 1.0, BF)
+    q, s = sevo.sevo_quantize_fp8(rows[:1, :2 * k], swiglu=True)
+    u = rows[:1, :2 * k].double()
+    check_codes(q, s, u[:, :k] / (1 + torch.exp(-u[:, :k])) * u[:, k:], rel=64 * 2.0 ** -24)
+    z = normal((2, 9), g)
+    ex, _ = sevo.sevo_moe_route(z[:1, :8], 3)
+    assert ex[0].tolist() == torch.sort(z[0, :8], descending=True)[1][:3].tolist()
