@@ -646,7 +646,7 @@ sevo_status sevo_pack_weight_fp8(const void* src, void* dst, int64_t n_out, int3
  *   x [m][k], row stride ldx bytes (>= k, a multiple of 16, below 2^23); x_scales
  *   row stride lds (>= m); w packed; out row stride ldo elements (>= n_out, a
  *   multiple of 4).
- * n_out % 64 == 0, k % 128 == 0; x_scales below 2^31 bytes.  The workspace is
+ * n_out % 64 == 0, at most 2^30; k % 128 == 0; x_scales below 2^31 bytes.  The workspace is
  * scratch of sevo_linear_fp8_workspace_bytes (0: may be NULL); calls that may
  * overlap in time each need their own.  The same call gives the same bits; the
  * bits of a row may depend on m (its plan).  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */

@@ -1440,9 +1440,9 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 // shape rules shared by the products
 sevo_status check_fp8_product(int n_out, int k, int64_t ldx) {
   if (n_out < 1 || k < 1) return fail(SEVO_ERR_INVALID_ARGUMENT, "n_out %d, k %d", n_out, k);
-  if (n_out % 64 || k % 128 || k >= 1 << 23)
-    return fail(SEVO_ERR_UNSUPPORTED, "n_out %d must be a multiple of 64 and k %d of 128 below 2^23",
-                n_out, k);
+  if (n_out % 64 || n_out > 1 << 30 || k % 128 || k >= 1 << 23)
+    return fail(SEVO_ERR_UNSUPPORTED,
+                "n_out %d must be a multiple of 64 up to 2^30 and k %d of 128 below 2^23", n_out, k);
   if (ldx < k || ldx % 16 || ldx >= 1 << 23)
     return fail(SEVO_ERR_INVALID_ARGUMENT, "ldx %lld must be a multiple of 16 in [k, 2^23)",
                 (long long)ldx);
@@ -1533,7 +1533,9 @@ SEVO_API sevo_status sevo_pack_weight_fp8(const void* src, void* dst, int64_t n_
 }
 
 SEVO_API size_t sevo_linear_fp8_workspace_bytes(int32_t m, int32_t n_out, int32_t k) {
-  if (m <= 0 || n_out <= 0 || k <= 0 || n_out % 64 || k % 128 || k >= 1 << 23) return 0;
+  if (m <= 0 || n_out <= 0 || k <= 0 || n_out % 64 || n_out > 1 << 30 || k % 128 || k >= 1 << 23 ||
+      (int64_t)m * (k / 128) * 4 >= (int64_t)1 << 31)  // (a product refuses as many rows)
+    return 0;
   return std::max(sevo::linear8_workspace_bytes(m, n_out, sevo::plan_linear8(m, n_out, k, 0)),
                   sevo::linear8_workspace_bytes(m, n_out, sevo::plan_linear8(m, n_out, k, 1)));
 }

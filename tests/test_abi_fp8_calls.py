@@ -43,3 +43,20 @@ def test_one_row_of_any_buffer():
     assert sevo._ld(torch.zeros(256, 1).t(), 1, 256) == 256
     assert sevo._ld(torch.zeros(3, 264)[:, :256], 3, 256) == 264
     assert sevo._ld(torch.zeros(1, 1 << 24, dtype=bf)[:, :512], 1, 512) == 512
+
+
+def test_sizes_near_the_end_of_int32():
+    """Refused, or planned, without an int32 that overflows (undefined, so that the
+    host-sanitized build ends there)."""
+    L = sevo.lib()
+    top = 2 ** 31
+    for m, n_out, k in ((top - 1, 64, 128), (top - 1, 4096, 25600), (1 << 29, 64, 128), (4, top - 64, 128),
+                        (4, (1 << 30) + 64, 128)):
+        assert L.sevo_linear_fp8_workspace_bytes(m, n_out, k) == 0
+    L.sevo_linear_fp8_workspace_bytes((1 << 29) - 1, 1 << 30, 128)
+    a = dict(m=4, n_out=top - 64, k=128, out_type=sevo.BF16, ldx=128, lds=4, ldo=top, x=F, x_scales=F,
+             w=F, w_scales=F, out=F, workspace=F, workspace_bytes=1 << 40)
+    assert L.sevo_linear_fp8(C.byref(sevo.LinearFp8Args(**a)), None) == sevo.UNSUPPORTED
+    a = dict(n=4, top_k=2, n_experts=8, n_out=top - 64, k=128, down=0, ldx=128, lds=4, x=F, x_scales=F,
+             w=F, w_scales=F, lists=F, out=F)
+    assert L.sevo_moe_linear_fp8(C.byref(sevo.MoeLinearFp8Args(**a)), None) == sevo.UNSUPPORTED
