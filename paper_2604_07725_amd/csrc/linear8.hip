@@ -7,11 +7,15 @@
 // scales multiplied once per row fragment).
 //
 // Two matrix instructions.  The 8-bit ones (16x16x128) have twice the rate of
-// bf16 but sum a block's products with a relative error of 1.4e-5 (measured, the
-// same for 16x16x32 and 32x32x64, unbiased, independent of k), far below the
-// 2^-9 of a result that is rounded to bf16, which is what they are used for.  A result kept in
-// fp32 takes the bf16 instruction on the codes converted to bf16, which is
-// exact (e4m3 has four significant bits): 1e-7.
+// bf16 but add in fewer bits.  Measured: the products of eight neighbouring
+// columns are cut toward zero at 2^-13 of the largest one's power of two (a subnormal
+// operand counts with the exponent -6), then added as in fp32; this gives the bf16
+// results bit for bit.  For normally distributed codes that is 1.4e-5 of a block's sum (norm),
+// -1e-5 on average where all products have one sign, and up to 2e-4 of the sum of
+// magnitudes where they differ by orders: below the 2^-8 of a result that is rounded
+// to bf16, which is what these instructions are used for, unless blocks cancel.  A
+// result kept in fp32 takes the bf16 instruction on the codes converted to bf16, which
+// is exact (e4m3 has four significant bits): 1e-7.
 //
 // A operand = 16 weight rows, B operand = 16 activation rows, 128 columns: lane
 // l holds row l % 16 and its 16-byte runs l / 16 and l / 16 + 4, so that a packed

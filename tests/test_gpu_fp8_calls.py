@@ -7,7 +7,8 @@ import pytest
 import torch
 
 from tests.gpu_helpers import say
-from tests.test_gpu_fp8 import BF, F8, check_codes, check_product, gen, normal, quantised, sevo, weights  # noqa: F401
+from tests.test_gpu_fp8 import (BF, F8, TOP, check_codes, check_product, gen, normal, quantised,  # noqa: F401
+                                sevo, weights)
 
 pytestmark = pytest.mark.gpu
 
@@ -183,3 +184,84 @@ def test_one_row_of_any_buffer(sevo):
     z = normal((2, 9), g)
     ex, _ = sevo.sevo_moe_route(z[:1, :8], 3)
     assert ex[0].tolist() == torch.sort(z[0, :8], descending=True)[1][:3].tolist()
+
+
+# ------------------------------------------------------------------ accuracy of the 8-bit sums
+def exponent(v):
+    """Exponents of e4m3 values, those of subnormal ones (and 0) as -6."""
+    return torch.frexp(v)[1].double().sub(1).clamp_min(-6)
+
+
+def block_sums(X, W):
+    """(exact, as the 8-bit instructions add, sum of magnitudes, largest products of
+    the groups of eight) of one block's rows X [m, 128], W [n, 128] (float64)."""
+    p = (X[:, None] * W[None]).view(X.shape[0], W.shape[0], 16, 8)
+    e = (exponent(X)[:, None] + exponent(W)[None]).view_as(p)
+    unit = torch.exp2(torch.where(p == 0, -18.0, e).amax(3, keepdim=True) - 13)
+    return (p.sum((2, 3)), (torch.trunc(p / unit) * unit).sum((2, 3)), p.abs().sum((2, 3)),
+            (unit * 2.0 ** 13).sum((2, 3)))
+
+
+def codes_of(kind, rows, k, g):
+    v = normal((rows, k), g)
+    if kind == "one sign":
+        v = v.abs()
+    elif kind == "wide":
+        v = v * torch.exp(3 * normal((rows, k), g))
+    elif kind == "small":                           # most codes subnormal
+        v = v * torch.where(torch.rand((rows, k), device="cuda", generator=g) < 0.1, 1.0, 2.0 ** -15)
+    return (v / v.abs().amax(1, keepdim=True) * TOP).to(F8)
+
+
+def cancel(X, W):
+    """W with its last 16 columns of each row changed so that the products with the
+    same row of X nearly cancel."""
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda").view(F8).float()
+    codes = codes[torch.isfinite(codes)].double()
+    x, w = X[:W.shape[0]].double(), W.double()[:X.shape[0]]
+    for j in range(x.shape[1] - 16, x.shape[1]):
+        rest = (x * w).sum(1) - x[:, j] * w[:, j]
+        w[:, j] = codes[(rest[:, None] + x[:, j:j + 1] * codes).abs().argmin(1)]
+    W = W.clone()
+    W[:w.shape[0]] = w.float().to(F8)
+    return W
+
+
+@pytest.mark.parametrize("kind", ["normal", "one sign", "wide", "small"])
+@pytest.mark.parametrize("m,n_out,E", [(5, 64, 0), (64, 256, 0), (2048, 1024, 0), (6, 128, 4), (700, 256, 4)])
+def test_sums_of_one_block(sevo, kind, m, n_out, E):
+    """What the header says of the inner sums, on one block (its scales 1), sums that
+    cancel among them: within the bound of the exact sum, and the sum of the cut
+    products to 2^-20 of the magnitudes (sixteen groups and the stages that join
+    them, each to about 2^-24 of the largest); fp32 results exact to fp32 rounding."""
+    say(f"one block {kind} m={m} n_out={n_out} E={E}")
+    g = gen(m + n_out)
+    k = 128
+    X8 = codes_of(kind, m, k, g)
+    W8 = codes_of(kind, max(E, 1) * n_out, k, g).view(max(E, 1), n_out, k)
+    W8 = torch.stack([cancel(X8, w) for w in W8])
+    w = sevo.sevo_pack_weight_fp8(W8)
+    xs = torch.ones(1, m, device="cuda")
+    ws = torch.ones(max(E, 1), -(-n_out // 128), 1, device="cuda")
+    rows = torch.arange(0, m, max(1, m // 48), device="cuda")
+    if E:
+        ex = (torch.arange(m, device="cuda") % E).to(torch.int32).view(m, 1)
+        out = {BF: sevo.sevo_moe_linear_fp8(X8, xs, w, ws, sevo.sevo_moe_lists(ex, E))}
+    else:
+        out = {t: sevo.sevo_linear_fp8(X8, xs, w[0], ws[0], out_dtype=t) for t in (BF, torch.float32)}
+    worst = 0.0
+    for e in range(max(E, 1)):
+        r = rows[rows % E == e] if E else rows
+        if not r.numel():
+            continue
+        exact, cut, mag, largest = block_sums(X8[r].double(), W8[e].double())
+        for t, y in out.items():
+            err = (y[r].double() - exact).abs()
+            if t == BF:
+                near = (y[r].double() - cut).abs()
+                assert (near <= cut.abs() * 2.0 ** -8 + mag * 2.0 ** -20).all(), "not the sum of the cut products"
+                assert (err <= exact.abs() * 2.0 ** -8 + 7 * 2.0 ** -13 * largest + mag * 2.0 ** -20).all()
+                worst = max(worst, float(((err - exact.abs() * 2.0 ** -8) / mag).max()))
+            else:
+                assert (err <= mag * 144 * 2.0 ** -24).all()
+    say(f"  furthest off: {worst:.1e} of the sum of magnitudes")
