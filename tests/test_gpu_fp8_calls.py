@@ -265,3 +265,81 @@ def test_sums_of_one_block(sevo, kind, m, n_out, E):
             else:
                 assert (err <= mag * 144 * 2.0 ** -24).all()
     say(f"  furthest off: {worst:.1e} of the sum of magnitudes")
+
+
+# ------------------------------------------------------------------ a layer around its attention
+@pytest.mark.parametrize("n", [1, 24, 300])
+def test_attention_half_of_a_layer(sevo, n):
+    """Norm, fp32 QKV product, QK norm + RoPE + append, paged attention, quantiser, output
+    projection, and the norm that adds it: each stage against float64 on what the
+    stage before it gave, and in a graph replayed between eager work."""
+    import oracle.decoder as od
+    from paper_2604_07725_amd import device_inputs as di, synth
+    from tests.gpu_helpers import ATTN_REL_TOL, make_population, to_np
+    say(f"attention half n={n}")
+    hq, hkv, d, H = 8, 2, 128, 512
+    shape = synth.ModelShape(1, H, hq, hkv, d, 256, 256)
+    pop = make_population(np.random.default_rng(n).integers(0, 200, size=n), shuffle=True, seed=4, extra=1)
+    tensors = di.device_weights(shape, 5)
+    model = sevo.sevo_init_model(shape, tensors, max_position=256)
+    pos = torch.from_numpy(pop.lengths.astype(np.int32)).cuda()
+    pt = torch.from_numpy(pop.page_table.astype(np.int32)).cuda()
+    pool0 = di.device_pools(shape, 5, pop.n_pages)[0]
+    g = gen(n)
+    wqkv, wo = weights(((hq + 2 * hkv) * d, H), g), weights((H, hq * d), g)
+    pqkv, po = sevo.sevo_pack_weight_fp8(wqkv[0]), sevo.sevo_pack_weight_fp8(wo[0])
+    gain = normal((H,), g, 0.1, BF) + 1
+    x0 = normal((n, H), g, 2.0)
+
+    def half(x, pool):
+        q8, s8 = sevo.sevo_add_rmsnorm_fp8(x, None, gain, 1e-6)
+        qkv = sevo.sevo_linear_fp8(q8, s8, pqkv, wqkv[1], out_dtype=torch.float32)
+        q = sevo.sevo_qk_norm_rope_append(model, 0, qkv, pos, pt, pool)
+        o = sevo.sevo_attn_decode(q, pool, pt, pos + 1)
+        a8, sa = sevo.sevo_quantize_fp8(o.view(n, hq * d))
+        y = sevo.sevo_linear_fp8(a8, sa, po, wo[1])
+        h8, sh = sevo.sevo_add_rmsnorm_fp8(x, y.unsqueeze(0), gain, 1e-6)
+        return q8, s8, qkv, q, o, a8, sa, y, h8, sh
+
+    x, pool = x0.clone(), pool0.clone()
+    q8, s8, qkv, q, o, a8, sa, y, h8, sh = half(x, pool)
+    check_product(qkv, q8, s8, *wqkv)
+    # bf16 of values whose angles and norms are in fp32: half a step and 2^-16 of the head's largest
+    lw = {k: to_np(v) for k, v in tensors["layers"][0].items() if k in ("q_norm", "k_norm")}
+    heads = to_np(qkv).reshape(n, hq + 2 * hkv, d)
+    p = pop.lengths.astype(np.int64)[:, None]
+    want = od.rope_rotate(od.rms_norm(heads[:, :hq], lw["q_norm"], shape.rms_eps), p, shape.rope_theta)
+    big = np.abs(want).max(-1, keepdims=True)
+    assert np.all(np.abs(to_np(q) - want) <= np.abs(want) * 2.0 ** -8 + big * 2.0 ** -16)
+    kw = od.rope_rotate(od.rms_norm(heads[:, hq:hq + hkv], lw["k_norm"], shape.rms_eps), p, shape.rope_theta)
+    hpool = to_np(pool)
+    ref = np.empty((n, hq, d))
+    for i in range(n):
+        K, V = od.gather_kv(hpool, pop.page_table[i], int(pop.lengths[i]) + 1)
+        big = np.abs(kw[i]).max(-1, keepdims=True)
+        assert np.all(np.abs(K[:, -1] - kw[i]) <= np.abs(kw[i]) * 2.0 ** -8 + big * 2.0 ** -16)
+        v = heads[i, hq + hkv:]
+        assert np.all(np.abs(V[:, -1] - v) <= np.abs(v) * 2.0 ** -8)
+        ref[i] = od.attention_dense(to_np(q[i]), K, V, d ** -0.5)
+    err = np.abs(to_np(o) - ref).max((1, 2)) / np.abs(ref).max((1, 2))
+    assert err.max() <= ATTN_REL_TOL
+    check_codes(a8, sa, o.view(n, hq * d).double(), rel=4 * 2.0 ** -24)
+    check_product(y, a8, sa, *wo)
+    assert torch.equal(x, x0 + y.float())
+    xd = x.double()
+    check_codes(h8, sh, xd / (xd.pow(2).mean(1, keepdim=True) + 1e-6).sqrt() * gain.double(), rel=64 * 2.0 ** -24)
+    # in a graph
+    xg, poolg = x0.clone(), pool0.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        xg.copy_(x0)
+        got = half(xg, poolg)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(xg, x) and torch.equal(poolg.view(torch.int16), pool.view(torch.int16))
+        for a, b in zip(got, (q8, s8, qkv, q, o, a8, sa, y, h8, sh)):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+        half(x0.clone(), pool0.clone())                       # eager work between
+    torch.cuda.synchronize()
+    model.close()
