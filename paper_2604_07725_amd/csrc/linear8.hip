@@ -263,10 +263,11 @@ __global__ __launch_bounds__(256) void linear8_sum_kernel(const float* __restric
 }
 
 // Zeros the output rows of the entries without an expert, which stand behind the lists:
-// every parts-th one, from the part-th on, by a whole workgroup.
-__device__ __forceinline__ void clear_unlisted(const Moe8Args& a, int part, int parts) {
+// every parts-th one, from the part-th on, by a whole workgroup.  listed: the entries
+// with one, offsets[n_experts].
+__device__ __forceinline__ void clear_unlisted(const Moe8Args& a, int listed, int part, int parts) {
   const int nk = a.n * a.top_k;
-  for (int i = a.offsets[a.n_experts] + part; i < nk; i += parts) {
+  for (int i = listed + part; i < nk; i += parts) {
     const int asg = a.assign[i], tok = asg / a.top_k;
     const size_t row = a.down ? (size_t)(asg - tok * a.top_k) * a.n + tok : (size_t)asg;
     for (int c = 8 * threadIdx.x; c < a.n_out; c += 8 * blockDim.x)
@@ -285,8 +286,8 @@ __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, q = lane >> 4;
   const int e = blockIdx.y;
-  if (a.clear) clear_unlisted(a, blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
-  const int off = a.offsets[e], ne = a.offsets[e + 1] - off;
+  const int off = a.offsets[e], ne = a.offsets[e + 1] - off, listed = a.offsets[a.n_experts];
+  if (a.clear) clear_unlisted(a, listed, blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
   const int KB = a.k >> 7, nrb = a.n_out >> 4;
   const int rb0 = blockIdx.x * 8 + 2 * wave;
   if (ne <= 0 || rb0 >= nrb) return;  // wave-uniform, no barrier follows
@@ -399,7 +400,7 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
   // grouped: each lane keeps the first tile, first entry and entries of experts lane + 64 j
   int e_tile[GR ? 4 : 1], e_first[GR ? 4 : 1], e_rows[GR ? 4 : 1];
   if constexpr (GR) {
-    if (g.clear) clear_unlisted(g, blockIdx.x, gridDim.x);
+    const int listed = g.offsets[g.n_experts];
     tiles_m = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -417,6 +418,7 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
       e_tile[j] = in ? tiles_m + incl - tiles : 0x7FFFFFFF;
       tiles_m += __builtin_amdgcn_readlane(incl, 63);
     }
+    if (g.clear) clear_unlisted(g, listed, blockIdx.x, gridDim.x);
   }
   const int total = tiles_m * tiles_n;
 

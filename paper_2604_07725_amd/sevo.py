@@ -10,7 +10,6 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
-import inspect
 import os
 import re
 
@@ -236,34 +235,26 @@ def _tensors(values):
             yield v.buffer
 
 
-def _on_its_stream(fn):
-    """A call with ``stream`` (a torch.cuda.Stream or a raw handle) allocates and
-    fills on that stream too.  The allocator hands memory out in the order of the
-    stream it is asked on: a workspace that belonged to the current stream would be
-    given to the next call while this one's kernels still use it.  What is returned
-    is marked as used by the current stream as well, where the caller may read it;
-    inputs are the caller's to keep until the stream has read them."""
-    at = list(inspect.signature(fn).parameters).index("stream")
-
-    @functools.wraps(fn)
-    def call(*args, **kw):
-        stream = args[at] if len(args) > at else kw.get("stream")
-        if stream is None:
-            return fn(*args, **kw)
-        device = next((t.device for t in _tensors((*args, *kw.values()))), None)
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(getattr(stream, "value", stream) or 0, device=device)
-        elif device is not None and stream.device != device:
-            raise ValueError(f"stream: of {stream.device}, the tensors on {device}")
-        current = torch.cuda.current_stream(device)
-        with torch.cuda.stream(stream):
-            out = fn(*args, **kw)
-        if current.cuda_stream != stream.cuda_stream:
-            for t in _tensors((out,)):
-                t.record_stream(current)
-        return out
-
-    return call
+def _on_stream(stream, fn, *args):
+    """fn(*args) for a call with ``stream`` (a torch.cuda.Stream or a raw handle):
+    what it allocates and fills belongs to that stream too.  The allocator hands
+    memory out in the order of the stream it is asked on: a workspace that belonged to
+    the current stream would be given to the next call while this one's kernels
+    still use it.  What is returned is marked as used by the current stream as well,
+    where the caller may read it; inputs are the caller's to keep until the stream
+    has read them."""
+    device = next(t.device for t in _tensors(args))
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(getattr(stream, "value", stream) or 0, device=device)
+    elif stream.device != device:
+        raise ValueError(f"stream: of {stream.device}, the tensors on {device}")
+    current = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        out = fn(*args)
+    if current.cuda_stream != stream.cuda_stream:
+        for t in _tensors((out,)):
+            t.record_stream(current)
+    return out
 
 
 def _p(t):
@@ -286,11 +277,13 @@ def sevo_attn_workspace_bytes(n, n_q_heads, n_kv_heads, head_dim, max_pages, num
                                                num_splits))
 
 
-@_on_its_stream
 def sevo_attn_decode(q, kv_pool, page_table, seq_lens, out=None, scale=None,
                      num_splits=0, workspace=None, stream=None):
     """o = paged GQA decode attention.  q [n, hq, d] bf16; kv_pool in the paged
     layout [P, hkv, 2, 16 d]; page_table int32 [n, max_pages]; seq_lens int32 [n]."""
+    if stream is not None:
+        return _on_stream(stream, sevo_attn_decode, q, kv_pool, page_table, seq_lens, out, scale,
+                          num_splits, workspace)
     n, hq, d = q.shape
     hkv = kv_pool.shape[1]
     max_pages = page_table.shape[1]
@@ -323,13 +316,15 @@ def sevo_attn_decode_noalloc(q, kv_pool, page_table, seq_lens, out, scale=None, 
 
 
 # ------------------------------------------------------------------ prefill
-@_on_its_stream
 def sevo_attn_prefill(q, kv_pool, page_table, seq_starts, max_seq_len, start_pos=None, out=None,
                       scale=None, stream=None):
     """Causal GQA prefill attention.  q [T, hq, d] bf16 (sequences back to back);
     kv_pool [P, hkv, 2, 16 d]; page_table int32 [n_seqs, max_pages]; seq_starts
     int32 [n_seqs + 1] and start_pos int32 [n_seqs] (or None) on the device;
     max_seq_len: host bound of the sequence lengths."""
+    if stream is not None:
+        return _on_stream(stream, sevo_attn_prefill, q, kv_pool, page_table, seq_starts,
+                          max_seq_len, start_pos, out, scale)
     T, hq, d = q.shape
     hkv = kv_pool.shape[1]
     n_seqs, max_pages = page_table.shape
@@ -350,7 +345,6 @@ def sevo_sample_workspace_bytes(n: int, vocab: int) -> int:
     return int(lib().sevo_sample_workspace_bytes(n, vocab))
 
 
-@_on_its_stream
 def sevo_logprob_sample(logits, temperature, seed, cand_uid, positions, out_tokens=None,
                         out_logprobs=None, workspace=None, stream=None, vocab=None,
                         conf_topk=0, out_conf=None, conf_sum=None, top_k=0, top_p=1.0,
@@ -360,6 +354,10 @@ def sevo_logprob_sample(logits, temperature, seed, cand_uid, positions, out_toke
     ``top_p`` / ``min_p`` inside the top-k set.  With ``conf_topk`` > 0 also the
     per-token self-confidence: returned as a third element (``out_conf``) and/or
     added to ``conf_sum``."""
+    if stream is not None:
+        return _on_stream(stream, sevo_logprob_sample, logits, temperature, seed, cand_uid,
+                          positions, out_tokens, out_logprobs, workspace, None, vocab, conf_topk,
+                          out_conf, conf_sum, top_k, top_p, min_p)
     n = logits.shape[0]
     vocab = logits.shape[1] if vocab is None else vocab
     if conf_topk and out_conf is None:
@@ -381,10 +379,11 @@ def sevo_logprob_sample(logits, temperature, seed, cand_uid, positions, out_toke
     return out_tokens, out_logprobs
 
 
-@_on_its_stream
 def sevo_group_confidence(conf_sum, token_counts, groups, out=None, stream=None):
     """GC [n_groups] from per-candidate confidence sums, token counts (int32)
     and groups int32 [n_groups, K] of candidate indices."""
+    if stream is not None:
+        return _on_stream(stream, sevo_group_confidence, conf_sum, token_counts, groups, out)
     n_groups, k = groups.shape
     if out is None:
         out = torch.empty(n_groups, dtype=torch.float32, device=conf_sum.device)
@@ -394,8 +393,9 @@ def sevo_group_confidence(conf_sum, token_counts, groups, out=None, stream=None)
 
 
 # ------------------------------------------------------------------ sub-steps
-@_on_its_stream
 def sevo_embed(embed, tokens, x=None, stream=None):
+    if stream is not None:
+        return _on_stream(stream, sevo_embed, embed, tokens, x)
     n = tokens.shape[0]
     hidden = embed.shape[1]
     if x is None:
@@ -405,8 +405,9 @@ def sevo_embed(embed, tokens, x=None, stream=None):
     return x
 
 
-@_on_its_stream
 def sevo_rmsnorm(x, gain, eps, out=None, stream=None):
+    if stream is not None:
+        return _on_stream(stream, sevo_rmsnorm, x, gain, eps, out)
     rows, cols = x.shape
     if out is None:
         out = torch.empty(rows, cols, dtype=torch.bfloat16, device=x.device)
@@ -414,11 +415,12 @@ def sevo_rmsnorm(x, gain, eps, out=None, stream=None):
     return out
 
 
-@_on_its_stream
 def sevo_add_rmsnorm(x, partials, gain, eps, out=None, stream=None):
     """x fp32 [rows, cols] += the partials fp32 [S, rows, cols] (in s order; None
     for none), in place; returns RMSNorm(x) * gain as bf16 in the tiled
     activation layout (a flat buffer of ceil(rows / 16) * 16 rows)."""
+    if stream is not None:
+        return _on_stream(stream, sevo_add_rmsnorm, x, partials, gain, eps, out)
     rows, cols = x.shape
     S = 0 if partials is None else partials.shape[0]
     if out is None:
@@ -439,7 +441,6 @@ def sevo_linear_plan(m, n_out, k, k_splits=0, mode=LINEAR_STORE):
     return tuple(int(v) for v in plan)
 
 
-@_on_its_stream
 def sevo_linear(x, w, mode=LINEAR_STORE, out=None, k_splits=0, workspace=None, stream=None,
                 m=None, x_tiled=False, out_tiled=False):
     """Y = x w^T (bf16 in, fp32 accumulate) with the STORE / ADD / SWIGLU epilogue.
@@ -448,6 +449,9 @@ def sevo_linear(x, w, mode=LINEAR_STORE, out=None, k_splits=0, workspace=None, s
     row-major [m, k] (row stride from the tensor), or with ``x_tiled`` a buffer
     in the tiled activation layout, whose row count ``m`` must be given.
     ``out_tiled`` (SWIGLU only) writes the bf16 product in the tiled layout."""
+    if stream is not None:
+        return _on_stream(stream, sevo_linear, x, w, mode, out, k_splits, workspace, None, m,
+                          x_tiled, out_tiled)
     n_out, k = w.shape
     if x_tiled:
         if m is None:
@@ -470,9 +474,10 @@ def sevo_linear(x, w, mode=LINEAR_STORE, out=None, k_splits=0, workspace=None, s
     return out
 
 
-@_on_its_stream
 def sevo_pack_weight(src, kind=PACK_PLAIN, dst=None, stream=None):
     """Row-major bf16 [n_out, k] -> a new tensor of the same shape in the packed layout."""
+    if stream is not None:
+        return _on_stream(stream, sevo_pack_weight, src, kind, dst)
     n_out, k = src.shape
     if dst is None:
         dst = torch.empty_like(src)
@@ -480,9 +485,10 @@ def sevo_pack_weight(src, kind=PACK_PLAIN, dst=None, stream=None):
     return dst
 
 
-@_on_its_stream
 def sevo_pack_kv(k_pool, v_pool, kv_pool=None, stream=None):
     """Plain K and V pools bf16 [pages, hkv, 16, d] -> the fused pool [pages, hkv, 2, 16 d]."""
+    if stream is not None:
+        return _on_stream(stream, sevo_pack_kv, k_pool, v_pool, kv_pool)
     pages, hkv, slots, d = k_pool.shape
     if kv_pool is None:
         kv_pool = torch.empty(pages, hkv, 2, slots * d, dtype=k_pool.dtype, device=k_pool.device)
@@ -491,9 +497,11 @@ def sevo_pack_kv(k_pool, v_pool, kv_pool=None, stream=None):
     return kv_pool
 
 
-@_on_its_stream
 def sevo_qk_norm_rope_append(model, layer, qkv, positions, page_table, kv_pool, q_out=None,
                              stream=None):
+    if stream is not None:
+        return _on_stream(stream, sevo_qk_norm_rope_append, model, layer, qkv, positions,
+                          page_table, kv_pool, q_out)
     n = qkv.shape[0]
     cfg = model.config
     if q_out is None:
@@ -629,7 +637,6 @@ class StepBuffers:
         return self.out_tokens, self.out_logprobs
 
 
-@_on_its_stream
 def sevo_decode_step(model: Model, tokens, positions, page_table, kv_pools, cand_uid,
                      seed, temperature=1.0, num_splits=0, keep_logits=False, stream=None,
                      conf_topk=0, conf_sum=None, top_k=0, top_p=1.0, min_p=0.0,
@@ -638,6 +645,10 @@ def sevo_decode_step(model: Model, tokens, positions, page_table, kv_pools, cand
     [, hidden]), hidden = the residual stream entering each layer and after the
     last [n_layers + 1, n, hidden].  ``workspace``: a caller's uint8 device
     buffer of at least sevo_step_workspace_bytes (else one is allocated)."""
+    if stream is not None:
+        return _on_stream(stream, sevo_decode_step, model, tokens, positions, page_table, kv_pools,
+                          cand_uid, seed, temperature, num_splits, keep_logits, None, conf_topk,
+                          conf_sum, top_k, top_p, min_p, keep_hidden, workspace)
     b = StepBuffers(model, tokens, positions, page_table, kv_pools, cand_uid, seed,
                     temperature, num_splits, keep_logits, conf_topk=conf_topk, conf_sum=conf_sum,
                     top_k=top_k, top_p=top_p, min_p=min_p, keep_hidden=keep_hidden,
@@ -649,11 +660,12 @@ def sevo_decode_step(model: Model, tokens, positions, page_table, kv_pools, cand
 
 
 # ------------------------------------------------------------------ mixture of experts
-@_on_its_stream
 def sevo_moe_ffn(model: Model, layer: int, h_tiled, n: int, stream=None, partials=None):
     """The MoE FFN of one layer on normed inputs in the tiled activation layout
     (n rows).  Returns (experts int32 [n, k], weights fp32 [n, k],
     partials fp32 [k, n, hidden]); ``partials`` may be given (written in full)."""
+    if stream is not None:
+        return _on_stream(stream, sevo_moe_ffn, model, layer, h_tiled, n, None, partials)
     shape = model.shape
     k = shape.top_k
     dev = h_tiled.device
@@ -694,12 +706,12 @@ def _ld(t, rows, cols):
     return t.stride()[0] if rows > 1 else cols
 
 
-def _call(name, i, stream, *args):
-    """The C call on device i, by default on its current stream."""
+def _call(name, i, *args):
+    """The C call on the current stream of device i."""
     if i < 0:
         raise ValueError(f"{name}: tensors on the CPU, expected a GPU")
     # the stream's handle alone: building a Stream object takes longer than the launch
-    s = torch._C._cuda_getCurrentRawStream(i) if stream is None else _stream(stream)
+    s = torch._C._cuda_getCurrentRawStream(i)
     fn = getattr(_lib or lib(), name)
     if torch._C._cuda_getDevice() == i:
         status = fn(*args, s)
@@ -714,13 +726,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-@_on_its_stream
 def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16=None,
                          stream=None):
     """x fp32 [rows, cols] += the partials [S, rows, cols] (fp32 or bf16, in s
     order; None for none), in place; returns RMSNorm(x) * gain in 8 bits: codes
     float8_e4m3fn [rows, cols] and scales fp32 [cols / 128, rows].  ``out_bf16``
     (bf16 [rows, cols]) receives the normed rows too."""
+    if stream is not None:
+        return _on_stream(stream, sevo_add_rmsnorm_fp8, x, partials, gain, eps, out, scales,
+                          out_bf16)
     rows, cols = x.shape
     dev, i = x.device, x.get_device()
     if not (x.dtype is torch.float32 and x.is_contiguous() and gain.dtype is torch.bfloat16 and
@@ -746,15 +760,16 @@ def sevo_add_rmsnorm_fp8(x, partials, gain, eps, out=None, scales=None, out_bf16
         rows, cols, S, BF16 if bf16 else F32, float(eps), x.data_ptr(),
         partials.data_ptr() if S else None, gain.data_ptr(), out.data_ptr(), scales.data_ptr(),
         None if out_bf16 is None else out_bf16.data_ptr())
-    _call("sevo_add_rmsnorm_fp8", i, stream, C.byref(a))
+    _call("sevo_add_rmsnorm_fp8", i, C.byref(a))
     return out, scales
 
 
-@_on_its_stream
 def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
     """bf16 rows [m, k] (row stride from the tensor) to codes float8_e4m3fn [m, k]
     and scales fp32 [k / 128, m]; with ``swiglu`` of silu(gate) * up, x [m, 2 k]
     holding the gate columns, then the up columns."""
+    if stream is not None:
+        return _on_stream(stream, sevo_quantize_fp8, x, swiglu, out, scales)
     m, k = x.shape
     dev, i = x.device, x.get_device()
     if not (x.dtype is torch.bfloat16 and x.is_contiguous()):
@@ -772,15 +787,16 @@ def sevo_quantize_fp8(x, swiglu=False, out=None, scales=None, stream=None):
         scales = torch.empty(k // SCALE_BLOCK, m, dtype=torch.float32, device=dev)
     else:
         _need("scales", scales, torch.float32, (k // SCALE_BLOCK, m), i)
-    _call("sevo_quantize_fp8", i, stream, x.data_ptr(), ldx, m, k, 1 if swiglu else 0,
+    _call("sevo_quantize_fp8", i, x.data_ptr(), ldx, m, k, 1 if swiglu else 0,
           out.data_ptr(), scales.data_ptr())
     return out, scales
 
 
-@_on_its_stream
 def sevo_pack_weight_fp8(src, dst=None, stream=None):
     """Row-major codes float8_e4m3fn [n_out, k] (or [E, n_out, k], the experts of a
     layer) -> a new tensor of the same shape in the packed 8-bit layout."""
+    if stream is not None:
+        return _on_stream(stream, sevo_pack_weight_fp8, src, dst)
     if src.dim() not in (2, 3):
         raise ValueError("src: [n_out, k] or [E, n_out, k]")
     _need("src", src, torch.float8_e4m3fn, None, src.get_device())
@@ -790,7 +806,7 @@ def sevo_pack_weight_fp8(src, dst=None, stream=None):
         dst = torch.empty_like(src)
     _need("dst", dst, torch.float8_e4m3fn, src.shape, src.get_device())
     k = src.shape[-1]
-    _call("sevo_pack_weight_fp8", src.get_device(), stream, _ptr(src), _ptr(dst), src.numel() // max(k, 1), k)
+    _call("sevo_pack_weight_fp8", src.get_device(), _ptr(src), _ptr(dst), src.numel() // max(k, 1), k)
     return dst
 
 
@@ -799,7 +815,6 @@ def sevo_linear_fp8_workspace_bytes(m, n_out, k) -> int:
     return int(lib().sevo_linear_fp8_workspace_bytes(m, n_out, k))
 
 
-@_on_its_stream
 def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16, workspace=None,
                     stream=None):
     """Y = X W^T of 8-bit operands: x codes [m, k] (row stride from the tensor) with
@@ -807,6 +822,9 @@ def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16
     scales [ceil(n_out / 128), k / 128].  Y bf16, or fp32 (``out_dtype``, or the
     type of ``out``, whose row stride is kept).  ``workspace``: a caller's uint8
     buffer of sevo_linear_fp8_workspace_bytes (else one is allocated)."""
+    if stream is not None:
+        return _on_stream(stream, sevo_linear_fp8, x, x_scales, w, w_scales, out, out_dtype,
+                          workspace)
     f8, f32t = torch.float8_e4m3fn, torch.float32
     m, k = x.shape
     n_out = w.shape[0]
@@ -840,11 +858,10 @@ def sevo_linear_fp8(x, x_scales, w, w_scales, out=None, out_dtype=torch.bfloat16
     a = LinearFp8Args(m, n_out, k, F32 if kind is f32t else BF16, _ld(x, m, k), _ld(x_scales, kb, m),
                       ldo, x.data_ptr(), x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(),
                       out.data_ptr(), None if workspace is None else workspace.data_ptr(), need)
-    _call("sevo_linear_fp8", i, stream, C.byref(a))
+    _call("sevo_linear_fp8", i, C.byref(a))
     return out
 
 
-@_on_its_stream
 def sevo_moe_route(logits, top_k, score="softmax", bias=None, n_groups=1, top_groups=1,
                    group_best=1, renormalise=True, scaling=1.0, out_experts=None,
                    out_weights=None, stream=None):
@@ -852,6 +869,9 @@ def sevo_moe_route(logits, top_k, score="softmax", bias=None, n_groups=1, top_gr
     [n, n_experts] (row stride from the tensor): ``score`` "softmax" or "sigmoid",
     a balance ``bias`` fp32 [n_experts] on the choice, the ``top_groups`` of
     ``n_groups`` expert groups by the sum of their ``group_best`` best."""
+    if stream is not None:
+        return _on_stream(stream, sevo_moe_route, logits, top_k, score, bias, n_groups, top_groups,
+                          group_best, renormalise, scaling, out_experts, out_weights)
     if score not in ("softmax", "sigmoid"):
         raise ValueError(f"score: {score!r}")
     n, E = logits.shape
@@ -872,7 +892,7 @@ def sevo_moe_route(logits, top_k, score="softmax", bias=None, n_groups=1, top_gr
                      int(n_groups), int(top_groups), int(group_best), 1 if renormalise else 0,
                      float(scaling), _ld(logits, n, E),
                      logits.data_ptr(), _ptr(bias), out_experts.data_ptr(), out_weights.data_ptr())
-    _call("sevo_moe_route", i, stream, C.byref(a))
+    _call("sevo_moe_route", i, C.byref(a))
     return out_experts, out_weights
 
 
@@ -888,10 +908,11 @@ def sevo_moe_lists_bytes(n, top_k, n_experts) -> int:
     return int(lib().sevo_moe_lists_bytes(n, top_k, n_experts))
 
 
-@_on_its_stream
 def sevo_moe_lists(experts, n_experts, buffer=None, stream=None) -> MoeLists:
     """Entry lists of experts int32 [n, top_k] for ``sevo_moe_linear_fp8``.
     ``buffer``: a caller's uint8 buffer of sevo_moe_lists_bytes."""
+    if stream is not None:
+        return _on_stream(stream, sevo_moe_lists, experts, n_experts, buffer)
     n, top_k = experts.shape
     i = experts.get_device()
     _need("experts", experts, torch.int32, (n, top_k), i)
@@ -900,12 +921,11 @@ def sevo_moe_lists(experts, n_experts, buffer=None, stream=None) -> MoeLists:
                              device=experts.device)
     else:
         _need("buffer", buffer, torch.uint8, None, i)
-    _call("sevo_moe_lists", i, stream, _ptr(experts), n, top_k, int(n_experts),
+    _call("sevo_moe_lists", i, _ptr(experts), n, top_k, int(n_experts),
           _ptr(buffer), buffer.numel())
     return MoeLists(n, top_k, int(n_experts), buffer)
 
 
-@_on_its_stream
 def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None, out=None,
                         stream=None):
     """The experts' products of a routing, bf16.  Without ``weights``: gate/up, x
@@ -913,6 +933,9 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
     down, x codes [n * top_k, k], returns the weighted partials [top_k, n, n_out].
     w packed codes [E, n_out, k], w_scales [E, ceil(n_out / 128), k / 128].  The rows
     of entries whose expert id is outside [0, E) are zero, or with ``out`` as they were."""
+    if stream is not None:
+        return _on_stream(stream, sevo_moe_linear_fp8, x, x_scales, w, w_scales, lists, weights,
+                          out)
     f8 = torch.float8_e4m3fn
     n, top_k, E = lists.n, lists.top_k, lists.n_experts
     down = weights is not None
@@ -939,15 +962,16 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
                          _ld(x_scales, k // SCALE_BLOCK, rows), x.data_ptr(),
                          x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr(), _ptr(weights),
                          lists.buffer.data_ptr(), out.data_ptr(), 1 if clear else 0)
-    _call("sevo_moe_linear_fp8", i, stream, C.byref(a))
+    _call("sevo_moe_linear_fp8", i, C.byref(a))
     return out
 
 
 # ------------------------------------------------------------------ read probe
-@_on_its_stream
 def sevo_hbm_read_probe(buf, page_order=None, grid=32768, sink=None, stream=None):
     """Read every byte of the device tensor ``buf`` once (sequentially, or as
     8 KB pages in the int32 order ``page_order``); returns the sink tensor."""
+    if stream is not None:
+        return _on_stream(stream, sevo_hbm_read_probe, buf, page_order, grid, sink)
     if sink is None:
         sink = torch.empty(grid * 16, dtype=torch.uint8, device=buf.device)
     nbytes = buf.numel() * buf.element_size()
