@@ -92,8 +92,8 @@ __device__ __forceinline__ void store4(void* out, size_t off, const f32x4& v, in
     *reinterpret_cast<f32x4*>(static_cast<float*>(out) + off) = v;
 }
 
-// Direct global -> LDS load of N bytes per lane at voff (checked against the
-// records) + soff (wave-uniform, not checked); lane i's bytes land at lds + N i.
+// Direct global -> LDS load of N bytes per lane at voff + soff (wave-uniform; the sum is
+// checked against the records, so both have to fit in them); lane i's bytes land at lds + N i.
 // ONCE: data that nothing else reads, past the caches.
 template <int N, bool ONCE = false>
 __device__ __forceinline__ void dma_s(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t soff,
@@ -116,7 +116,7 @@ __device__ __forceinline__ void dma_s(__amdgpu_buffer_rsrc_t r, uint32_t voff, u
 // the products of a third (three or four: no faster, 16 x 6144 x 4096 7.6 / 7.6 / 8.2).
 // Measured in graphs, weights cold: 8 x 51200 x 5120 52.7 us (5.0 TB/s), 16 x 6144 x 4096 7.6
 // (3.3), of which 3.4 a launch; from 32 rows on the CU's path from L2 bounds it, on which
-// the activations come too: 64 x 4096 x 12288 19.2 (2.7).  M tiles of 64 rows read the
+// the activations come too: 64 x 4096 x 12288 in four splits 14.0 (3.6), their sum 3.9.  M tiles of 64 rows read the
 // weights half as often as those of 32: 64 x 10240 x 5120 to fp32 24.1 -> 20.4 (LDS tiles
 // before), 128 x 6144 x 4096 to fp32 19.9 -> 15.5, 203 x 4096 x 4096 16.2 -> 14.3.
 template <int MB, int RB, bool EXACT>
@@ -278,9 +278,10 @@ __device__ __forceinline__ void clear_unlisted(const Moe8Args& a, int listed, in
 // The product grouped by expert for few entries an expert: a stream of the chosen
 // experts' weights.  A wave takes two 16-row weight blocks of one expert over the
 // whole k, a workgroup 128 rows (one row of weight scales); the expert's entries come
-// 16 at a time, gathered through its list (more than 16 read its weights again,
-// mostly from a cache).
-// 30B-A3B gate/up of 64 tokens, 8 of 128 experts each: 63 us, 6.3 TB/s.
+// 16 at a time, gathered through its list, and each 16 read its weights again.
+// 30B-A3B gate/up of 64 tokens, 8 of 128 experts each: 63 us, 6.3 TB/s.  Where tokens
+// agree few experts have long lists: the same 8 for all 64 (four passes over 25 MB)
+// 38 us, 16 between them 30, one expert in every token's 8 77.
 __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -366,7 +367,8 @@ __global__ __launch_bounds__(256) void moe8_kernel(Moe8Args a) {
 // Grouped (GR): the m-tiles are tiles of the experts' lists and a tile's rows are
 // gathered per lane.
 // Bounds: large products the matrix cores, at the clock that the power allows (8192 x
-// 24576 x 4096 677 us, 2.43 PFLOP/s; the library's product with one scale 658); some
+// 24576 x 4096 665 to 707 us by the card, 2.3 to 2.5 PFLOP/s; the library's product with one
+// scale 658); some
 // hundred rows the reads from LDS, 0.38 us a stage of 128 x 128 x 128 alone on a CU, and
 // the way from L2, 0.5 to 0.6 with all CUs busy (512 x 8192 x 5120 29 us).
 template <int BM, int BN, int NW, int NS, bool EXACT, bool GR>
@@ -528,9 +530,10 @@ __global__ __launch_bounds__(64 * NW) void tile8_kernel(Linear8Args a, int kb_ch
     for (int i = 0; i <= D; ++i) {
       if (i < i0 || i >= i1) continue;
       if (i < DW) {
-        // (an expert with so few entries has one tile, and its weights are read once: 12
-        // entries an expert 81.5 + 51 -> 77.5 + 47 us; with tiles that share them it costs
-        // 5%)
+        // (32-row tiles are for 32 entries an expert or fewer on average.  Where these are
+        // spread evenly an expert has one tile and its weights are read once: 12 entries
+        // an expert 81.5 + 51 -> 77.5 + 47 us.  An expert with a longer list has more tiles,
+        // which read its weights past the caches too: with tiles that share them it costs 5%.)
         dma_s<16, GR && BM == 32>(rsrc(wb), lane * 16, (st0 + st) * 8192 + w_soff[i],
                                   so + BM * 128 + (wave + NW * i) * 1024);
       } else if (i == DW + XH) {
@@ -948,7 +951,11 @@ hipError_t launch_linear8(const Linear8Args& a, const Linear8Plan& p, float* wor
 // 46 / 88 + 51; 24 - / 79 + 47 / 81 + 50 / 87 + 56; 32 - / 92 + 53 / 93 + 57 / 90 + 55; 40 - / 98 +
 // 60 / 94 + 59; 64 - / 116 + 70 / 97 + 62 / 96 + 63; 128 - / - / 119 + 74 / 125 + 82; 200 - / - /
 // 149 + 103 / 153 + 99; 256 - / - / 173 + 122 / 166 + 111; 512 - / - / 288 + 204 / 264 + 189).  64
-// rows were never the best by more than 2%.
+// rows were never the best by more than 2%.  The lists' own lengths are on the device: the
+// rule goes by their mean, and these times are of independent routings.  Where tokens agree
+// the same rule gives, independent / 16 experts / the same 8 for every token: 64 tokens
+// 65 + 35 / 30 + 16 / 38 + 20; 256 72 + 41 / 31 + 24 / 28 + 15; 512 93 + 53 / 54 + 34 / 43 + 27;
+// 4096 166 + 108 / 120 + 76 / 101 + 67.
 constexpr int kStreamEntries = 4;
 
 namespace {

@@ -3,7 +3,8 @@
 Every function here packs torch tensors into the C structs of
 ``include/sevo.h`` and calls the same-named C entry point; all arithmetic of
 the decode step runs in the HIP kernels of the library.  PyTorch provides
-device memory and the current stream.  There is no fallback: a missing or
+device memory and the current stream; a call with ``stream`` runs on that one
+and what it returns belongs to it.  There is no fallback: a missing or
 unloadable library raises.
 """
 from __future__ import annotations
