@@ -246,7 +246,9 @@ def _on_stream(stream, fn, *args):
     has read them."""
     device = next(t.device for t in _tensors(args))
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(getattr(stream, "value", stream) or 0, device=device)
+        handle = getattr(stream, "value", stream)
+        stream = (torch.cuda.ExternalStream(handle, device=device) if handle
+                  else torch.cuda.default_stream(device))  # (of 0 torch would make a new stream)
     elif stream.device != device:
         raise ValueError(f"stream: of {stream.device}, the tensors on {device}")
     current = torch.cuda.current_stream(device)

@@ -343,3 +343,49 @@ def test_attention_half_of_a_layer(sevo, n):
         half(x0.clone(), pool0.clone())                       # eager work between
     torch.cuda.synchronize()
     model.close()
+
+
+def test_stream_arguments_in_a_graph(sevo):
+    """A capture that forks to a stream of its own and joins it: what the calls there
+    allocate is the graph's, and every replay gives the eager bits."""
+    g = gen(32)
+    m, n_out, k = 48, 512, 12288
+    assert sevo.sevo_linear_fp8_workspace_bytes(m, n_out, k) > 0
+    wq, ws = weights((n_out, k), g)
+    w = sevo.sevo_pack_weight_fp8(wq)
+    x = normal((m, k), g, 1.0, BF)
+    side = torch.cuda.Stream()
+
+    def both(s):
+        here = torch.cuda.current_stream()
+        s.wait_stream(here)
+        a = sevo.sevo_linear_fp8(*sevo.sevo_quantize_fp8(x, stream=s), w, ws, stream=s)
+        b = sevo.sevo_linear_fp8(*sevo.sevo_quantize_fp8(-x), w, ws)
+        here.wait_stream(s)
+        return a, b, a.float() + b.float()
+
+    want = [t.clone() for t in both(side)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both(side)
+    for turn in range(4):
+        x.copy_(normal((m, k), gen(turn), 1.0, BF))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in both(side)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), turn
+
+
+def test_default_stream_by_its_handle(sevo):
+    x = normal((8, 256), gen(2), 1.0, BF)
+    want = sevo.sevo_quantize_fp8(x)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = sevo.sevo_quantize_fp8(x, stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0].view(torch.uint8), want[0].view(torch.uint8)) and torch.equal(got[1], want[1])
+    assert stream_of(got[0]) == 0
