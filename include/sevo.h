@@ -603,7 +603,8 @@ size_t sevo_moe_workspace_bytes(const sevo_model* m, int32_t n);
  * x fp32 [rows][cols]; partials fp32 or bf16 (partial_type) [n_partials][rows]
  * [cols], NULL when n_partials = 0; gain bf16 [cols]; out [rows][cols]; scales
  * fp32 [cols / 128][rows]; out_bf16 row-major [rows][cols].  cols % 128 == 0, at
- * most 32768; 0 <= n_partials <= 16.  A row's result does not depend on the
+ * most 32768; 0 <= n_partials <= 16; rows of 2^32 threads or more (64 a row up to
+ * 512 columns, 1024 beyond 4096: 4 million rows) are UNSUPPORTED.  A row's result does not depend on the
  * other rows.  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP. */
 typedef struct {
   int32_t rows, cols, n_partials, partial_type;
@@ -622,7 +623,8 @@ sevo_status sevo_add_rmsnorm_fp8(const sevo_add_rmsnorm_fp8_args* a, void* strea
  * output projection); swiglu 1: y = silu(x[:, :k]) * x[:, k:], x [m][2 k] (a
  * gate/up product before the down projection), in fp32.  ldx: row stride of x in
  * elements, a multiple of 8, at least k (2 k); out [m][k]; scales [k / 128][m].
- * k % 128 == 0.  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP. */
+ * k % 128 == 0; m up to 2^28 / ceil(k / 512) - 16.  Errors: INVALID_ARGUMENT, UNSUPPORTED,
+ * HIP. */
 sevo_status sevo_quantize_fp8(const void* x, int64_t ldx, int32_t m, int32_t k, int32_t swiglu,
                               void* out, float* scales, void* stream);
 
@@ -683,7 +685,7 @@ size_t sevo_linear_fp8_workspace_bytes(int32_t m, int32_t n_out, int32_t k);
  * Ties go to the lower group and the lower expert; a NaN is chosen after every
  * other value, so top_k distinct experts always come back.
  *   out_experts int32 [n][top_k]; out_weights fp32 [n][top_k].
- * n_experts 1..256; top_k 1..16; n_experts % n_groups == 0, n_groups <= 64,
+ * n up to 2^28 - 16; n_experts 1..256; top_k 1..16; n_experts % n_groups == 0, n_groups <= 64,
  * group_best <= n_experts / n_groups, top_k <= top_groups n_experts / n_groups.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP. */
 #define SEVO_ROUTE_SOFTMAX 0

@@ -235,6 +235,9 @@ struct AddNormFp8Args {
   bf16_t* out_bf16;      // the normed rows in bf16 too (null: none)
 };
 hipError_t launch_add_rmsnorm_fp8(const AddNormFp8Args& a, hipStream_t st);
+// Rows that one launch holds (fewer than 2^32 threads)
+int64_t add_rmsnorm_fp8_max_rows(int cols);
+int64_t quantize_fp8_max_rows(int k);
 // x [m][k] (swiglu: [m][2 k], gate columns then up) with row stride ldx
 hipError_t launch_quantize_fp8(const bf16_t* x, int64_t ldx, int m, int k, int swiglu, uint8_t* out,
                                float* scales, hipStream_t st);

@@ -136,6 +136,10 @@ __global__ __launch_bounds__(T) void add_rmsnorm_fp8_kernel(AddNormFp8Args a, in
   }
 }
 
+int64_t add_rmsnorm_fp8_max_rows(int cols) {  // a workgroup each, of the most threads that cols takes
+  return (((int64_t)1 << 32) - 1) / (cols <= 512 ? 64 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024);
+}
+
 hipError_t launch_add_rmsnorm_fp8(const AddNormFp8Args& a, hipStream_t st) {
   if (a.rows == 0) return hipSuccess;
   // Partials are read past the caches once a call's data cannot stay in the last-level
@@ -197,6 +201,10 @@ __global__ __launch_bounds__(256) void quantize_fp8_kernel(const bf16_t* __restr
     if (j == i) keep = s;
   }
   if (j < R && r0 + j < m) scales[(size_t)(c >> 7) * m + r0 + j] = keep;
+}
+
+int64_t quantize_fp8_max_rows(int k) {  // four rows of 512 columns a wave, four waves a workgroup
+  return (((int64_t)1 << 26) - 4) / ((k + 511) / 512) * 4;
 }
 
 hipError_t launch_quantize_fp8(const bf16_t* x, int64_t ldx, int m, int k, int swiglu, uint8_t* out,

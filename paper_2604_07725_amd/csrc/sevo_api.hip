@@ -1483,6 +1483,8 @@ SEVO_API sevo_status sevo_add_rmsnorm_fp8(const sevo_add_rmsnorm_fp8_args* a, vo
     return fail(SEVO_ERR_INVALID_ARGUMENT, "partial_type %d", a->partial_type);
   if (a->cols % 128 || a->cols > 32768)
     return fail(SEVO_ERR_UNSUPPORTED, "cols %d must be a multiple of 128, at most 32768", a->cols);
+  if (a->rows > sevo::add_rmsnorm_fp8_max_rows(a->cols))
+    return fail(SEVO_ERR_UNSUPPORTED, "rows %d of %d columns: fewer a call", a->rows, a->cols);
   if (a->rows == 0) return SEVO_OK;
   if (bad_ptr(a->x) || bad_ptr(a->gain) || bad_ptr(a->out) || bad_ptr(a->scales) ||
       (a->n_partials > 0 && bad_ptr(a->partials)) || (a->out_bf16 && !aligned16(a->out_bf16)))
@@ -1504,6 +1506,8 @@ SEVO_API sevo_status sevo_quantize_fp8(const void* x, int64_t ldx, int32_t m, in
     return fail(SEVO_ERR_INVALID_ARGUMENT, "m %d, k %d, swiglu %d", m, k, swiglu);
   if (k % 128 || k >= 1 << 24)
     return fail(SEVO_ERR_UNSUPPORTED, "k %d must be a multiple of 128 below 2^24", k);
+  if (m > sevo::quantize_fp8_max_rows(k))
+    return fail(SEVO_ERR_UNSUPPORTED, "m %d of %d columns: fewer rows a call", m, k);
   if (ldx < (int64_t)k * (1 + swiglu) || ldx % 8)
     return fail(SEVO_ERR_INVALID_ARGUMENT, "ldx %lld must be a multiple of 8, at least the row",
                 (long long)ldx);
@@ -1588,6 +1592,8 @@ SEVO_API sevo_status sevo_moe_route(const sevo_moe_route_args* a, void* stream) 
                 "n_groups %d, top_groups %d, group_best %d do not fit %d experts, %d a token",
                 a->n_groups, a->top_groups, a->group_best, a->n_experts, a->top_k);
   if (a->ld < a->n_experts) return fail(SEVO_ERR_INVALID_ARGUMENT, "ld %lld", (long long)a->ld);
+  if (a->n > (1 << 28) - 16)  // (16 threads a token, 2^32 in a launch)
+    return fail(SEVO_ERR_UNSUPPORTED, "n %d: fewer tokens a call", a->n);
   if (a->n == 0) return SEVO_OK;
   if (!a->logits || !a->out_experts || !a->out_weights)
     return fail(SEVO_ERR_INVALID_ARGUMENT, "null pointer");

@@ -60,3 +60,22 @@ def test_sizes_near_the_end_of_int32():
     a = dict(n=4, top_k=2, n_experts=8, n_out=top - 64, k=128, down=0, ldx=128, lds=4, x=F, x_scales=F,
              w=F, w_scales=F, lists=F, out=F)
     assert L.sevo_moe_linear_fp8(C.byref(sevo.MoeLinearFp8Args(**a)), None) == sevo.UNSUPPORTED
+
+
+def test_rows_of_more_than_a_launch():
+    """Calls of 2^32 threads and more are refused on the host, whatever the launch
+    would do with them."""
+    L = sevo.lib()
+    for rows, cols in ((1 << 26, 512), (1 << 24, 2048), (1 << 23, 4096), (1 << 22, 32768)):
+        a = dict(rows=rows, cols=cols, n_partials=0, eps=1e-6, x=F, gain=F, out=F, scales=F)
+        assert L.sevo_add_rmsnorm_fp8(C.byref(sevo.AddRmsnormFp8Args(**a)), None) == sevo.UNSUPPORTED
+        a.update(rows=rows - 1, x=0)                                   # one fewer: the next check
+        assert L.sevo_add_rmsnorm_fp8(C.byref(sevo.AddRmsnormFp8Args(**a)), None) == sevo.INVALID_ARGUMENT
+    for m, k in ((1 << 28, 512), (1 << 24, 8192)):
+        assert L.sevo_quantize_fp8(F, k, m, k, 0, F, F, None) == sevo.UNSUPPORTED
+        assert L.sevo_quantize_fp8(0, k, m - 16, k, 0, F, F, None) == sevo.INVALID_ARGUMENT
+    a = dict(n=1 << 28, n_experts=1, top_k=1, n_groups=1, top_groups=1, group_best=1, scaling=1.0, ld=1,
+             logits=F, out_experts=F, out_weights=F)
+    assert L.sevo_moe_route(C.byref(sevo.MoeRouteArgs(**a)), None) == sevo.UNSUPPORTED
+    a.update(n=(1 << 28) - 16, logits=0)
+    assert L.sevo_moe_route(C.byref(sevo.MoeRouteArgs(**a)), None) == sevo.INVALID_ARGUMENT
