@@ -742,6 +742,144 @@ typedef struct {
 
 sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void* stream);
 
+/* ------------------------------------------------------------------ 8-bit cache
+ * The paged KV cache in 8 bits (OCP e4m3 codes, an fp32 scale for each token and
+ * kv head of K and of V): half the bytes of the bf16 cache, the page size, page
+ * tables and page order its own, one pool per layer:
+ *     pool uint8 [num_pages][n_kv_heads][SEVO_KV8_TILE_BYTES(head_dim)]; per (page, kv head)
+ *     K codes   element (slot s, dim e) at (e/64)*1024 + s*64 + e%64
+ *     V codes   16 head_dim bytes further, element (s, e) at (e/64)*1024 + (s/4)*256
+ *               + (e%16)*16 + ((e/16)%4)*4 + s%4
+ *     scales    32 head_dim bytes in: fp32 [16] of K, then fp32 [16] of V, one a slot
+ * A block is the head_dim values y of one token and head: scale = max(max |y| / 448,
+ * 2^-64), code = y times the fp32 reciprocal of the scale, rounded to nearest even.  A
+ * block that holds a NaN or an infinity gets the scale NaN and the codes 0: whoever sees
+ * the token gets a NaN, whoever does not is left alone.
+ * head_dim 64 or 128 (else UNSUPPORTED).  Here and below, arrays of int32 and of single fp32
+ * numbers (ids, lengths, positions, page tables, uniform numbers, tokens, log-probabilities)
+ * need 4-byte alignment only. */
+#define SEVO_KV8_TILE_BYTES(head_dim) (32 * (head_dim) + 128)
+
+/* sevo_qk_norm_rope_append into the 8-bit cache, for one or more tokens a candidate
+ * (drafted tokens behind the last one, a prefill's): K after norm and RoPE, and V, are
+ * quantised from fp32.
+ *   qkv fp32 [n][(n_q_heads + 2 n_kv_heads) head_dim];  positions int32 [n]
+ *   rows int32 [n]: token i's row of the page table, NULL: row i
+ *   page_table int32 [n_rows][max_pages];  q_out bf16 [n][n_q_heads][head_dim]
+ * A token whose position is outside [0, max_position) gets q = 0 and is not appended; nor is
+ * one whose row, page or page id is outside the table or the pool: a padded batch gives
+ * its spare tokens the position -1.  Tokens of one call have slots of their own (of two
+ * with one slot, either may be kept, byte by byte).  n below 2^24.  Errors:
+ * INVALID_ARGUMENT, UNSUPPORTED, HIP. */
+sevo_status sevo_qk_norm_rope_append_fp8(const sevo_model* m, int32_t layer, const float* qkv,
+                                         int32_t n, const int32_t* positions, const int32_t* rows,
+                                         const int32_t* page_table, int32_t n_rows,
+                                         int32_t max_pages, int64_t num_pages, void* q_out,
+                                         void* kv_pool, void* stream);
+
+/* Pages of the bf16 pool -> pages of an 8-bit pool (a prefill's cache before a decode on
+ * 8 bits), and back (an 8-bit cache for sevo_attn_prefill; each value code * scale
+ * rounded to bf16).  Entry j copies page src_pages[j] to page dst_pages[j] (int32 [count],
+ * NULL: page j), all kv heads and all 16 slots.  A source id outside [0,
+ * src_num_pages) gives a page of zeros, a destination id outside [0, dst_num_pages) drops the
+ * entry; destinations differ from each other.  The pools must not overlap.  count up
+ * to 2^31 / n_kv_heads (more: UNSUPPORTED), 0 is a no-op; with NULL ids at most the pool's
+ * pages (INVALID_ARGUMENT).  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP. */
+typedef struct {
+  int32_t n_kv_heads, head_dim;
+  int64_t count, src_num_pages, dst_num_pages;
+  const void* src;
+  void* dst;
+  const int32_t* src_pages;
+  const int32_t* dst_pages;
+} sevo_kv_pages_args;
+
+sevo_status sevo_pack_kv_fp8(const sevo_kv_pages_args* a, void* stream);   /* bf16 -> 8 bits */
+sevo_status sevo_unpack_kv_fp8(const sevo_kv_pages_args* a, void* stream); /* 8 bits -> bf16 */
+
+/* sevo_attn_decode over the 8-bit cache, for n_tokens new tokens a candidate (1: a decode
+ * step; more: the last token and drafts behind it).  Candidate i has m_i =
+ * q_lens[i] new tokens (NULL: n_tokens; taken into [0, n_tokens]), the last m_i of its seq_lens[i]
+ * keys; token t sees the keys up to its own:
+ *   o[i][t][j] = softmax_u(scale * q[i][t][j] . K_i[c][u]) V_i[c][u],
+ *   u < seq_lens[i] - m_i + t + 1,  c = j / (n_q_heads / n_kv_heads).
+ *   q, out   bf16 [n][n_tokens][n_q_heads][head_dim];  a row that sees no key gets 0
+ *   rows t >= m_i of out are left as they were, or set to 0 with clear_rest 1
+ *   page_table int32 [n][max_pages];  seq_lens int32 [n], 0 <= len <= 16 max_pages
+ * n_tokens 1..16; n_q_heads / n_kv_heads any whole number up to 16.  A page id outside
+ * [0, num_pages) contributes no keys.  The cache is cut into splits by the lengths of
+ * all candidates (on the device) and joined in split order: the same call gives the same
+ * bits, those of a row may depend on the other candidates' lengths.  Scores, softmax
+ * statistics and sums in fp32.  The workspace is scratch of
+ * sevo_attn_fp8_workspace_bytes (0: may be NULL); calls that may overlap in time each need
+ * their own.  Errors: INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP. */
+typedef struct {
+  int32_t n, n_tokens, n_q_heads, n_kv_heads, head_dim, page_size, max_pages, clear_rest;
+  int64_t num_pages;
+  const void* q;
+  const void* kv_pool;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  const int32_t* q_lens;
+  float scale;
+  void* out;
+  void* workspace;
+  size_t workspace_bytes;
+} sevo_attn_fp8_args;
+
+sevo_status sevo_attn_decode_fp8(const sevo_attn_fp8_args* a, void* stream);
+size_t sevo_attn_fp8_workspace_bytes(int32_t n, int32_t n_tokens, int32_t n_q_heads,
+                                     int32_t n_kv_heads, int32_t head_dim, int32_t max_pages);
+
+/* ------------------------------------------------------------------ drafted tokens
+ * Verification of n_drafts drafted tokens a candidate against the target model
+ * (speculative sampling), from given uniform numbers.  With p_t = softmax(logits row t /
+ * temperature) of candidate i and q_t = softmax(draft_logits row t / temperature) -- NULL:
+ * every draft is certain, q_t(x_t) = 1 -- and m_i = counts[i] drafts (NULL: n_drafts; taken into
+ * [0, n_drafts]):
+ *   draft t is accepted while u_t q_t(x_t) < p_t(x_t), t = 0, 1, .. < m_i
+ *   behind the a_i accepted ones one more token is drawn: where a draft was rejected from
+ *   max(p_t - q_t, 0), normalised (from p_t where nothing of it is left, or the draft row
+ *   holds a NaN), else from p of row m_i; the first index at which the running sum in
+ *   index order exceeds u_last times the total.
+ * So the emitted tokens are distributed as samples of the target.  temperature 0: a draft is
+ * accepted if it is the row's largest logit (ties -> lowest index), which is also the token
+ * behind them; log-probabilities under T = 1.  A draft id outside the vocabulary is
+ * rejected.  A row whose logits hold a NaN or a +inf, or nothing above -inf, accepts nothing
+ * and draws the id -1 with the log-probability NaN.
+ * Exponentials and sums are in float64 (a choice is a comparison of sums over the
+ * vocabulary), so are temperature and the comparisons.
+ *   logits fp32 [n][n_drafts + 1] rows of stride ld: row t of a candidate follows its
+ *     token t (0: the last token before the drafts); rows t > m_i are not read
+ *   draft_logits fp32 [n][n_drafts] rows of stride ld_draft, or NULL
+ *   draft_tokens int32 [n][n_drafts];  uniforms fp32 [n][n_drafts + 1] in [0, 1), the last
+ *     of each row for the drawn token;  counts int32 [n] or NULL
+ *   out_tokens int32 [n][n_drafts + 1]: accepted, drawn, then -1
+ *   out_logprobs fp32 [n][n_drafts + 1]: log p_t of each emitted token, then 0
+ *   out_accepted int32 [n]: a_i (a_i + 1 tokens are emitted)
+ * n_drafts 0..16 (0: draft_tokens may be NULL); ld, ld_draft multiples of 4, at least
+ * vocab; vocab up to 2^24.  The workspace is scratch of sevo_verify_workspace_bytes; calls
+ * that may overlap in time each need their own.  Errors: INVALID_ARGUMENT, UNSUPPORTED,
+ * WORKSPACE_TOO_SMALL, HIP. */
+typedef struct {
+  int32_t n, n_drafts, vocab;
+  int64_t ld, ld_draft;
+  double temperature;
+  const float* logits;
+  const float* draft_logits;
+  const int32_t* draft_tokens;
+  const float* uniforms;
+  const int32_t* counts;
+  int32_t* out_tokens;
+  float* out_logprobs;
+  int32_t* out_accepted;
+  void* workspace;
+  size_t workspace_bytes;
+} sevo_verify_args;
+
+sevo_status sevo_verify_drafts(const sevo_verify_args* a, void* stream);
+size_t sevo_verify_workspace_bytes(int32_t n, int32_t n_drafts, int32_t vocab);
+
 /* ------------------------------------------------------------------ utilities */
 
 /* Streaming-read microbenchmark (measurement tooling, not part of the decode

@@ -286,6 +286,68 @@ struct Moe8Args {
 };
 hipError_t launch_moe8(const Moe8Args& a, hipStream_t st);
 
+// ---- kv8.hip: the paged 8-bit cache (layout in kv8.h)
+// page-table rows of a call: [0, n_rows); a token whose row, position or page id is outside
+// is not appended
+hipError_t launch_append8(const RopeAppendArgs& a, int n_rows, uint8_t* pool, hipStream_t st);
+struct KvPagesArgs {
+  int hkv, d;
+  int64_t count, src_num_pages, dst_num_pages;  // count hkv < 2^31
+  const void* src;
+  void* dst;
+  const int32_t* src_pages;  // [count], null: 0, 1, ..
+  const int32_t* dst_pages;
+};
+// to8: bf16 pool -> 8-bit pool, else back
+hipError_t launch_pack_kv8(const KvPagesArgs& a, int to8, hipStream_t st);
+
+// ---- attn_decode8.hip
+constexpr int kAttn8MinChunk = 32;      // pages of a split, at least (but for a candidate's only one)
+constexpr int kAttn8Workgroups = 2048;  // workgroups aimed at where the pages allow
+struct Attn8Plan {
+  int nc, col_tiles;  // column tiles of 16 query rows per workgroup; workgroups per kv head and split
+  int target;         // splits aimed at, over all candidates
+  long long max_splits;
+};
+Attn8Plan plan_attn8(int n, int hq, int hkv, int tokens, int max_pages);
+struct Attn8Args {
+  int n, tokens, hq, hkv, d, max_pages, clear_rest;
+  int col_tiles, target, max_splits;
+  int64_t num_pages;
+  const bf16_t* q;  // [n][tokens][hq][d]
+  const uint8_t* kv_pool;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  const int32_t* q_lens;  // null: every candidate has `tokens` new ones
+  float scale_log2;
+  bf16_t* out;
+  float* part_ml;   // [max_splits][hkv][tokens hq / hkv][2]
+  float* part_acc;  // [max_splits][hkv][tokens hq / hkv][d]
+};
+hipError_t launch_attn8(const Attn8Args& a, const Attn8Plan& p, hipStream_t st);
+
+// ---- verify.hip
+constexpr int kVerifyChunk = 4096;  // vocabulary entries of a partial
+constexpr int kVerifyMaxDrafts = 16;
+struct VerifyArgs {
+  int n, drafts, vocab, chunks;
+  int64_t ld, ld_draft;  // row strides; candidate i's rows are (drafts + 1) i .. and drafts i ..
+  double temp;
+  const float* logits;
+  const float* draft_logits;  // null: each draft is certain under its own distribution
+  const int32_t* draft_tokens;
+  const float* uniforms;      // [n][drafts + 1]
+  const int32_t* n_drafts;    // null: all have `drafts`
+  int32_t* out_tokens;
+  float* out_logprobs;
+  int32_t* out_accepted;
+  double* part_sum;   // [rows][chunks]: sums of exp, relative to the chunk's largest logit
+  float* part_max;    // [rows][chunks]
+  int32_t* part_arg;  // [rows][chunks]: the largest logit's index (temp 0)
+  double* rest_sum;   // [n][chunks]: of max(p - q, 0)
+};
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t st);
+
 // ---- moe_route.hip
 struct MoeRouteArgs {
   int n, n_experts, top_k, sigmoid, n_groups, top_groups, group_best, renormalise;

@@ -1661,6 +1661,248 @@ SEVO_API sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void
   return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_moe_linear_fp8");
 }
 
+// ------------------------------------------------------------------ 8-bit cache
+namespace {
+
+// arrays that are read word by word
+bool bad_words(const void* p) { return !p || (reinterpret_cast<uintptr_t>(p) & 3); }
+bool odd_words(const void* p) { return reinterpret_cast<uintptr_t>(p) & 3; }  // (may be null)
+
+sevo_status check_kv8_dim(int d) {
+  if (d != 64 && d != 128) return fail(SEVO_ERR_UNSUPPORTED, "head_dim %d not in {64, 128}", d);
+  return SEVO_OK;
+}
+
+sevo_status kv_pages(const sevo_kv_pages_args* a, int to8, const char* name, void* stream) {
+  if (!a) return fail(SEVO_ERR_INVALID_ARGUMENT, "null args");
+  if (a->n_kv_heads < 1 || a->count < 0 || a->src_num_pages < 0 || a->dst_num_pages < 0)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "n_kv_heads %d, count %lld, pages %lld and %lld",
+                a->n_kv_heads, (long long)a->count, (long long)a->src_num_pages,
+                (long long)a->dst_num_pages);
+  if (sevo_status s = check_kv8_dim(a->head_dim)) return s;
+  if (a->count > 0x7FFFFFFF / a->n_kv_heads)
+    return fail(SEVO_ERR_UNSUPPORTED, "count %lld of %d heads: fewer pages a call",
+                (long long)a->count, a->n_kv_heads);
+  if ((!a->src_pages && a->count > a->src_num_pages) ||
+      (!a->dst_pages && a->count > a->dst_num_pages))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "count %lld past the pool's pages", (long long)a->count);
+  if (a->count == 0) return SEVO_OK;
+  // an empty pool (no page of which any id can name) may be null
+  if ((a->src_num_pages && bad_ptr(a->src)) || (a->dst_num_pages && bad_ptr(a->dst)) ||
+      odd_words(a->src_pages) || odd_words(a->dst_pages))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  const size_t b16 = 64 * (size_t)a->head_dim, b8 = SEVO_KV8_TILE_BYTES((size_t)a->head_dim);
+  const int64_t most = ((int64_t)1 << 46) / a->n_kv_heads;  // pages of a pool that an address reaches
+  if (a->src_num_pages > most || a->dst_num_pages > most)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "pages past any memory");
+  if (overlap(a->src, (size_t)a->src_num_pages * a->n_kv_heads * (to8 ? b16 : b8), a->dst,
+              (size_t)a->dst_num_pages * a->n_kv_heads * (to8 ? b8 : b16)))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "source and destination pools overlap");
+  sevo::KvPagesArgs k;
+  k.hkv = a->n_kv_heads; k.d = a->head_dim; k.count = a->count;
+  k.src_num_pages = a->src_num_pages; k.dst_num_pages = a->dst_num_pages;
+  k.src = a->src; k.dst = a->dst; k.src_pages = a->src_pages; k.dst_pages = a->dst_pages;
+  hipError_t e = sevo::launch_pack_kv8(k, to8, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, name);
+}
+
+// shape rules of the 8-bit attention
+sevo_status check_attn8_shape(int n, int tokens, int hq, int hkv, int d, int max_pages) {
+  if (n < 0 || max_pages < 1)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "n %d, max_pages %d", n, max_pages);
+  if (sevo_status s = check_kv8_dim(d)) return s;
+  if (tokens < 1 || tokens > 16)
+    return fail(SEVO_ERR_UNSUPPORTED, "n_tokens %d outside [1, 16]", tokens);
+  if (hkv < 1 || hq < 1 || hq % hkv || hq / hkv > 16)
+    return fail(SEVO_ERR_UNSUPPORTED, "n_q_heads %d / n_kv_heads %d: a whole number up to 16", hq,
+                hkv);
+  const int64_t grid = (int64_t)1 << 31;
+  if (max_pages > 0x7FFFFFFF / SEVO_PAGE_SIZE || (int64_t)n * max_pages > (int64_t)1 << 40 ||
+      (int64_t)hq * tokens >= grid)
+    return fail(SEVO_ERR_UNSUPPORTED, "more keys or heads than a call takes");
+  if (n > 0) {
+    const sevo::Attn8Plan p = sevo::plan_attn8(n, hq, hkv, tokens, max_pages);
+    if ((int64_t)hq * tokens * n >= grid / 256 || p.max_splits * hkv * p.col_tiles >= grid / 256)
+      return fail(SEVO_ERR_UNSUPPORTED, "n %d of %d heads and %d tokens: fewer candidates a call", n,
+                  hq, tokens);
+  }
+  return SEVO_OK;
+}
+
+struct Attn8Layout {
+  size_t ml, acc, total;
+};
+Attn8Layout attn8_layout(int hq, int tokens, int d, int max_pages, const sevo::Attn8Plan& p) {
+  Attn8Layout L{0, 0, 0};
+  if (max_pages <= sevo::kAttn8MinChunk) return L;  // one split a candidate: no partials
+  const size_t rows = (size_t)p.max_splits * hq * tokens;
+  L.acc = round_up(rows * 2 * sizeof(float), 256);
+  L.total = L.acc + round_up(rows * d * sizeof(float), 256);
+  return L;
+}
+
+}  // namespace
+
+SEVO_API sevo_status sevo_qk_norm_rope_append_fp8(const sevo_model* m, int32_t layer,
+                                                  const float* qkv, int32_t n,
+                                                  const int32_t* positions, const int32_t* rows,
+                                                  const int32_t* page_table, int32_t n_rows,
+                                                  int32_t max_pages, int64_t num_pages,
+                                                  void* q_out, void* kv_pool, void* stream) {
+  if (!m) return fail(SEVO_ERR_INVALID_ARGUMENT, "null model");
+  if (layer < 0 || layer >= m->cfg.n_layers) return fail(SEVO_ERR_INVALID_ARGUMENT, "bad layer");
+  if (n < 0 || n_rows < 1 || max_pages < 1 || num_pages < 1 || (!rows && n_rows < n))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "n %d, n_rows %d, max_pages %d, num_pages %lld", n,
+                n_rows, max_pages, (long long)num_pages);
+  // (a launch holds fewer than 2^32 threads)
+  if (n > (1 << 24) - 1) return fail(SEVO_ERR_UNSUPPORTED, "n %d: fewer tokens a call", n);
+  if (n == 0) return SEVO_OK;
+  if (bad_ptr(qkv) || bad_ptr(q_out) || bad_ptr(kv_pool) || bad_words(positions) ||
+      bad_words(page_table) || odd_words(rows))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  sevo::RopeAppendArgs r;
+  fill_rope_args(m, layer, qkv, 1, n, positions, page_table, max_pages, num_pages, q_out, nullptr, r);
+  if (r.qk_norm && (bad_ptr(r.q_gain) || bad_ptr(r.k_gain)))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned norm gain");
+  r.row_of_token = rows;
+  hipError_t e = sevo::launch_append8(r, n_rows, static_cast<uint8_t*>(kv_pool),
+                                      static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_qk_norm_rope_append_fp8");
+}
+
+SEVO_API sevo_status sevo_pack_kv_fp8(const sevo_kv_pages_args* a, void* stream) {
+  return kv_pages(a, 1, "sevo_pack_kv_fp8", stream);
+}
+
+SEVO_API sevo_status sevo_unpack_kv_fp8(const sevo_kv_pages_args* a, void* stream) {
+  return kv_pages(a, 0, "sevo_unpack_kv_fp8", stream);
+}
+
+SEVO_API size_t sevo_attn_fp8_workspace_bytes(int32_t n, int32_t n_tokens, int32_t n_q_heads,
+                                              int32_t n_kv_heads, int32_t head_dim,
+                                              int32_t max_pages) {
+  if (n <= 0 || check_attn8_shape(n, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages)) return 0;
+  return attn8_layout(n_q_heads, n_tokens, head_dim, max_pages,
+                      sevo::plan_attn8(n, n_q_heads, n_kv_heads, n_tokens, max_pages)).total;
+}
+
+SEVO_API sevo_status sevo_attn_decode_fp8(const sevo_attn_fp8_args* a, void* stream) {
+  if (!a) return fail(SEVO_ERR_INVALID_ARGUMENT, "null args");
+  if (sevo_status s = check_attn8_shape(a->n, a->n_tokens, a->n_q_heads, a->n_kv_heads, a->head_dim,
+                                        a->max_pages))
+    return s;
+  if (a->page_size != SEVO_PAGE_SIZE)
+    return fail(SEVO_ERR_UNSUPPORTED, "page_size %d != 16", a->page_size);
+  if (a->num_pages < 1) return fail(SEVO_ERR_INVALID_ARGUMENT, "num_pages < 1");
+  if (!std::isfinite(a->scale) || a->scale <= 0.f)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "scale must be finite and > 0");
+  if (a->clear_rest != 0 && a->clear_rest != 1)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "clear_rest %d", a->clear_rest);
+  if (a->n == 0) return SEVO_OK;
+  if (bad_ptr(a->q) || bad_ptr(a->kv_pool) || bad_words(a->page_table) || bad_words(a->seq_lens) ||
+      bad_ptr(a->out) || odd_words(a->q_lens))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  const sevo::Attn8Plan p =
+      sevo::plan_attn8(a->n, a->n_q_heads, a->n_kv_heads, a->n_tokens, a->max_pages);
+  const Attn8Layout L = attn8_layout(a->n_q_heads, a->n_tokens, a->head_dim, a->max_pages, p);
+  if (a->workspace_bytes < L.total)
+    return fail(SEVO_ERR_WORKSPACE_TOO_SMALL, "attention needs %zu workspace bytes, got %zu",
+                L.total, a->workspace_bytes);
+  if (L.total && bad_ptr(a->workspace))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned workspace");
+  sevo::Attn8Args k;
+  k.n = a->n; k.tokens = a->n_tokens; k.hq = a->n_q_heads; k.hkv = a->n_kv_heads;
+  k.d = a->head_dim; k.max_pages = a->max_pages; k.clear_rest = a->clear_rest;
+  k.col_tiles = p.col_tiles; k.target = p.target; k.max_splits = (int)p.max_splits;
+  k.num_pages = a->num_pages;
+  k.q = static_cast<const sevo::bf16_t*>(a->q);
+  k.kv_pool = static_cast<const uint8_t*>(a->kv_pool);
+  k.page_table = a->page_table; k.seq_lens = a->seq_lens; k.q_lens = a->q_lens;
+  k.scale_log2 = a->scale * 1.4426950408889634f;
+  k.out = static_cast<sevo::bf16_t*>(a->out);
+  char* ws = static_cast<char*>(a->workspace);
+  k.part_ml = L.total ? reinterpret_cast<float*>(ws + L.ml) : nullptr;
+  k.part_acc = L.total ? reinterpret_cast<float*>(ws + L.acc) : nullptr;
+  hipError_t e = sevo::launch_attn8(k, p, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_attn_decode_fp8");
+}
+
+// ------------------------------------------------------------------ drafted tokens
+namespace {
+
+constexpr int kVerifyMaxVocab = 1 << 24;
+
+sevo_status check_verify_shape(int n, int drafts, int vocab) {
+  if (n < 0 || vocab < 1) return fail(SEVO_ERR_INVALID_ARGUMENT, "n %d, vocab %d", n, vocab);
+  if (drafts < 0 || drafts > sevo::kVerifyMaxDrafts || vocab > kVerifyMaxVocab)
+    return fail(SEVO_ERR_UNSUPPORTED, "n_drafts %d outside [0, %d] or vocab %d past 2^24", drafts,
+                sevo::kVerifyMaxDrafts, vocab);
+  const int64_t chunks = (vocab + sevo::kVerifyChunk - 1) / sevo::kVerifyChunk;
+  if ((int64_t)n * (2 * drafts + 1) * chunks >= (int64_t)1 << 23)
+    return fail(SEVO_ERR_UNSUPPORTED, "n %d of %d drafts: fewer candidates a call", n, drafts);
+  return SEVO_OK;
+}
+
+struct VerifyLayout {
+  size_t sum, rest, max, arg, total;
+};
+VerifyLayout verify_layout(int n, int drafts, int vocab) {
+  const size_t chunks = (vocab + sevo::kVerifyChunk - 1) / sevo::kVerifyChunk;
+  const size_t parts = (size_t)n * (2 * drafts + 1) * chunks;
+  VerifyLayout L;
+  L.sum = 0;
+  L.rest = round_up(parts * 8, 256);
+  L.max = L.rest + round_up(n * chunks * 8, 256);
+  L.arg = L.max + round_up(parts * 4, 256);
+  L.total = L.arg + round_up(parts * 4, 256);
+  return L;
+}
+
+}  // namespace
+
+SEVO_API size_t sevo_verify_workspace_bytes(int32_t n, int32_t n_drafts, int32_t vocab) {
+  if (n <= 0 || check_verify_shape(n, n_drafts, vocab)) return 0;
+  return verify_layout(n, n_drafts, vocab).total;
+}
+
+SEVO_API sevo_status sevo_verify_drafts(const sevo_verify_args* a, void* stream) {
+  if (!a) return fail(SEVO_ERR_INVALID_ARGUMENT, "null args");
+  if (sevo_status s = check_verify_shape(a->n, a->n_drafts, a->vocab)) return s;
+  if (!std::isfinite(a->temperature) || a->temperature < 0.0)
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "temperature must be finite and >= 0");
+  // below, logits / temperature leaves the range in which they can be told apart
+  if (a->temperature > 0.0 && a->temperature < 1e-30)
+    return fail(SEVO_ERR_UNSUPPORTED, "temperature %g: 0 or at least 1e-30", a->temperature);
+  const bool dist = a->draft_logits && a->n_drafts > 0;
+  if (a->ld < a->vocab || a->ld % 4 || (dist && (a->ld_draft < a->vocab || a->ld_draft % 4)))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "ld %lld, ld_draft %lld: multiples of 4, at least vocab",
+                (long long)a->ld, (long long)a->ld_draft);
+  if (a->n == 0) return SEVO_OK;
+  if (bad_ptr(a->logits) || bad_words(a->uniforms) || (a->n_drafts && bad_words(a->draft_tokens)) ||
+      (a->draft_logits && !aligned16(a->draft_logits)) || odd_words(a->counts) ||
+      bad_words(a->out_tokens) || bad_words(a->out_logprobs) || bad_words(a->out_accepted))
+    return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
+  const VerifyLayout L = verify_layout(a->n, a->n_drafts, a->vocab);
+  if (a->workspace_bytes < L.total)
+    return fail(SEVO_ERR_WORKSPACE_TOO_SMALL, "verification needs %zu workspace bytes, got %zu",
+                L.total, a->workspace_bytes);
+  if (bad_ptr(a->workspace)) return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned workspace");
+  sevo::VerifyArgs v;
+  v.n = a->n; v.drafts = a->n_drafts; v.vocab = a->vocab;
+  v.chunks = (a->vocab + sevo::kVerifyChunk - 1) / sevo::kVerifyChunk;
+  v.ld = a->ld; v.ld_draft = a->ld_draft; v.temp = a->temperature;
+  v.logits = a->logits; v.draft_logits = dist ? a->draft_logits : nullptr;
+  v.draft_tokens = a->draft_tokens; v.uniforms = a->uniforms; v.n_drafts = a->counts;
+  v.out_tokens = a->out_tokens; v.out_logprobs = a->out_logprobs; v.out_accepted = a->out_accepted;
+  char* ws = static_cast<char*>(a->workspace);
+  v.part_sum = reinterpret_cast<double*>(ws + L.sum);
+  v.rest_sum = reinterpret_cast<double*>(ws + L.rest);
+  v.part_max = reinterpret_cast<float*>(ws + L.max);
+  v.part_arg = reinterpret_cast<int32_t*>(ws + L.arg);
+  hipError_t e = sevo::launch_verify(v, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_verify_drafts");
+}
+
 // ------------------------------------------------------------------ utilities
 SEVO_API sevo_status sevo_fill_normal_bf16(void* dst, int64_t count, uint64_t key, int64_t offset,
                                            float mul, float add, int32_t use_add, void* stream) {

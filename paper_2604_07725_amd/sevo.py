@@ -136,6 +136,28 @@ class MoeLinearFp8Args(C.Structure):
                 ("clear_unlisted", i32)]
 
 
+class KvPagesArgs(C.Structure):
+    _fields_ = [("n_kv_heads", i32), ("head_dim", i32), ("count", i64), ("src_num_pages", i64),
+                ("dst_num_pages", i64), ("src", vp), ("dst", vp), ("src_pages", vp),
+                ("dst_pages", vp)]
+
+
+class AttnFp8Args(C.Structure):
+    _fields_ = [("n", i32), ("n_tokens", i32), ("n_q_heads", i32), ("n_kv_heads", i32),
+                ("head_dim", i32), ("page_size", i32), ("max_pages", i32), ("clear_rest", i32),
+                ("num_pages", i64), ("q", vp), ("kv_pool", vp), ("page_table", vp),
+                ("seq_lens", vp), ("q_lens", vp), ("scale", f32), ("out", vp), ("workspace", vp),
+                ("workspace_bytes", sz)]
+
+
+class VerifyArgs(C.Structure):
+    _fields_ = [("n", i32), ("n_drafts", i32), ("vocab", i32), ("ld", i64), ("ld_draft", i64),
+                ("temperature", C.c_double), ("logits", vp), ("draft_logits", vp),
+                ("draft_tokens", vp), ("uniforms", vp), ("counts", vp), ("out_tokens", vp),
+                ("out_logprobs", vp), ("out_accepted", vp), ("workspace", vp),
+                ("workspace_bytes", sz)]
+
+
 _SIGS = {
     "sevo_status_string": ([i32], C.c_char_p),
     "sevo_last_error": ([], C.c_char_p),
@@ -177,6 +199,13 @@ _SIGS = {
     "sevo_moe_lists": ([vp, i32, i32, i32, vp, sz, vp], i32),
     "sevo_moe_lists_bytes": ([i32, i32, i32], sz),
     "sevo_moe_linear_fp8": ([C.POINTER(MoeLinearFp8Args), vp], i32),
+    "sevo_qk_norm_rope_append_fp8": ([vp, i32, vp, i32, vp, vp, vp, i32, i32, i64, vp, vp, vp], i32),
+    "sevo_pack_kv_fp8": ([C.POINTER(KvPagesArgs), vp], i32),
+    "sevo_unpack_kv_fp8": ([C.POINTER(KvPagesArgs), vp], i32),
+    "sevo_attn_decode_fp8": ([C.POINTER(AttnFp8Args), vp], i32),
+    "sevo_attn_fp8_workspace_bytes": ([i32, i32, i32, i32, i32, i32], sz),
+    "sevo_verify_drafts": ([C.POINTER(VerifyArgs), vp], i32),
+    "sevo_verify_workspace_bytes": ([i32, i32, i32], sz),
     "sevo_profile_begin": ([i32, C.c_uint32], i32),
     "sevo_profile_end": ([C.POINTER(f32), C.POINTER(i32)], i32),
 }
@@ -967,6 +996,246 @@ def sevo_moe_linear_fp8(x, x_scales, w, w_scales, lists: MoeLists, weights=None,
                          lists.buffer.data_ptr(), out.data_ptr(), 1 if clear else 0)
     _call("sevo_moe_linear_fp8", i, C.byref(a))
     return out
+
+
+# ------------------------------------------------------------------ 8-bit cache
+def sevo_kv8_tile_bytes(head_dim) -> int:
+    """Bytes of one (page, kv head) of the 8-bit cache (SEVO_KV8_TILE_BYTES)."""
+    return 2 * PAGE_SIZE * head_dim + 8 * PAGE_SIZE
+
+
+def _kv8_dims(kv_pool, name="kv_pool"):
+    """(pages, kv heads, head_dim) of an 8-bit pool uint8 [pages, hkv, 32 d + 128]."""
+    _need(name, kv_pool, torch.uint8, None, kv_pool.get_device())
+    if kv_pool.dim() != 3 or kv_pool.shape[2] not in (sevo_kv8_tile_bytes(64), sevo_kv8_tile_bytes(128)):
+        raise ValueError(f"{name}: shape {tuple(kv_pool.shape)}, expected [pages, kv heads, 32 d + 128], "
+                         "d 64 or 128")
+    pages, hkv, tile = kv_pool.shape
+    return pages, hkv, (tile - 8 * PAGE_SIZE) // (2 * PAGE_SIZE)
+
+
+def sevo_qk_norm_rope_append_fp8(model, layer, qkv, positions, page_table, kv_pool, rows=None,
+                                 q_out=None, stream=None):
+    """sevo_qk_norm_rope_append into the 8-bit cache uint8 [pages, hkv, 32 d + 128]: qkv fp32
+    [n, (hq + 2 hkv) d], positions int32 [n]; ``rows`` int32 [n]: each token's row
+    of the page table (else row i), for several tokens a candidate.  A token with a position
+    of -1 is not appended.  Returns q bf16 [n, hq, d]."""
+    if stream is not None:
+        return _on_stream(stream, sevo_qk_norm_rope_append_fp8, model, layer, qkv, positions,
+                          page_table, kv_pool, rows, q_out)
+    cfg = model.config
+    hq, hkv, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    n, i = qkv.shape[0], qkv.get_device()
+    n_rows, max_pages = page_table.shape
+    pages = kv_pool.shape[0]
+    i32t = torch.int32
+    if not (qkv.dtype is torch.float32 and qkv.shape == (n, (hq + 2 * hkv) * d) and
+            qkv.is_contiguous() and positions.dtype is i32t and positions.shape == (n,) and
+            positions.is_contiguous() and page_table.dtype is i32t and
+            page_table.is_contiguous() and kv_pool.dtype is torch.uint8 and
+            kv_pool.shape == (pages, hkv, sevo_kv8_tile_bytes(d)) and kv_pool.is_contiguous() and
+            positions.get_device() == page_table.get_device() == kv_pool.get_device() == i):
+        _need("qkv", qkv, torch.float32, (n, (hq + 2 * hkv) * d), i)
+        _need("positions", positions, i32t, (n,), i)
+        _need("page_table", page_table, i32t, (n_rows, max_pages), i)
+        _need("kv_pool", kv_pool, torch.uint8, (pages, hkv, sevo_kv8_tile_bytes(d)), i)
+    if rows is not None:
+        _need("rows", rows, i32t, (n,), i)
+    if q_out is None:
+        q_out = torch.empty(n, hq, d, dtype=torch.bfloat16, device=qkv.device)
+    else:
+        _need("q_out", q_out, torch.bfloat16, (n, hq, d), i)
+    _call("sevo_qk_norm_rope_append_fp8", i, model.handle, int(layer), qkv.data_ptr(), n,
+          positions.data_ptr(), _ptr(rows), page_table.data_ptr(), n_rows, max_pages, pages,
+          q_out.data_ptr(), kv_pool.data_ptr())
+    return q_out
+
+
+def _kv_pages(name, src, dst, hkv, d, src_pages, dst_pages):
+    """The pages entry points: page ids, counts, the call."""
+    i = src.get_device()
+    lists = [(n, t) for n, t in (("src_pages", src_pages), ("dst_pages", dst_pages)) if t is not None]
+    count = lists[0][1].shape[0] if lists else src.shape[0]
+    for n, t in lists:
+        _need(n, t, torch.int32, (count,), i)
+    a = KvPagesArgs(hkv, d, count, src.shape[0], dst.shape[0], src.data_ptr(), dst.data_ptr(),
+                    _ptr(src_pages), _ptr(dst_pages))
+    _call(name, i, C.byref(a))
+    return dst
+
+
+def _made_pages(src, src_pages, dst_pages):
+    """Pages of the pool that a call without a destination makes: one per entry."""
+    if dst_pages is not None:
+        raise ValueError("dst_pages: needs the pool that they are of")
+    return src.shape[0] if src_pages is None else src_pages.shape[0]
+
+
+def sevo_pack_kv_fp8(kv_pool, kv_pool8=None, src_pages=None, dst_pages=None, stream=None):
+    """Pages of the bf16 pool [pages, hkv, 2, 16 d] to pages of the 8-bit pool ``kv_pool8``
+    uint8 [pages, hkv, 32 d + 128] (else a new one, a page per entry): entry j takes page
+    src_pages[j] to page dst_pages[j] (int32, default j)."""
+    if stream is not None:
+        return _on_stream(stream, sevo_pack_kv_fp8, kv_pool, kv_pool8, src_pages, dst_pages)
+    _need("kv_pool", kv_pool, torch.bfloat16, None, kv_pool.get_device())
+    if kv_pool.dim() != 4 or kv_pool.shape[2] != 2 or kv_pool.shape[3] % PAGE_SIZE:
+        raise ValueError(f"kv_pool: shape {tuple(kv_pool.shape)}, expected [pages, kv heads, 2, 16 d]")
+    hkv, d = kv_pool.shape[1], kv_pool.shape[3] // PAGE_SIZE
+    if kv_pool8 is None:
+        kv_pool8 = torch.empty(_made_pages(kv_pool, src_pages, dst_pages), hkv, sevo_kv8_tile_bytes(d),
+                               dtype=torch.uint8, device=kv_pool.device)
+    else:
+        _need("kv_pool8", kv_pool8, torch.uint8, (kv_pool8.shape[0], hkv, sevo_kv8_tile_bytes(d)),
+              kv_pool.get_device())
+    return _kv_pages("sevo_pack_kv_fp8", kv_pool, kv_pool8, hkv, d, src_pages, dst_pages)
+
+
+def sevo_unpack_kv_fp8(kv_pool8, kv_pool=None, src_pages=None, dst_pages=None, stream=None):
+    """Pages of the 8-bit pool uint8 [pages, hkv, 32 d + 128] to pages of the bf16 pool
+    ``kv_pool`` [pages, hkv, 2, 16 d] (else a new one, a page per entry), as in
+    ``sevo_pack_kv_fp8``."""
+    if stream is not None:
+        return _on_stream(stream, sevo_unpack_kv_fp8, kv_pool8, kv_pool, src_pages, dst_pages)
+    _, hkv, d = _kv8_dims(kv_pool8, "kv_pool8")
+    if kv_pool is None:
+        kv_pool = torch.empty(_made_pages(kv_pool8, src_pages, dst_pages), hkv, 2, PAGE_SIZE * d,
+                              dtype=torch.bfloat16, device=kv_pool8.device)
+    else:
+        _need("kv_pool", kv_pool, torch.bfloat16, (kv_pool.shape[0], hkv, 2, PAGE_SIZE * d),
+              kv_pool8.get_device())
+    return _kv_pages("sevo_unpack_kv_fp8", kv_pool8, kv_pool, hkv, d, src_pages, dst_pages)
+
+
+@functools.lru_cache(maxsize=1024)  # (a plan from the sizes alone)
+def sevo_attn_fp8_workspace_bytes(n, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages) -> int:
+    return int(lib().sevo_attn_fp8_workspace_bytes(n, n_tokens, n_q_heads, n_kv_heads, head_dim,
+                                                   max_pages))
+
+
+def sevo_attn_decode_fp8(q, kv_pool, page_table, seq_lens, q_lens=None, out=None, scale=None,
+                         workspace=None, stream=None):
+    """Paged GQA decode attention over the 8-bit cache uint8 [pages, hkv, 32 d + 128].
+    q bf16 [n, hq, d], or [n, T, hq, d] with T new tokens a candidate, the last q_lens[i]
+    (int32 [n], default T) of its seq_lens[i] keys, each of which sees the keys up to its own.
+    Rows past q_lens[i] are 0, or with ``out`` as they were.  ``workspace``: a caller's
+    uint8 buffer of sevo_attn_fp8_workspace_bytes (else one is allocated)."""
+    if stream is not None:
+        return _on_stream(stream, sevo_attn_decode_fp8, q, kv_pool, page_table, seq_lens, q_lens,
+                          out, scale, workspace)
+    if q.dim() == 3:
+        (n, hq, d), T = q.shape, 1
+    elif q.dim() == 4:
+        n, T, hq, d = q.shape
+    else:
+        raise ValueError(f"q: shape {tuple(q.shape)}, expected [n, hq, d] or [n, T, hq, d]")
+    i = q.get_device()
+    max_pages = page_table.shape[1]
+    pages, hkv = kv_pool.shape[0], kv_pool.shape[1]
+    i32t = torch.int32
+    if not (q.dtype is torch.bfloat16 and q.is_contiguous() and kv_pool.dtype is torch.uint8 and
+            kv_pool.shape == (pages, hkv, sevo_kv8_tile_bytes(d)) and kv_pool.is_contiguous() and
+            page_table.dtype is i32t and page_table.shape == (n, max_pages) and
+            page_table.is_contiguous() and seq_lens.dtype is i32t and seq_lens.shape == (n,) and
+            seq_lens.is_contiguous() and
+            kv_pool.get_device() == page_table.get_device() == seq_lens.get_device() == i):
+        _need("q", q, torch.bfloat16, None, i)
+        _need("kv_pool", kv_pool, torch.uint8, (pages, hkv, sevo_kv8_tile_bytes(d)), i)
+        _need("page_table", page_table, i32t, (n, max_pages), i)
+        _need("seq_lens", seq_lens, i32t, (n,), i)
+    if q_lens is not None:
+        _need("q_lens", q_lens, i32t, (n,), i)
+    clear = out is None
+    if clear:
+        out = torch.empty_like(q)
+    else:
+        _need("out", out, torch.bfloat16, q.shape, i)
+    if workspace is not None:
+        _need("workspace", workspace, torch.uint8, None, i)
+        need = workspace.numel()
+    else:
+        need = sevo_attn_fp8_workspace_bytes(n, T, hq, hkv, d, max_pages)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    a = AttnFp8Args(n, T, hq, hkv, d, PAGE_SIZE, max_pages, 1 if clear else 0, pages, q.data_ptr(),
+                    kv_pool.data_ptr(), page_table.data_ptr(), seq_lens.data_ptr(), _ptr(q_lens),
+                    float(d ** -0.5 if scale is None else scale), out.data_ptr(), _ptr(workspace),
+                    need)
+    _call("sevo_attn_decode_fp8", i, C.byref(a))
+    return out
+
+
+# ------------------------------------------------------------------ drafted tokens
+@functools.lru_cache(maxsize=1024)
+def sevo_verify_workspace_bytes(n, n_drafts, vocab) -> int:
+    return int(lib().sevo_verify_workspace_bytes(n, n_drafts, vocab))
+
+
+def _ld3(name, t, vocab):
+    """Row stride of logits [n, rows, >= vocab] whose rows are equally spaced."""
+    n, r, v = t.shape
+    if n * r <= 1:
+        return -(-vocab // 4) * 4  # (one row has none)
+    ld = t.stride(1) if r > 1 else t.stride(0)
+    if n > 1 and t.stride(0) != r * ld:
+        raise ValueError(f"{name}: strides {tuple(t.stride())}, expected equally spaced rows")
+    return ld
+
+
+def sevo_verify_drafts(logits, draft_tokens, uniforms, temperature=1.0, draft_logits=None,
+                       n_drafts=None, vocab=None, out_tokens=None, out_logprobs=None,
+                       out_accepted=None, workspace=None, stream=None):
+    """Verification of drafted tokens: target logits fp32 [n, T + 1, ld] (the first ``vocab``
+    columns, default all; rows equally spaced), draft_tokens int32 [n, T], uniforms fp32
+    [n, T + 1] in [0, 1), draft_logits fp32 [n, T, ld] of the model that drafted (None: every draft is
+    certain), n_drafts int32 [n]: each candidate's number of drafts (default T).
+    Returns (tokens int32 [n, T + 1]: the accepted drafts, the token drawn behind them,
+    then -1; logprobs fp32 [n, T + 1]; accepted int32 [n])."""
+    if stream is not None:
+        return _on_stream(stream, sevo_verify_drafts, logits, draft_tokens, uniforms, temperature,
+                          draft_logits, n_drafts, vocab, out_tokens, out_logprobs, out_accepted,
+                          workspace)
+    if logits.dim() != 3 or logits.shape[1] < 1:
+        raise ValueError(f"logits: shape {tuple(logits.shape)}, expected [n, T + 1, ld]")
+    n, rows, width = logits.shape
+    T = rows - 1
+    dev, i = logits.device, logits.get_device()
+    vocab = width if vocab is None else int(vocab)
+    if vocab > width:
+        raise ValueError(f"vocab: {vocab}, logits of {width} columns")
+    f32t, i32t = torch.float32, torch.int32
+    _need("logits", logits, f32t, None, i, contiguous=False)
+    _need("draft_tokens", draft_tokens, i32t, (n, T), i)
+    _need("uniforms", uniforms, f32t, (n, rows), i)
+    ld, ldd = _ld3("logits", logits, vocab), 0
+    if draft_logits is not None:
+        _need("draft_logits", draft_logits, f32t, None, i, contiguous=False)
+        if draft_logits.dim() != 3 or draft_logits.shape[:2] != (n, T) or draft_logits.shape[2] < vocab:
+            raise ValueError(f"draft_logits: shape {tuple(draft_logits.shape)}, expected [{n}, {T}, ld]")
+        ldd = _ld3("draft_logits", draft_logits, vocab)
+    if n_drafts is not None:
+        _need("n_drafts", n_drafts, i32t, (n,), i)
+    if out_tokens is None:
+        out_tokens = torch.empty(n, rows, dtype=i32t, device=dev)
+    else:
+        _need("out_tokens", out_tokens, i32t, (n, rows), i)
+    if out_logprobs is None:
+        out_logprobs = torch.empty(n, rows, dtype=f32t, device=dev)
+    else:
+        _need("out_logprobs", out_logprobs, f32t, (n, rows), i)
+    if out_accepted is None:
+        out_accepted = torch.empty(n, dtype=i32t, device=dev)
+    else:
+        _need("out_accepted", out_accepted, i32t, (n,), i)
+    if workspace is None:
+        workspace = torch.empty(sevo_verify_workspace_bytes(n, T, vocab), dtype=torch.uint8, device=dev)
+    else:
+        _need("workspace", workspace, torch.uint8, None, i)
+    a = VerifyArgs(n, T, vocab, ld, ldd, float(temperature), logits.data_ptr(), _ptr(draft_logits),
+                   draft_tokens.data_ptr(), uniforms.data_ptr(), _ptr(n_drafts),
+                   out_tokens.data_ptr(), out_logprobs.data_ptr(), out_accepted.data_ptr(),
+                   workspace.data_ptr(), workspace.numel())
+    _call("sevo_verify_drafts", i, C.byref(a))
+    return out_tokens, out_logprobs, out_accepted
 
 
 # ------------------------------------------------------------------ read probe
