@@ -20,6 +20,8 @@
 //        (to 2^-17 of itself): the probabilities keep their 32-bit accuracy.
 // More than 16 query rows per kv head are further column tiles of the same page (NC), so
 // the cache is read once for all new tokens.
+#include <algorithm>
+
 #include "kernels.h"
 #include "kv8.h"
 
@@ -39,99 +41,107 @@ __device__ __forceinline__ bf16x8v codes_bf16(uint32_t a, uint32_t b) {
             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true))});
 }
 
-__device__ __forceinline__ int pages_of(const int32_t* lens, int i, int max_pages) {
-  int len = lens[i];
-  len = len < 0 ? 0 : (len > max_pages * kPage ? max_pages * kPage : len);
-  return (len + kPage - 1) / kPage;
+__device__ __forceinline__ int keys_of(const int32_t* lens, int i, int max_pages) {
+  const int len = lens[i];
+  return len < 0 ? 0 : (len > max_pages * kPage ? max_pages * kPage : len);
 }
+__device__ __forceinline__ int pages_of(int keys) { return (keys + kPage - 1) / kPage; }
 
-// The split plan, the same in every workgroup of both kernels: splits of at most `chunk`
-// pages, chunk = max(kMinChunk, all pages / target); candidate i has max(1, ceil(pages_i /
-// chunk)) of them.  Calls of a 256-thread workgroup.
+// The split plan, the same in every wave of both kernels: candidate i has max(1, ceil(pages_i /
+// chunk)) splits.  The chunk is the least that gives all workgroups a place at once (then
+// nothing waits for a second round that would be part empty); where that leaves chunks of
+// more than kAttn8LongChunk pages, whose ends would be ragged, several rounds of shorter ones.
 struct Split {
   int cand, index, count, first;  // candidate, split of it, its number of splits, its first flat id
-};
-struct PlanLds {
-  long long sum[4];
-  int scan[4], cand, index, count, first;
+  int len;                        // its keys
 };
 
-__device__ __forceinline__ int wave_scan(int v) {  // inclusive
+// sum over the wave, every lane gets it; inclusive scan (row shifts, then the rows' last lanes
+// carried on): in registers, a shuffle through LDS costs 100 clocks a step
+__device__ __forceinline__ int wave_sum_i(int v) {
+  v += lane_xor<1>(v);
+  v += lane_xor<2>(v);
+  v += lane_xor<4>(v);
+  v += lane_xor<8>(v);
+  v += lane_xor<16>(v);
+  return v + lane_xor<32>(v);
+}
+__device__ __forceinline__ int wave_scan_i(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast 15 into rows 1, 3
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast 31 into rows 2, 3
+}
+
+// flat >= 0: the split with that flat id (cand -1 behind the last); flat < 0: all of candidate ~flat.
+// Each wave by itself, a candidate per lane: no barrier, and one read of the lengths where there
+// are at most 64.
+__device__ __forceinline__ Split find_split(const Attn8Args& a, int flat) {
   const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(v, d);
-    if (lane >= d) v += o;
+  int keys = lane < a.n ? keys_of(a.seq_lens, lane, a.max_pages) : 0;
+  int all = pages_of(keys);
+  for (int i = lane + 64; i < a.n; i += 64) all += pages_of(keys_of(a.seq_lens, i, a.max_pages));
+  all = __builtin_amdgcn_readfirstlane(wave_sum_i(all));  // (below 2^31: n max_pages is)
+  int chunk = (all + a.one_round - 1) / a.one_round;
+  if (chunk > kAttn8LongChunk) chunk = max(kAttn8LongChunk / 2, (all + a.rounds - 1) / a.rounds);
+  chunk = max(chunk, a.min_chunk);
+  int base = 0;
+  Split r{-1, 0, 0, 0, 0};
+  for (int i0 = 0; i0 < a.n; i0 += 64) {
+    const int i = i0 + lane;
+    if (i0) keys = i < a.n ? keys_of(a.seq_lens, i, a.max_pages) : 0;
+    const int s = i < a.n ? max(1, (pages_of(keys) + chunk - 1) / chunk) : 0;
+    const int in = wave_scan_i(s);
+    const int first = base + in - s;
+    const bool hit = flat >= 0 ? s > 0 && flat >= first && flat < first + s : i == ~flat;
+    const uint64_t who = __builtin_amdgcn_ballot_w64(hit);
+    if (who) {
+      // scalars, so that what follows from them is scalar too
+      const int l = __builtin_ctzll(who);
+      r.cand = i0 + l;
+      r.first = __builtin_amdgcn_readlane(first, l);
+      r.count = __builtin_amdgcn_readlane(s, l);
+      r.len = __builtin_amdgcn_readlane(keys, l);
+      r.index = flat - r.first;
+      break;
+    }
+    base += __builtin_amdgcn_readlane(in, 63);
   }
-  return v;
+  return r;
 }
 
-// flat >= 0: the split with that flat id (cand -1 behind the last); flat < 0: all of candidate ~flat
-__device__ __forceinline__ Split find_split(const int32_t* lens, int n, int max_pages, int target,
-                                            int flat, PlanLds& L) {
-  const int t = threadIdx.x, w = t >> 6;
-  long long own = 0;
-  for (int i = t; i < n; i += 256) own += pages_of(lens, i, max_pages);
-#pragma unroll
-  for (int d = 32; d; d >>= 1) own += __shfl_xor(own, d);
-  if ((t & 63) == 0) L.sum[w] = own;
-  if (t == 0) L.cand = -1;
-  __syncthreads();
-  const long long all = L.sum[0] + L.sum[1] + L.sum[2] + L.sum[3];
-  long long chunk = (all + target - 1) / target;
-  if (chunk < kAttn8MinChunk) chunk = kAttn8MinChunk;
-  int base = 0;
-  for (int i0 = 0; i0 < n; i0 += 256) {
-    const int i = i0 + t;
-    int s = 0;
-    if (i < n) {
-      const int pg = pages_of(lens, i, max_pages);
-      s = pg ? (int)((pg + chunk - 1) / chunk) : 1;
-    }
-    const int in = wave_scan(s);
-    if ((t & 63) == 63) L.scan[w] = in;
-    __syncthreads();
-    int before = base;
-    for (int x = 0; x < w; ++x) before += L.scan[x];
-    const int first = before + in - s;
-    if (flat >= 0 ? (s > 0 && flat >= first && flat < first + s) : i == ~flat) {
-      L.cand = i;
-      L.index = flat - first;
-      L.count = s;
-      L.first = first;
-    }
-    base += L.scan[0] + L.scan[1] + L.scan[2] + L.scan[3];
-    __syncthreads();
-  }
-  // the same in every lane: scalars, so that what follows from them is scalar too
-  return Split{__builtin_amdgcn_readfirstlane(L.cand), __builtin_amdgcn_readfirstlane(L.index),
-               __builtin_amdgcn_readfirstlane(L.count), __builtin_amdgcn_readfirstlane(L.first)};
+// column cc (below 2^11) of a kv head's query rows: token cc / G, head cc % G of its group
+__device__ __forceinline__ int token_of(const Attn8Args& a, int cc) {
+  return (int)(((float)cc + 0.5f) * a.inv_group);
 }
+// running maxima start here: finite, so that what a column has not seen needs no case of its own
+constexpr float kNoScore = -3e38f;
+
+// waves per SIMD that the registers of NC column tiles leave room for
+constexpr int waves8(int d, int nc) { return nc == 1 || (nc == 2 && d == 64) ? 3 : 2; }
 
 }  // namespace
 
-template <int D, int NC>
-__global__ __launch_bounds__(256, NC == 1 ? 2 : 1) void attn8_split_kernel(Attn8Args a) {
+template <int D, int NC, int PF>
+__global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Args a) {
   constexpr int NA = D / 64;   // 64-dim blocks of a tile
   constexpr int NB = D / 16;   // 16-dim blocks of the output
   constexpr int kStride = D + 4;
-  __shared__ PlanLds plan;
   __shared__ float w_m[4][16], w_l[4][16];
   __shared__ __align__(16) float w_acc[4][16][kStride];
 
   // workgroups in the order (split, kv head, NC column tiles): the heads of a page, adjacent in
   // the pool, are read together, each through the XCD that its workgroup number falls to
-  const int per = a.hkv * a.col_tiles;
-  const int flat = blockIdx.x / per, rest = blockIdx.x - flat * per;
-  const int c = rest / a.col_tiles, cg = rest - c * a.col_tiles;
-  const Split sp = find_split(a.seq_lens, a.n, a.max_pages, a.target, flat, plan);
+  const int flat = blockIdx.y;
+  const int c = a.col_tiles == 1 ? blockIdx.x : blockIdx.x / a.col_tiles;
+  const int cg = blockIdx.x - c * a.col_tiles;
+  const Split sp = find_split(a, flat);
   const int i = sp.cand;
   if (i < 0) return;
-  int len = a.seq_lens[i];
-  len = len < 0 ? 0 : (len > a.max_pages * kPage ? a.max_pages * kPage : len);
-  const int npg = (len + kPage - 1) / kPage;
-  int m = a.q_lens ? a.q_lens[i] : a.tokens;
-  m = m < 0 ? 0 : (m > a.tokens ? a.tokens : m);
+  const int len = sp.len;
+  const int npg = pages_of(len);
   // the candidate's pages in even shares, each an even number of pages
   const int share = ((npg + sp.count - 1) / sp.count + 1) & ~1;
   const int pbeg = sp.index * share;
@@ -140,38 +150,7 @@ __global__ __launch_bounds__(256, NC == 1 ? 2 : 1) void attn8_split_kernel(Attn8
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, grp = lane >> 4;
-  const int G = a.hq / a.hkv, cols = a.tokens * G;
-
-  bf16x8v qf[NC][NA][2];
-  int lim[NC];  // keys that the lane's column sees
-#pragma unroll
-  for (int t = 0; t < NC; ++t) {
-    const int cc = (cg * NC + t) * 16 + col;
-    const int tok = cc / G, head = cc - tok * G;
-    const bool on = cc < cols && tok < m;
-    lim[t] = on ? len - m + tok + 1 : 0;
-    const bf16_t* qr = a.q + (((size_t)i * a.tokens + tok) * a.hq + (size_t)c * G + head) * D;
-#pragma unroll
-    for (int x = 0; x < NA; ++x)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u32x4 w{0u, 0u, 0u, 0u};
-        if (on) w = *reinterpret_cast<const u32x4*>(qr + 64 * x + 16 * grp + 8 * h);
-        qf[t][x][h] = __builtin_bit_cast(bf16x8v, w);
-      }
-  }
-  // pages that every query row of the candidate sees in full need no mask (columns
-  // without a row compute what is not stored)
-  const int full = (len - m + 1) / kPage;
-  float m_run[NC], l_run[NC];
-  f32x4 acc[NC][NB];
-#pragma unroll
-  for (int t = 0; t < NC; ++t) {
-    m_run[t] = -INFINITY;
-    l_run[t] = 0.f;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) acc[t][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  const int G = a.group, cols = a.tokens * G;
 
   const int32_t* ptr = a.page_table + (size_t)i * a.max_pages;
   const int pairs = (pend - pbeg + 1) / 2;                 // pairs of the split
@@ -190,67 +169,151 @@ __global__ __launch_bounds__(256, NC == 1 ? 2 : 1) void attn8_split_kernel(Attn8
       }
     }
   };
-  struct Page {
-    u32x4 k[NA], v[NA], ks, vs;
-  };
-  constexpr uint32_t kTile = kv8_tile_bytes(D);
-  const uint32_t koff = col * 64 + grp * 16, voff = lane * 16;
-  auto load = [&](Page& r, int id) {
-    const uint8_t* base = a.kv_pool + (id < 0 ? 0 : ((size_t)id * a.hkv + c) * kTile);
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(base), 0, id < 0 ? 0 : (int)kTile, 0x00020000);
-#pragma unroll
-    for (int x = 0; x < NA; ++x)
-      r.k[x] = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)koff, x * 1024, 2);
-#pragma unroll
-    for (int x = 0; x < NA; ++x)
-      r.v[x] = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)voff, 16 * D + x * 1024, 2);
-    r.ks = __builtin_amdgcn_raw_buffer_load_b128(rs, grp * 16, 32 * D, 2);
-    r.vs = __builtin_amdgcn_raw_buffer_load_b128(rs, grp * 16, 32 * D + 64, 2);
-  };
+  fetch_ids(0);
+  int m = a.q_lens ? a.q_lens[i] : a.tokens;
+  m = m < 0 ? 0 : (m > a.tokens ? a.tokens : m);
 
-  // one pair of pages, the first at logical page pg; ok0, ok1: in the pool
-  auto consume = [&](Page& A, Page& B, int pg, bool ok0, bool ok1) {
-    const bool masked = pg + 2 > full || !ok0 || !ok1;
-    const int u0 = pg * kPage + 4 * grp;  // the lane's tokens u0 .. + 3 and u0 + 16 .. + 3
-    if (masked) {
-      // what lies behind the last key may hold anything, also NaN codes
-      const int n0 = len - u0, n1 = len - u0 - kPage;
-      const uint32_t k0 = n0 >= 4 ? ~0u : (n0 <= 0 ? 0u : (1u << (8 * n0)) - 1u);
-      const uint32_t k1 = n1 >= 4 ? ~0u : (n1 <= 0 ? 0u : (1u << (8 * n1)) - 1u);
+  // The query rows' fragments, dims 64 x + 16 grp + 8 h .. + 7 of the lane's column: in registers,
+  // or from three column tiles on, where those are short, in LDS, once for the four waves.
+  constexpr bool kQLds = NC >= 3;
+  __shared__ __align__(16) u32x4 q_lds[kQLds ? NC * NA * 2 : 1][64];
+  bf16x8v qf[kQLds ? 1 : NC][NA][2];
+  int lim[NC];  // keys that the lane's column sees
 #pragma unroll
-      for (int x = 0; x < NA; ++x) {
-        A.v[x] &= k0;
-        B.v[x] &= k1;
-      }
-    }
-    const f32x4 ks0 = __builtin_bit_cast(f32x4, A.ks) * a.scale_log2;
-    const f32x4 ks1 = __builtin_bit_cast(f32x4, B.ks) * a.scale_log2;
-    const f32x4 vs0 = __builtin_bit_cast(f32x4, A.vs), vs1 = __builtin_bit_cast(f32x4, B.vs);
-    f32x4 s0[NC], s1[NC];
-#pragma unroll
-    for (int t = 0; t < NC; ++t) s0[t] = s1[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < NC; ++t) {
+    const int cc = (cg * NC + t) * 16 + col;
+    const int tok = token_of(a, cc), head = cc - tok * G;
+    const bool on = cc < cols && tok < m;
+    lim[t] = on ? len - m + tok + 1 : 0;
+    if (kQLds && (t & 3) != wave) continue;
+    const bf16_t* qr = a.q + (((size_t)i * a.tokens + tok) * a.hq + (size_t)c * G + head) * D;
 #pragma unroll
     for (int x = 0; x < NA; ++x)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const bf16x8v wa = codes_bf16(A.k[x][2 * h], A.k[x][2 * h + 1]);
-        const bf16x8v wb = codes_bf16(B.k[x][2 * h], B.k[x][2 * h + 1]);
+        u32x4 w{0u, 0u, 0u, 0u};
+        if (on) w = *reinterpret_cast<const u32x4*>(qr + 64 * x + 16 * grp + 8 * h);
+        if constexpr (kQLds) q_lds[(t * NA + x) * 2 + h][lane] = w;
+        else qf[t][x][h] = __builtin_bit_cast(bf16x8v, w);
+      }
+  }
+  if constexpr (kQLds) __syncthreads();
+  auto q_frag = [&](int t, int x, int h, int at) {
+    if constexpr (kQLds) return __builtin_bit_cast(bf16x8v, q_lds[(t * NA + x) * 2 + h][at]);
+    else return qf[t][x][h];
+  };
+  // pages that every query row of the candidate sees in full need no mask (columns
+  // without a row compute what is not stored)
+  const int full = (len - m + 1) / kPage;
+  float m_run[NC], l_run[NC];
+  f32x4 acc[NC][NB];
+#pragma unroll
+  for (int t = 0; t < NC; ++t) {
+    m_run[t] = kNoScore;
+    l_run[t] = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[t][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // PF pairs of pages in registers.  K of a later pair is read as soon as this pair's scores are
+  // formed, the scales after its probabilities, V after its output, into the registers that just
+  // became free: each load has PF iterations to arrive.
+  constexpr uint32_t kTile = kv8_tile_bytes(D);
+  const uint32_t koff = col * 64 + grp * 16, voff = lane * 16;
+  struct Pair {
+    u32x4 k[2][NA], v[2][NA], sk[2], sv[2];
+    int id[2];
+  };
+  Pair set[PF];
+  auto tile_of = [&](int id) {
+    const uint8_t* base = a.kv_pool + (id < 0 ? 0 : ((size_t)id * a.hkv + c) * kTile);
+    // no records, no read
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, id < 0 ? 0 : (int)kTile,
+                                             0x00020000);
+  };
+  auto load_k = [&](Pair& r, int n) {  // the wave's n-th pair (past the last the ids are -1: nothing is read)
+    if ((n & 63) == 0 && n) fetch_ids(n);
+    r.id[0] = __builtin_amdgcn_readlane(id0, n & 63);
+    r.id[1] = __builtin_amdgcn_readlane(id1, n & 63);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const __amdgpu_buffer_rsrc_t rs = tile_of(r.id[p]);
+#pragma unroll
+      for (int x = 0; x < NA; ++x)
+        r.k[p][x] = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)koff, x * 1024, 2);
+    }
+  };
+  auto load_s = [&](Pair& r) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const __amdgpu_buffer_rsrc_t rs = tile_of(r.id[p]);
+      r.sk[p] = __builtin_amdgcn_raw_buffer_load_b128(rs, grp * 16, 32 * D, 2);
+      r.sv[p] = __builtin_amdgcn_raw_buffer_load_b128(rs, grp * 16, 32 * D + 64, 2);
+    }
+  };
+  auto load_v = [&](Pair& r) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const __amdgpu_buffer_rsrc_t rs = tile_of(r.id[p]);
+#pragma unroll
+      for (int x = 0; x < NA; ++x)
+        r.v[p][x] = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)voff, 16 * D + x * 1024, 2);
+    }
+  };
+  auto step = [&](Pair& r, int n) {
+    const int pg = pbeg + 2 * (wave + 4 * n);  // the pair's first page
+    const bool ok0 = r.id[0] >= 0, ok1 = r.id[1] >= 0;
+    const bool masked = pg + 2 > full || !ok0 || !ok1;
+    const int u0 = pg * kPage + 4 * grp;  // the lane's tokens u0 .. + 3 and u0 + 16 .. + 3
+    int q_at = lane;  // opaque, or the reads of q would be moved out of the loop, into registers
+    if constexpr (kQLds) asm volatile("" : "+v"(q_at));
+    f32x4 s[NC][2];
+#pragma unroll
+    for (int t = 0; t < NC; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < NA; ++x)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8v wa = codes_bf16(r.k[0][x][2 * h], r.k[0][x][2 * h + 1]);
+        const bf16x8v wb = codes_bf16(r.k[1][x][2 * h], r.k[1][x][2 * h + 1]);
 #pragma unroll
         for (int t = 0; t < NC; ++t) {
-          s0[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, qf[t][x][h], s0[t], 0, 0, 0);
-          s1[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, qf[t][x][h], s1[t], 0, 0, 0);
+          const bf16x8v q = q_frag(t, x, h, q_at);
+          s[t][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, q, s[t][0], 0, 0, 0);
+          s[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, q, s[t][1], 0, 0, 0);
         }
       }
+    f32x4 ks[2], vs[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      ks[p] = __builtin_bit_cast(f32x4, r.sk[p]) * a.scale_log2;
+      vs[p] = __builtin_bit_cast(f32x4, r.sv[p]);
+    }
+    if (masked) {
+      // What lies behind the last key may hold anything, also NaN codes: no codes are kept of it.
+      // A scale that is no number goes into the scores of those who see the token instead: as a
+      // factor it would reach the others too (0 NaN).
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int left = len - u0 - kPage * p;
+        const uint32_t keep = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
+#pragma unroll
+        for (int x = 0; x < NA; ++x) r.v[p][x] &= keep;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float nan = vs[p][e] * 0.f;
+          ks[p][e] += nan;
+          vs[p][e] = nan == 0.f ? vs[p][e] : 0.f;
+        }
+      }
+    }
+    load_k(r, n + PF);
     bf16x8v ph[NC], pl[NC];
 #pragma unroll
     for (int t = 0; t < NC; ++t) {
       float z[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        z[e] = s0[t][e] * ks0[e];
-        z[4 + e] = s1[t][e] * ks1[e];
-      }
+      for (int e = 0; e < 8; ++e) z[e] = s[t][e / 4][e & 3] * ks[e / 4][e & 3];
       if (masked) {
         const int v0 = ok0 ? lim[t] - u0 : 0, v1 = ok1 ? lim[t] - u0 - kPage : 0;
 #pragma unroll
@@ -265,72 +328,61 @@ __global__ __launch_bounds__(256, NC == 1 ? 2 : 1) void attn8_split_kernel(Attn8
       const bool raise = top > m_run[t] + kLazyLog2;
       if (__builtin_amdgcn_ballot_w64(raise)) {
         const float mn = raise ? top : m_run[t];
-        const float alpha = raise ? __builtin_amdgcn_exp2f(m_run[t] - mn) : 1.f;  // 0 on the first page
+        const float alpha = __builtin_amdgcn_exp2f(m_run[t] - mn);  // 0 on the first page, 1 without a raise
         l_run[t] *= alpha;
 #pragma unroll
         for (int b = 0; b < NB; ++b) acc[t][b] *= alpha;
         m_run[t] = mn;
       }
-      const float mz = m_run[t] == -INFINITY ? 0.f : m_run[t];
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         float p[2];
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          const float pr = __builtin_amdgcn_exp2f(z[e + y] - mz);
+          const float pr = __builtin_amdgcn_exp2f(z[e + y] - m_run[t]);
           l_run[t] += pr;
-          const float vs = e < 4 ? vs0[(e + y) & 3] : vs1[(e + y) & 3];
-          // a masked token's scale may be anything: it does not enter
-          p[y] = masked && z[e + y] == -INFINITY ? 0.f : pr * vs;
+          p[y] = pr * vs[e / 4][(e + y) & 3];
         }
-        const __bf16 h0 = (__bf16)p[0], h1 = (__bf16)p[1];
-        hi[e / 2] = __builtin_bit_cast(uint32_t, bf16x2v{h0, h1});
-        lo[e / 2] = pack_bf16x2(p[0] - (float)h0, p[1] - (float)h1);
+        hi[e / 2] = pack_bf16x2(p[0], p[1]);
+        lo[e / 2] = pack_bf16x2(p[0] - bf16_lo(hi[e / 2]), p[1] - bf16_hi(hi[e / 2]));
       }
       ph[t] = __builtin_bit_cast(bf16x8v, u32x4{hi[0], hi[1], hi[2], hi[3]});
       pl[t] = __builtin_bit_cast(bf16x8v, u32x4{lo[0], lo[1], lo[2], lo[3]});
     }
+    load_s(r);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const bf16x8v w = codes_bf16(A.v[b / 4][b % 4], B.v[b / 4][b % 4]);
+      const bf16x8v w = codes_bf16(r.v[0][b / 4][b % 4], r.v[1][b / 4][b % 4]);
 #pragma unroll
       for (int t = 0; t < NC; ++t) {
         acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, pl[t], acc[t][b], 0, 0, 0);
         acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, ph[t], acc[t][b], 0, 0, 0);
       }
     }
+    load_v(r);
   };
-
   if (mine > 0) {
-    fetch_ids(0);
-    Page A0, B0, A1, B1;
-    auto ida = [&](int k) { return __builtin_amdgcn_readlane(id0, k & 63); };
-    auto idb = [&](int k) { return __builtin_amdgcn_readlane(id1, k & 63); };
-    int a0 = ida(0), b0 = idb(0), a1 = -1, b1 = -1;
-    load(A0, a0);
-    load(B0, b0);
-    for (int k = 0;;) {
-      // the next pair's loads are in flight while this one is consumed (past the
-      // wave's last pair the ids are -1: nothing is read)
-      if (((k + 1) & 63) == 0) fetch_ids(k + 1);
-      a1 = ida(k + 1);
-      b1 = idb(k + 1);
-      load(A1, a1);
-      load(B1, b1);
-      consume(A0, B0, pbeg + 2 * (wave + 4 * k), a0 >= 0, b0 >= 0);
-      if (++k >= mine) break;
-      if (((k + 1) & 63) == 0) fetch_ids(k + 1);
-      a0 = ida(k + 1);
-      b0 = idb(k + 1);
-      load(A0, a0);
-      load(B0, b0);
-      consume(A1, B1, pbeg + 2 * (wave + 4 * k), a1 >= 0, b1 >= 0);
-      if (++k >= mine) break;
+#pragma unroll
+    for (int y = 0; y < PF; ++y) {
+      load_k(set[y], y);
+      load_s(set[y]);
+      load_v(set[y]);
+    }
+    for (int n = 0;;) {
+      step(set[0], n);
+      if (++n >= mine) break;
+      if constexpr (PF > 1) {
+        step(set[PF - 1], n);
+        if (++n >= mine) break;
+      }
     }
   }
 
-  // the four waves of each column tile, in order; a candidate's only split is the result
+  // The four waves of each column tile joined, in order: 16 threads a column, D / 16 dims each.
+  // A candidate's only split is the result.
+  constexpr int E = D / 16;
+  const int j = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * E;
 #pragma unroll
   for (int t = 0; t < NC; ++t) {
     const float l = xor32_sum(xor16_sum(l_run[t]));
@@ -343,30 +395,39 @@ __global__ __launch_bounds__(256, NC == 1 ? 2 : 1) void attn8_split_kernel(Attn8
     for (int b = 0; b < NB; ++b)
       *reinterpret_cast<f32x4*>(&w_acc[wave][col][16 * b + 4 * grp]) = acc[t][b];
     __syncthreads();
-    for (int idx = threadIdx.x; idx < 16 * D; idx += 256) {
-      const int j = idx / D, e = idx - j * D;
-      const int cc = (cg * NC + t) * 16 + j;
-      const int tok = cc / G, head = c * G + cc - tok * G;
-      if (cc >= cols) continue;
-      float M = -INFINITY;
+    const int cc = (cg * NC + t) * 16 + j;
+    if (cc < cols) {
+      const float M = fmaxf(fmaxf(w_m[0][j], w_m[1][j]), fmaxf(w_m[2][j], w_m[3][j]));
+      float S = 0.f, O[E];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) M = fmaxf(M, w_m[w][j]);
-      const float mz = M == -INFINITY ? 0.f : M;
-      float S = 0.f, O = 0.f;
+      for (int e = 0; e < E; ++e) O[e] = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float f = exp2f(w_m[w][j] - mz);
+        const float f = __builtin_amdgcn_exp2f(w_m[w][j] - M);
         S += w_l[w][j] * f;
-        O += w_acc[w][j][e] * f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) O[e] += w_acc[w][j][e0 + e] * f;
       }
       if (sp.count == 1) {
-        if (tok < m || a.clear_rest)
-          a.out[(((size_t)i * a.tokens + tok) * a.hq + head) * D + e] =
-              f32_to_bf16(S == 0.f || tok >= m ? 0.f : O / S);
+        const int tok = token_of(a, cc), head = c * G + cc - tok * G;
+        if (tok < m || a.clear_rest) {
+          uint32_t o[E / 2];
+          const float inv = S == 0.f ? 0.f : 1.f / S;
+#pragma unroll
+          for (int e = 0; e < E; e += 2)
+            o[e / 2] = tok < m ? pack_bf16x2(O[e] * inv, O[e + 1] * inv) : 0u;
+          uint32_t* dst = reinterpret_cast<uint32_t*>(
+              a.out + (((size_t)i * a.tokens + tok) * a.hq + head) * D + e0);
+#pragma unroll
+          for (int e = 0; e < E / 2; ++e) dst[e] = o[e];
+        }
       } else {
         const size_t slot = ((size_t)flat * a.hkv + c) * cols + cc;
-        a.part_acc[slot * D + e] = O;
-        if (e == 0) {
+        float* dst = a.part_acc + slot * D + e0;
+#pragma unroll
+        for (int e = 0; e < E; e += 4)
+          *reinterpret_cast<f32x4*>(dst + e) = f32x4{O[e], O[e + 1], O[e + 2], O[e + 3]};
+        if (e0 == 0) {
           a.part_ml[slot * 2] = M;
           a.part_ml[slot * 2 + 1] = S;
         }
@@ -375,115 +436,138 @@ __global__ __launch_bounds__(256, NC == 1 ? 2 : 1) void attn8_split_kernel(Attn8
   }
 }
 
-// Joins the splits of one (candidate, kv head, query row), in split order within each wave and
-// then over the waves, so the same call gives the same bits.
-template <int D>
+// Joins the splits of one query row, in a fixed order: the same call gives the same bits.  W waves a
+// row (1: four rows a workgroup), each takes every W-th split, eight of them in flight: what it
+// takes is a few memory latencies.
+template <int D, int W>
 __global__ __launch_bounds__(256) void attn8_join_kernel(Attn8Args a) {
   constexpr int E = D / 64;
-  __shared__ PlanLds plan;
-  __shared__ float w_m[4], w_l[4], w_acc[4][D];
-  const int rows = a.hq * a.tokens;
-  const int i = blockIdx.x / rows;
-  const Split sp = find_split(a.seq_lens, a.n, a.max_pages, a.target, ~i, plan);
+  constexpr int U = 8;
+  __shared__ float w_m[W], w_l[W], w_acc[W][D];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.group, cols = a.tokens * G;
+  const int cc = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  if (cc >= cols) return;  // (behind the last row of the last workgroup, W = 1)
+  const int c = blockIdx.y, i = blockIdx.z;
+  const Split sp = find_split(a, ~i);
   if (sp.count <= 1) return;
-  const int G = a.hq / a.hkv, cols = a.tokens * G;
-  const int c = (blockIdx.x - i * rows) / cols, cc = blockIdx.x - i * rows - c * cols;
-  const int tok = cc / G, head = c * G + cc - tok * G;
+  const int tok = token_of(a, cc), head = c * G + cc - tok * G;
   int m = a.q_lens ? a.q_lens[i] : a.tokens;
   m = m < 0 ? 0 : (m > a.tokens ? a.tokens : m);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   bf16_t* o = a.out + (((size_t)i * a.tokens + tok) * a.hq + head) * D;
   if (tok >= m) {
-    if (a.clear_rest && threadIdx.x < D) o[threadIdx.x] = 0;
+    if (a.clear_rest && (W == 1 || wave == 0))
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[lane + 64 * e] = 0;
     return;
   }
   const size_t step = (size_t)a.hkv * cols;  // slots between a candidate's splits
   const size_t slot0 = ((size_t)sp.first * a.hkv + c) * cols + cc;
-  float M = -INFINITY, S = 0.f, O[E];
+  float M = kNoScore, S = 0.f, O[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) O[e] = 0.f;
-  // a wave takes every fourth split, four of them in flight
-  for (int s0 = w; s0 < sp.count; s0 += 16) {
-    float ms[4], ls[4], ac[4][E];
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const int s = s0 + 4 * y;
-      ms[y] = -INFINITY;
-      ls[y] = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) ac[y][e] = 0.f;
-      if (s < sp.count) {
-        const size_t slot = slot0 + s * step;
-        ms[y] = a.part_ml[slot * 2];
-        ls[y] = a.part_ml[slot * 2 + 1];
-#pragma unroll
-        for (int e = 0; e < E; ++e) ac[y][e] = a.part_acc[slot * D + lane + 64 * e];
-      }
+  for (int s0 = W == 1 ? 0 : wave; s0 < sp.count; s0 += 64 * W) {
+    // a split per lane: its share of the sum; then the splits' rows, U of them in flight (past the
+    // last one the last again, with the share 0)
+    const int mine = min(64, (sp.count - s0 + W - 1) / W);
+    float ml = kNoScore, ll = 0.f;
+    if (lane < mine) {
+      const float2 p = *reinterpret_cast<const float2*>(a.part_ml + (slot0 + (size_t)(s0 + W * lane) * step) * 2);
+      ml = p.x;
+      ll = p.y;
     }
-    float top = M;
+    float ac[U][E];
+    auto rows = [&](int y0) {
 #pragma unroll
-    for (int y = 0; y < 4; ++y) top = fmaxf(top, ms[y]);
-    const float tz = top == -INFINITY ? 0.f : top;
-    const float f0 = exp2f(M - tz);
-    S *= f0;
+      for (int y = 0; y < U; ++y) {
+        const float* r = a.part_acc + (slot0 + (size_t)(s0 + W * min(y0 + y, mine - 1)) * step) * D;
+#pragma unroll
+        for (int e = 0; e < E; ++e) ac[y][e] = r[lane + 64 * e];
+      }
+    };
+    rows(0);
+    const float top = fmaxf(M, wave_max(ml));
+    const float f0 = __builtin_amdgcn_exp2f(M - top), f = lane < mine ? __builtin_amdgcn_exp2f(ml - top) : 0.f;
+    S = S * f0 + wave_sum(ll * f);
 #pragma unroll
     for (int e = 0; e < E; ++e) O[e] *= f0;
+    for (int y0 = 0;;) {
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const float f = exp2f(ms[y] - tz);
-      S += ls[y] * f;
+      for (int y = 0; y < U; ++y) {
+        const float fy = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), (y0 + y) & 63));
+        const float g = y0 + y < mine ? fy : 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) O[e] += ac[y][e] * f;
+        for (int e = 0; e < E; ++e) O[e] += ac[y][e] * g;
+      }
+      if ((y0 += U) >= mine) break;
+      rows(y0);
     }
     M = top;
   }
-  if (lane == 0) {
-    w_m[w] = M;
-    w_l[w] = S;
-  }
-#pragma unroll
-  for (int e = 0; e < E; ++e) w_acc[w][lane + 64 * e] = O[e];
-  __syncthreads();
-  if (threadIdx.x < D) {
-    const int e = threadIdx.x;
-    float T = fmaxf(fmaxf(w_m[0], w_m[1]), fmaxf(w_m[2], w_m[3]));
-    T = T == -INFINITY ? 0.f : T;
-    float L = 0.f, A = 0.f;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const float f = exp2f(w_m[x] - T);
-      L += w_l[x] * f;
-      A += w_acc[x][e] * f;
+  if constexpr (W > 1) {
+    if (lane == 0) {
+      w_m[wave] = M;
+      w_l[wave] = S;
     }
-    o[e] = f32_to_bf16(L == 0.f ? 0.f : A / L);
+#pragma unroll
+    for (int e = 0; e < E; ++e) w_acc[wave][lane + 64 * e] = O[e];
+    __syncthreads();
+    if (wave) return;
+    M = w_m[0];
+#pragma unroll
+    for (int x = 1; x < W; ++x) M = fmaxf(M, w_m[x]);
+    S = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) O[e] = 0.f;
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+      const float f = __builtin_amdgcn_exp2f(w_m[x] - M);
+      S += w_l[x] * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) O[e] += w_acc[x][lane + 64 * e] * f;
+    }
   }
+  const float inv = S == 0.f ? 0.f : 1.f / S;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[lane + 64 * e] = f32_to_bf16(O[e] * inv);
 }
 
 template <int D>
 static hipError_t launch_attn8_d(const Attn8Args& a, int nc, hipStream_t st) {
-  const dim3 grid((unsigned)(a.hkv * a.col_tiles * a.max_splits));
+  const dim3 grid((unsigned)(a.hkv * a.col_tiles), (unsigned)a.max_splits);
   auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a); };
-  if (nc == 1) go(attn8_split_kernel<D, 1>);
-  else if (nc == 2) go(attn8_split_kernel<D, 2>);
-  else go(attn8_split_kernel<D, 4>);
+  if (nc == 1) go(attn8_split_kernel<D, 1, D == 64 ? 2 : 1>);
+  else if (nc == 2) go(attn8_split_kernel<D, 2, 1>);
+  else if (nc == 3) go(attn8_split_kernel<D, 3, 1>);
+  else go(attn8_split_kernel<D, 4, 1>);
   hipError_t e = hipGetLastError();
   // pages that one split holds: every candidate has one, nothing to join
-  if (e != hipSuccess || a.max_pages <= kAttn8MinChunk) return e;
-  hipLaunchKernelGGL(attn8_join_kernel<D>, dim3((unsigned)(a.hq * a.tokens * a.n)), dim3(256),
-                     0, st, a);
-  return hipGetLastError();
+  if (e != hipSuccess || a.max_pages <= kAttn8OneSplit) return e;
+  const unsigned cols = (unsigned)(a.tokens * a.group);
+  auto join = [&](auto kern, unsigned groups) {
+    hipLaunchKernelGGL(kern, dim3(groups, (unsigned)a.hkv, (unsigned)a.n), dim3(256), 0, st, a);
+    return hipGetLastError();
+  };
+  // few candidates have many splits each, and few rows
+  if (a.one_round > 12 * a.n) return join(attn8_join_kernel<D, 4>, cols);
+  return join(attn8_join_kernel<D, 1>, (cols + 3) / 4);
 }
 
-Attn8Plan plan_attn8(int n, int hq, int hkv, int tokens, int max_pages) {
+Attn8Plan plan_attn8(int n, int hq, int hkv, int d, int tokens, int max_pages) {
   Attn8Plan p;
   const int cols = tokens * (hq / hkv), tiles = (cols + 15) / 16;
-  p.nc = tiles >= 3 ? 4 : tiles;
-  p.col_tiles = (tiles + p.nc - 1) / p.nc;
-  const int per = hkv * p.col_tiles;  // workgroups of a split
-  p.target = (kAttn8Workgroups + per - 1) / per;
-  // at most all pages / chunk + one more a candidate, and never more than the pages' own count
-  const long long most = (long long)n * ((max_pages + kAttn8MinChunk - 1) / kAttn8MinChunk);
-  const long long s = (long long)p.target + n;
+  p.col_tiles = (tiles + kAttn8MaxTiles - 1) / kAttn8MaxTiles;
+  p.nc = (tiles + p.col_tiles - 1) / p.col_tiles;
+  const int per = hkv * p.col_tiles;                          // workgroups of a split
+  const int places = std::max(1, 256 * waves8(d, p.nc) / per);  // splits that are resident at once
+  // all pages / chunk + n splits at most
+  p.one_round = std::max(std::max(places - n, places / 2), 1);
+  p.rounds = std::max(kAttn8Rounds * 256 / per, 1);
+  // a join costs 5 us: short candidates are one split
+  p.min_chunk = max_pages <= kAttn8OneSplit ? kAttn8OneSplit : kAttn8MinChunk;
+  const long long most = (long long)n * ((max_pages + p.min_chunk - 1) / p.min_chunk);
+  const long long s = (long long)std::max(p.one_round, p.rounds) + n;
   p.max_splits = s < most ? s : most;
   return p;
 }

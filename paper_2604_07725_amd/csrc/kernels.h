@@ -302,17 +302,24 @@ struct KvPagesArgs {
 hipError_t launch_pack_kv8(const KvPagesArgs& a, int to8, hipStream_t st);
 
 // ---- attn_decode8.hip
-constexpr int kAttn8MinChunk = 32;      // pages of a split, at least (but for a candidate's only one)
-constexpr int kAttn8Workgroups = 2048;  // workgroups aimed at where the pages allow
+constexpr int kAttn8MinChunk = 16;   // pages of a split, at least (but for a candidate's only one)
+constexpr int kAttn8OneSplit = 32;   // page tables up to this width: one split a candidate
+constexpr int kAttn8LongChunk = 192;  // beyond, several rounds of workgroups
+constexpr int kAttn8Rounds = 8;       // workgroups per CU that those aim at
+constexpr int kAttn8MaxTiles = 4;       // column tiles of a workgroup
 struct Attn8Plan {
   int nc, col_tiles;  // column tiles of 16 query rows per workgroup; workgroups per kv head and split
-  int target;         // splits aimed at, over all candidates
+  int one_round;      // splits aimed at, over all candidates: all resident at once
+  int rounds;         // in several rounds
+  int min_chunk;      // pages of a split, at least
   long long max_splits;
 };
-Attn8Plan plan_attn8(int n, int hq, int hkv, int tokens, int max_pages);
+Attn8Plan plan_attn8(int n, int hq, int hkv, int d, int tokens, int max_pages);
 struct Attn8Args {
   int n, tokens, hq, hkv, d, max_pages, clear_rest;
-  int col_tiles, target, max_splits;
+  int col_tiles, one_round, rounds, min_chunk, max_splits;
+  int group;        // hq / hkv
+  float inv_group;  // 1 / group
   int64_t num_pages;
   const bf16_t* q;  // [n][tokens][hq][d]
   const uint8_t* kv_pool;

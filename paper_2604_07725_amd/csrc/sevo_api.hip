@@ -1717,15 +1717,11 @@ sevo_status check_attn8_shape(int n, int tokens, int hq, int hkv, int d, int max
     return fail(SEVO_ERR_UNSUPPORTED, "n_q_heads %d / n_kv_heads %d: a whole number up to 16", hq,
                 hkv);
   const int64_t grid = (int64_t)1 << 31;
-  if (max_pages > 0x7FFFFFFF / SEVO_PAGE_SIZE || (int64_t)n * max_pages > (int64_t)1 << 40 ||
-      (int64_t)hq * tokens >= grid)
-    return fail(SEVO_ERR_UNSUPPORTED, "more keys or heads than a call takes");
-  if (n > 0) {
-    const sevo::Attn8Plan p = sevo::plan_attn8(n, hq, hkv, tokens, max_pages);
-    if ((int64_t)hq * tokens * n >= grid / 256 || p.max_splits * hkv * p.col_tiles >= grid / 256)
-      return fail(SEVO_ERR_UNSUPPORTED, "n %d of %d heads and %d tokens: fewer candidates a call", n,
-                  hq, tokens);
-  }
+  if (max_pages > 0x7FFFFFFF / SEVO_PAGE_SIZE || (int64_t)n * max_pages >= grid || hkv > 65535)
+    return fail(SEVO_ERR_UNSUPPORTED, "%d candidates of %d pages, %d kv heads: more than a call takes",
+                n, max_pages, hkv);
+  if (n > 0 && (n > 65535 || sevo::plan_attn8(n, hq, hkv, d, tokens, max_pages).max_splits > 65535))
+    return fail(SEVO_ERR_UNSUPPORTED, "n %d: fewer candidates a call", n);
   return SEVO_OK;
 }
 
@@ -1734,7 +1730,7 @@ struct Attn8Layout {
 };
 Attn8Layout attn8_layout(int hq, int tokens, int d, int max_pages, const sevo::Attn8Plan& p) {
   Attn8Layout L{0, 0, 0};
-  if (max_pages <= sevo::kAttn8MinChunk) return L;  // one split a candidate: no partials
+  if (max_pages <= sevo::kAttn8OneSplit) return L;  // one split a candidate: no partials
   const size_t rows = (size_t)p.max_splits * hq * tokens;
   L.acc = round_up(rows * 2 * sizeof(float), 256);
   L.total = L.acc + round_up(rows * d * sizeof(float), 256);
@@ -1783,7 +1779,7 @@ SEVO_API size_t sevo_attn_fp8_workspace_bytes(int32_t n, int32_t n_tokens, int32
                                               int32_t max_pages) {
   if (n <= 0 || check_attn8_shape(n, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages)) return 0;
   return attn8_layout(n_q_heads, n_tokens, head_dim, max_pages,
-                      sevo::plan_attn8(n, n_q_heads, n_kv_heads, n_tokens, max_pages)).total;
+                      sevo::plan_attn8(n, n_q_heads, n_kv_heads, head_dim, n_tokens, max_pages)).total;
 }
 
 SEVO_API sevo_status sevo_attn_decode_fp8(const sevo_attn_fp8_args* a, void* stream) {
@@ -1803,7 +1799,7 @@ SEVO_API sevo_status sevo_attn_decode_fp8(const sevo_attn_fp8_args* a, void* str
       bad_ptr(a->out) || odd_words(a->q_lens))
     return fail(SEVO_ERR_INVALID_ARGUMENT, "null or misaligned pointer");
   const sevo::Attn8Plan p =
-      sevo::plan_attn8(a->n, a->n_q_heads, a->n_kv_heads, a->n_tokens, a->max_pages);
+      sevo::plan_attn8(a->n, a->n_q_heads, a->n_kv_heads, a->head_dim, a->n_tokens, a->max_pages);
   const Attn8Layout L = attn8_layout(a->n_q_heads, a->n_tokens, a->head_dim, a->max_pages, p);
   if (a->workspace_bytes < L.total)
     return fail(SEVO_ERR_WORKSPACE_TOO_SMALL, "attention needs %zu workspace bytes, got %zu",
@@ -1813,7 +1809,8 @@ SEVO_API sevo_status sevo_attn_decode_fp8(const sevo_attn_fp8_args* a, void* str
   sevo::Attn8Args k;
   k.n = a->n; k.tokens = a->n_tokens; k.hq = a->n_q_heads; k.hkv = a->n_kv_heads;
   k.d = a->head_dim; k.max_pages = a->max_pages; k.clear_rest = a->clear_rest;
-  k.col_tiles = p.col_tiles; k.target = p.target; k.max_splits = (int)p.max_splits;
+  k.group = a->n_q_heads / a->n_kv_heads; k.inv_group = 1.f / k.group;
+  k.col_tiles = p.col_tiles; k.one_round = p.one_round; k.rounds = p.rounds; k.min_chunk = p.min_chunk; k.max_splits = (int)p.max_splits;
   k.num_pages = a->num_pages;
   k.q = static_cast<const sevo::bf16_t*>(a->q);
   k.kv_pool = static_cast<const uint8_t*>(a->kv_pool);
