@@ -334,8 +334,13 @@ struct Attn8Args {
 hipError_t launch_attn8(const Attn8Args& a, const Attn8Plan& p, hipStream_t st);
 
 // ---- verify.hip
-constexpr int kVerifyChunk = 4096;  // vocabulary entries of a partial
+constexpr int kVerifyChunk = 2048;  // vocabulary entries of a partial
 constexpr int kVerifyMaxDrafts = 16;
+struct alignas(16) VerifyPart {  // of a row, or kVerifyChunk entries of it
+  double sum;   // of exp, relative to the largest logit
+  float max;    // the largest logit
+  int32_t arg;  // its first index (temp 0)
+};
 struct VerifyArgs {
   int n, drafts, vocab, chunks;
   int64_t ld, ld_draft;  // row strides; candidate i's rows are (drafts + 1) i .. and drafts i ..
@@ -348,9 +353,7 @@ struct VerifyArgs {
   int32_t* out_tokens;
   float* out_logprobs;
   int32_t* out_accepted;
-  double* part_sum;   // [rows][chunks]: sums of exp, relative to the chunk's largest logit
-  float* part_max;    // [rows][chunks]
-  int32_t* part_arg;  // [rows][chunks]: the largest logit's index (temp 0)
+  VerifyPart* parts;  // [rows][chunks]
   double* rest_sum;   // [n][chunks]: of max(p - q, 0)
 };
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t st);

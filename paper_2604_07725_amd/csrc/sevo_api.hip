@@ -1841,17 +1841,15 @@ sevo_status check_verify_shape(int n, int drafts, int vocab) {
 }
 
 struct VerifyLayout {
-  size_t sum, rest, max, arg, total;
+  size_t parts, rest, total;
 };
 VerifyLayout verify_layout(int n, int drafts, int vocab) {
   const size_t chunks = (vocab + sevo::kVerifyChunk - 1) / sevo::kVerifyChunk;
   const size_t parts = (size_t)n * (2 * drafts + 1) * chunks;
   VerifyLayout L;
-  L.sum = 0;
-  L.rest = round_up(parts * 8, 256);
-  L.max = L.rest + round_up(n * chunks * 8, 256);
-  L.arg = L.max + round_up(parts * 4, 256);
-  L.total = L.arg + round_up(parts * 4, 256);
+  L.parts = 0;
+  L.rest = round_up(parts * sizeof(sevo::VerifyPart), 256);
+  L.total = L.rest + round_up(n * chunks * sizeof(double), 256);
   return L;
 }
 
@@ -1892,10 +1890,8 @@ SEVO_API sevo_status sevo_verify_drafts(const sevo_verify_args* a, void* stream)
   v.draft_tokens = a->draft_tokens; v.uniforms = a->uniforms; v.n_drafts = a->counts;
   v.out_tokens = a->out_tokens; v.out_logprobs = a->out_logprobs; v.out_accepted = a->out_accepted;
   char* ws = static_cast<char*>(a->workspace);
-  v.part_sum = reinterpret_cast<double*>(ws + L.sum);
+  v.parts = reinterpret_cast<sevo::VerifyPart*>(ws + L.parts);
   v.rest_sum = reinterpret_cast<double*>(ws + L.rest);
-  v.part_max = reinterpret_cast<float*>(ws + L.max);
-  v.part_arg = reinterpret_cast<int32_t*>(ws + L.arg);
   hipError_t e = sevo::launch_verify(v, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_verify_drafts");
 }

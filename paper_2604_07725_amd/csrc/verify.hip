@@ -10,8 +10,8 @@
 // from its neighbour by 1e-6 of the mass and less, so a sum in 32 bits would move
 // choices.  Exponentials and sums are in 64 bits throughout (2^-50 relative each), which
 // the rows' reads cover: bound by HBM, then by the vector ALU.  Three kernels:
-//   1. per (row, 4096 entries): the largest logit and the sum of exponentials relative to it;
-//   2. (a draft distribution given) per (candidate, 4096 entries): the sum of max(p - q, 0) of the
+//   1. per (row, 2048 entries): the largest logit and the sum of exponentials relative to it;
+//   2. (a draft distribution given) per (candidate, 2048 entries): the sum of max(p - q, 0) of the
 //      row where the candidate's drafts end;
 //   3. per candidate: the chunk that holds the drawn point, and in it the entry.
 // Kernels 2 and 3 find the number of accepted drafts from 1's sums, each workgroup for its
@@ -47,19 +47,45 @@ __device__ __forceinline__ double exp2d(double x) {
   return __builtin_amdgcn_ldexp(y, x == x ? (int)n : 0);
 }
 
+// the two words of a double through a lane permutation in registers
+template <typename F>
+__device__ __forceinline__ double by_words(double v, F&& f) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)f((uint32_t)b) | ((uint64_t)f((uint32_t)(b >> 32)) << 32));
+}
+template <int J>
+__device__ __forceinline__ double lane_xor64(double v) {
+  return by_words(v, [](uint32_t x) { return lane_xor<J>(x); });
+}
+__device__ __forceinline__ double row16_sum64(double v) {
+  v += lane_xor64<1>(v);
+  v += lane_xor64<2>(v);
+  v += lane_xor64<4>(v);
+  return v + lane_xor64<8>(v);
+}
 __device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  v = row16_sum64(v);
+  v += lane_xor64<16>(v);
+  return v + lane_xor64<32>(v);
+}
+// lanes without a source get 0
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp64(double v) {
+  return by_words(v, [](uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false);
+  });
 }
 __device__ __forceinline__ double wave_scan64(double v) {  // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
+  v += dpp64<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+  v += dpp64<0x112, 0xF>(v);
+  v += dpp64<0x114, 0xF>(v);
+  v += dpp64<0x118, 0xF>(v);
+  v += dpp64<0x142, 0xA>(v);  // row_bcast 15 into rows 1, 3
+  return v + dpp64<0x143, 0xC>(v);  // row_bcast 31 into rows 2, 3
+}
+// the value of lane l, the same for all
+__device__ __forceinline__ double lane64(double v, int l) {
+  return by_words(v, [l](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); });
 }
 
 // entries v .. v + 3 of a row, -inf at and past vocab (nothing is read there)
@@ -93,70 +119,115 @@ __device__ __forceinline__ double log2_scale(const VerifyArgs& a) {
   return 1.4426950408889634074 / (a.temp == 0.0 ? 1.0 : a.temp);
 }
 
+
+// The sums' exponential, factor * 2^(d c): factor * 2^(k / 32) from a table in LDS (its 32 entries are
+// 64 banks: no two lanes conflict), times a degree-5 polynomial on [-1/64, 1/64] (1.4e-16 relative),
+// scaled by 2^n in the table entry's exponent: 11 operations in 64 bits an entry, half of exp2d's.
+// d at most 0; what is more than 2^900 below 1, also a -inf (and a NaN), is taken for 2^-900
+// (a factor of 2^-24 at least then stays a normal number).
+struct ExpTable {
+  double t[32];
+};
+__device__ __forceinline__ void make_table(ExpTable& T, double factor) {
+  const int j = threadIdx.x & 63;
+  if (j < 32) T.t[j] = factor * exp2d(j * (1.0 / 32.0));
+}
+struct ExpScale {
+  double c32, least;
+  __device__ __forceinline__ explicit ExpScale(double c) : c32(32.0 * c), least(-900.0 / c) {}
+};
+__device__ __forceinline__ void exp_parts(const ExpTable& T, const ExpScale& E, double d, double& poly,
+                                          double& entry) {
+  const double magic = 6755399441055744.0;  // 1.5 2^52: the sum's low bits are d c32 rounded
+  d = __builtin_fmax(d, E.least);
+  const double t = __builtin_fma(d, E.c32, magic);
+  const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+  const double r = __builtin_fma(d, E.c32, magic - t);
+  const uint64_t b = __builtin_bit_cast(uint64_t, T.t[k & 31]);
+  double y = 3.9737266313166245e-11;
+  y = __builtin_fma(y, r, 9.172616498159851e-09);
+  y = __builtin_fma(y, r, 1.6938509724215757e-06);
+  y = __builtin_fma(y, r, 0.0002345961981972034);
+  y = __builtin_fma(y, r, 0.02166084939249829);
+  poly = __builtin_fma(y, r, 1.0);
+  const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)(k >> 5) << 20);
+  entry = __builtin_bit_cast(double, (uint64_t)(uint32_t)b | ((uint64_t)hi << 32));
+}
+
 }  // namespace
 
-__global__ __launch_bounds__(256) void verify_rows_kernel(VerifyArgs a) {
-  __shared__ float s_max[4];
-  __shared__ double s_sum[4];
-  __shared__ int s_arg[4];
-  const size_t row = blockIdx.x / a.chunks;
-  const int chunk = blockIdx.x - (unsigned)(row * a.chunks);
-  const size_t targets = (size_t)a.n * (a.drafts + 1);
-  // rows behind a candidate's last draft are not read
-  if (row < targets) {
-    const int i = (int)(row / (a.drafts + 1));
-    if ((int)(row - (size_t)i * (a.drafts + 1)) > drafts_of(a, i)) return;
-  } else {
-    const int i = (int)((row - targets) / a.drafts);
-    if ((int)(row - targets - (size_t)i * a.drafts) >= drafts_of(a, i)) return;
+// A wave per (row, 2048 entries), 32 a lane in registers from one read: no barrier but the
+// table's, so that some waves' loads are in flight while others compute.
+__global__ __launch_bounds__(256, 6) void verify_rows_kernel(VerifyArgs a) {
+  __shared__ ExpTable T;
+  constexpr int J = kVerifyChunk / 256;
+  const int lane = threadIdx.x & 63;
+  const unsigned job = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned row = job / a.chunks;
+  const int chunk = job - row * a.chunks;
+  const unsigned targets = a.n * (a.drafts + 1);
+  // rows behind a candidate's last draft are not read, nor is anything past the last row
+  bool on = row < targets + (a.draft_logits && a.temp != 0.0 ? a.n * a.drafts : 0);
+  if (on) {
+    const unsigned own = row < targets ? row : row - targets;
+    const unsigned each = row < targets ? a.drafts + 1 : a.drafts;
+    const int i = (int)(own / each);
+    on = (int)(own - i * each) < drafts_of(a, i) + (row < targets ? 1 : 0);
   }
-  const float* r = row_ptr(a, row);
-  const int v0 = chunk * kVerifyChunk + threadIdx.x * 4;
-  f32x4 z[kPer / 4];
+  f32x4 z[J];
+  if (on) {
+    const float* r = row_ptr(a, row);
+    const int v0 = chunk * kVerifyChunk + lane * 4;
+    if ((chunk + 1) * kVerifyChunk <= a.vocab) {
 #pragma unroll
-  for (int j = 0; j < kPer / 4; ++j) z[j] = row4(r, v0 + 1024 * j, a.vocab);
+      for (int j = 0; j < J; ++j)
+        z[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(r + v0 + 256 * j));
+    } else {
+#pragma unroll
+      for (int j = 0; j < J; ++j) z[j] = row4(r, v0 + 256 * j, a.vocab);
+    }
+  }
+  if (threadIdx.x < 64) make_table(T, 1.0);
+  __syncthreads();
+  if (!on) return;
   float m = -INFINITY;
 #pragma unroll
-  for (int j = 0; j < kPer / 4; ++j) m = fmaxf(fmaxf(fmaxf(m, z[j].x), fmaxf(z[j].y, z[j].z)), z[j].w);
+  for (int j = 0; j < J; ++j) m = fmaxf(fmaxf(fmaxf(m, z[j].x), fmaxf(z[j].y, z[j].z)), z[j].w);
   m = wave_max(m);
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if (lane == 0) s_max[w] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-  const double c = log2_scale(a);
-  const double mc = m == -INFINITY ? 0.0 : (double)m;
+  const ExpScale E(log2_scale(a));
+  const double md = m;
   double sum = 0.0;
-  int arg = 0x7FFFFFFF;
+  bool none = false;  // a NaN or a +inf: no distribution
 #pragma unroll
-  for (int j = 0; j < kPer / 4; ++j)
+  for (int j = 0; j < J; ++j) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      sum += exp2d(((double)z[j][k] - mc) * c);
-      if (z[j][k] == m) arg = min(arg, v0 + 1024 * j + k);
+      none |= !(z[j][k] <= 3.402823466e38f);
+      double y, e;
+      exp_parts(T, E, (double)z[j][k] - md, y, e);
+      sum = __builtin_fma(y, e, sum);
     }
+    __builtin_amdgcn_sched_barrier(0);  // (four at a time: all at once take twice the registers)
+  }
+  if (m == -INFINITY) sum = 0.0;
+  if (none) sum = NAN;
   sum = wave_sum64(sum);
-  arg = wave_min(arg);
-  if (lane == 0) {
-    s_sum[w] = sum;
-    s_arg[w] = arg;
+  int arg = 0x7FFFFFFF;
+  if (a.temp == 0.0) {
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (z[j][k] == m) arg = min(arg, chunk * kVerifyChunk + lane * 4 + 256 * j + k);
+    arg = wave_min(arg);
   }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const size_t at = row * a.chunks + chunk;
-    a.part_max[at] = m;
-    a.part_sum[at] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
-    a.part_arg[at] = min(min(s_arg[0], s_arg[1]), min(s_arg[2], s_arg[3]));
-  }
+  if (lane == 0) a.parts[(size_t)row * a.chunks + chunk] = VerifyPart{sum, m, arg};
 }
 
 namespace {
 
 // a row's largest logit, its sum of exponentials, its first largest entry
-struct RowSum {
-  double sum;
-  float max;
-  int arg;
-};
+using RowSum = VerifyPart;
 struct Decision {
   int taken, count;
 };
@@ -165,23 +236,44 @@ struct VerifyLds {
   int taken;
 };
 
-// one wave: the row's partials joined, every lane gets the result
+// over the 16 lanes of a row of the wave, every lane gets it
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, lane_xor<1>(v));
+  v = fmaxf(v, lane_xor<2>(v));
+  v = fmaxf(v, lane_xor<4>(v));
+  return fmaxf(v, lane_xor<8>(v));
+}
+
+// 16 lanes: the row's partials joined, every lane gets the result
 __device__ __forceinline__ RowSum join_row(const VerifyArgs& a, size_t row) {
-  const int lane = threadIdx.x & 63;
-  const float* pm = a.part_max + row * a.chunks;
-  const double* ps = a.part_sum + row * a.chunks;
-  const int32_t* pa = a.part_arg + row * a.chunks;
+  const int q = threadIdx.x & 15;
+  const VerifyPart* p = a.parts + row * a.chunks;
+  constexpr int U = 5;  // partials of a lane in flight: 80 chunks, 163840 entries
+  VerifyPart v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) v[u] = p[min(q + 16 * u, a.chunks - 1)];
   float m = -INFINITY;
-  for (int k = lane; k < a.chunks; k += 64) m = fmaxf(m, pm[k]);
-  m = wave_max(m);
+#pragma unroll
+  for (int u = 0; u < U; ++u) m = fmaxf(m, v[u].max);
+  for (int k = q + 16 * U; k < a.chunks; k += 16) m = fmaxf(m, p[k].max);
+  m = row16_max(m);
   const double mc = m == -INFINITY ? 0.0 : (double)m, c = log2_scale(a);
   double s = 0.0;
   int arg = 0x7FFFFFFF;
-  for (int k = lane; k < a.chunks; k += 64) {
-    s += ps[k] * exp2d(((double)pm[k] - mc) * c);
-    if (pm[k] == m) arg = min(arg, pa[k]);
-  }
-  return RowSum{wave_sum64(s), m, wave_min(arg)};
+  auto add = [&](const VerifyPart& x) {
+    s += x.sum * exp2d(((double)x.max - mc) * c);
+    if (x.max == m) arg = min(arg, x.arg);
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (q + 16 * u < a.chunks) add(v[u]);
+  for (int k = q + 16 * U; k < a.chunks; k += 16) add(p[k]);
+  s = row16_sum64(s);
+  arg = min(arg, lane_xor<1>(arg));
+  arg = min(arg, lane_xor<2>(arg));
+  arg = min(arg, lane_xor<4>(arg));
+  arg = min(arg, lane_xor<8>(arg));
+  return RowSum{s, m, arg};
 }
 
 // a sum that a distribution can have: not of a row with a NaN, a +inf or nothing above -inf
@@ -191,30 +283,43 @@ __device__ __forceinline__ double prob(const VerifyArgs& a, const RowSum& r, flo
   return exp2d(((double)z - (double)r.max) * log2_scale(a)) / r.sum;
 }
 
-// The sums of candidate i's rows into LDS, and how many drafts are accepted.  All threads.
+// The sums of candidate i's rows into LDS, and how many drafts are accepted.  All threads: 16 lanes
+// a row, so that a call with 4 drafts takes two memory latencies.
 __device__ __forceinline__ Decision decide(const VerifyArgs& a, int i, VerifyLds& L) {
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int count = drafts_of(a, i);
   const bool dist = a.draft_logits && a.temp != 0.0;
-  const int rows = count + 1 + (dist ? count : 0);
-  for (int r = w; r < rows; r += 4) {
-    const RowSum s = join_row(a, r <= count ? target_row(a, i, r) : draft_row(a, i, r - count - 1));
-    if (lane == 0) L.row[r <= count ? r : kVerifyMaxDrafts + r - count] = s;
+  const int rows = a.drafts + 1 + (dist ? a.drafts : 0);
+  // (rows behind the last draft are joined too, and not looked at: the count is read beside them)
+  const int count = drafts_of(a, i);
+  const bool mine = w == 0 && lane < count;
+  int x = -1;
+  double u = 0.0;
+  float zx = 0.f, yx = 0.f;
+  if (mine) {
+    x = a.draft_tokens[(size_t)i * a.drafts + lane];
+    u = a.uniforms[(size_t)i * (a.drafts + 1) + lane];
+    if (x >= 0 && x < a.vocab) {
+      zx = row_ptr(a, target_row(a, i, lane))[x];
+      if (dist) yx = row_ptr(a, draft_row(a, i, lane))[x];
+    }
+  }
+  for (int r0 = 0; r0 < rows; r0 += 16) {
+    const int r = r0 + (threadIdx.x >> 4);
+    if (r < rows) {
+      const RowSum s = join_row(a, r <= a.drafts ? target_row(a, i, r) : draft_row(a, i, r - a.drafts - 1));
+      if ((lane & 15) == 0) L.row[r <= a.drafts ? r : kVerifyMaxDrafts + r - a.drafts] = s;
+    }
   }
   __syncthreads();
   if (w == 0) {
     bool ok = true;
-    if (lane < count) {
-      const int x = a.draft_tokens[(size_t)i * a.drafts + lane];
+    if (mine) {
       const RowSum r = L.row[lane];
       ok = false;
-      if (x >= 0 && x < a.vocab && fine(r.sum)) {
-        const double p = a.temp == 0.0 ? (x == r.arg ? 1.0 : 0.0)
-                                       : prob(a, r, row_ptr(a, target_row(a, i, lane))[x]);
-        double q = 1.0;
-        if (dist) q = prob(a, L.row[kVerifyMaxDrafts + 1 + lane], row_ptr(a, draft_row(a, i, lane))[x]);
-        ok = a.temp == 0.0 ? p == 1.0 : (double)a.uniforms[(size_t)i * (a.drafts + 1) + lane] * q < p;
-      }
+      if (x >= 0 && x < a.vocab && fine(r.sum))
+        ok = a.temp == 0.0
+                 ? x == r.arg
+                 : u * (dist ? prob(a, L.row[kVerifyMaxDrafts + 1 + lane], yx) : 1.0) < prob(a, r, zx);
     }
     const uint64_t bad = __builtin_amdgcn_ballot_w64(!ok);
     if (lane == 0) L.taken = bad ? min(count, (int)__builtin_ctzll(bad)) : count;
@@ -297,15 +402,58 @@ __device__ __forceinline__ double chunk_sum(const Weights& W, int chunk, double*
 
 }  // namespace
 
-__global__ __launch_bounds__(256) void verify_rest_kernel(VerifyArgs a) {
+// A workgroup per candidate and four chunks, a wave per chunk; the rows' 1 / sums are factors of the
+// exponentials' tables.
+__global__ __launch_bounds__(256, 4) void verify_rest_kernel(VerifyArgs a) {
   __shared__ VerifyLds L;
-  __shared__ double red[4];
-  const int i = blockIdx.x / a.chunks, chunk = blockIdx.x - i * a.chunks;
+  __shared__ ExpTable P, Q;
+  const int groups = (a.chunks + 3) / 4;
+  const int i = blockIdx.x / groups;
+  const int chunk = (blockIdx.x - i * groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Decision d = decide(a, i, L);
   if (d.taken == d.count) return;
-  const Weights W = weights(a, i, d, L, true);
-  const double s = chunk_sum(W, chunk, red);
-  if (threadIdx.x == 0) a.rest_sum[(size_t)i * a.chunks + chunk] = s;
+  const RowSum t = L.row[d.taken], q = L.row[kVerifyMaxDrafts + 1 + d.taken];
+  const float* tr = row_ptr(a, target_row(a, i, d.taken));
+  const float* dr = row_ptr(a, draft_row(a, i, d.taken));
+  const int v0 = chunk * kVerifyChunk + (threadIdx.x & 63) * 4;
+  constexpr int J = kVerifyChunk / 256;
+  f32x4 z[J], y[J];
+  if ((chunk + 1) * kVerifyChunk <= a.vocab) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      z[j] = *reinterpret_cast<const f32x4*>(tr + v0 + 256 * j);
+      y[j] = *reinterpret_cast<const f32x4*>(dr + v0 + 256 * j);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      z[j] = row4(tr, v0 + 256 * j, a.vocab);
+      y[j] = row4(dr, v0 + 256 * j, a.vocab);
+    }
+  }
+  if (threadIdx.x < 64) make_table(P, 1.0 / t.sum);
+  else if (threadIdx.x < 128) make_table(Q, 1.0 / q.sum);
+  __syncthreads();
+  if (chunk >= a.chunks) return;
+  const ExpScale E(log2_scale(a));
+  const double mt = t.max, mq = q.max;
+  double s = 0.0;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // no multiply-add into the difference: of equal rows nothing is left
+#pragma clang fp contract(off)
+      double pp, pe, qp, qe;
+      exp_parts(P, E, (double)z[j][k] - mt, pp, pe);
+      exp_parts(Q, E, (double)y[j][k] - mq, qp, qe);
+      const double r = pp * pe - qp * qe;
+      s += __builtin_fmax(r, 0.0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  s = wave_sum64(s);
+  if ((threadIdx.x & 63) == 0) a.rest_sum[(size_t)i * a.chunks + chunk] = s;
 }
 
 __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
@@ -315,6 +463,7 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
   __shared__ int s_chunk, s_tok, s_last;
   const int i = blockIdx.x;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const double point = a.uniforms[(size_t)i * (a.drafts + 1) + a.drafts];
   const Decision d = decide(a, i, L);
   const RowSum row = L.row[d.taken];
   const bool valid = fine(row.sum);
@@ -333,33 +482,35 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
     auto weight_of = [&](int k) -> double {
       if (residual && a.draft_logits) return a.rest_sum[(size_t)i * a.chunks + k];
       if (residual && k == hole) return left;
-      return a.part_sum[prow + k] * exp2d(((double)a.part_max[prow + k] - (double)row.max) * W.c);
+      const VerifyPart p = a.parts[prow + k];
+      return p.sum * exp2d(((double)p.max - (double)row.max) * W.c);
     };
     for (int pass = 0;; ++pass) {
       // wave 0: total, then the first chunk whose running sum passes the drawn point
       if (w == 0) {
-        double total = 0.0;
-        for (int k0 = 0; k0 < a.chunks; k0 += 64)
+        const double first = lane < a.chunks ? weight_of(lane) : 0.0;
+        double total = wave_sum64(first);
+        for (int k0 = 64; k0 < a.chunks; k0 += 64)
           total += wave_sum64(k0 + lane < a.chunks ? weight_of(k0 + lane) : 0.0);
-        const double target = (double)a.uniforms[(size_t)i * (a.drafts + 1) + a.drafts] * total;
+        const double target = point * total;
         int found = -1, last = -1;
         double before = 0.0, last_before = 0.0, run = 0.0;
         for (int k0 = 0; k0 < a.chunks && found < 0; k0 += 64) {
-          const double x = k0 + lane < a.chunks ? weight_of(k0 + lane) : 0.0;
+          const double x = k0 == 0 ? first : k0 + lane < a.chunks ? weight_of(k0 + lane) : 0.0;
           const double in = wave_scan64(x);
           const uint64_t over = __builtin_amdgcn_ballot_w64(x > 0.0 && run + in > target);
           const uint64_t some = __builtin_amdgcn_ballot_w64(x > 0.0);
           if (over) {
             const int l = __builtin_ctzll(over);
             found = k0 + l;
-            before = run + __shfl(in - x, l);
+            before = run + lane64(in - x, l);
           }
           if (some) {
             const int l = 63 - __builtin_clzll(some);
             last = k0 + l;
-            last_before = run + __shfl(in - x, l);
+            last_before = run + lane64(in - x, l);
           }
-          run += __shfl(in, 63);
+          run += lane64(in, 63);
         }
         // a point at the very end (a uniform number of 1, or rounding): the last entry
         if (found < 0) {
@@ -374,7 +525,8 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
         }
       }
       __syncthreads();
-      const bool good = s_total > 0.0 && s_total < INFINITY;
+      // (far below any rounding of the differences: nothing but shares of 2^-900)
+      const bool good = s_total > 1e-250 && s_total < INFINITY;
       if (good || !residual) break;
       // nothing left of the residual: the target's own distribution
       residual = false;
@@ -451,11 +603,13 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
   const bool dist = a.draft_logits && a.temp != 0.0 && a.drafts > 0;
   const long long rows = (long long)a.n * (a.drafts + 1) + (dist ? (long long)a.n * a.drafts : 0);
-  hipLaunchKernelGGL(verify_rows_kernel, dim3((unsigned)(rows * a.chunks)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(verify_rows_kernel, dim3((unsigned)((rows * a.chunks + 3) / 4)), dim3(256), 0,
+                     st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (dist) {
-    hipLaunchKernelGGL(verify_rest_kernel, dim3((unsigned)((long long)a.n * a.chunks)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(verify_rest_kernel, dim3((unsigned)(a.n * ((a.chunks + 3) / 4))), dim3(256),
+                       0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

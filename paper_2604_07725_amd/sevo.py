@@ -1004,14 +1004,7 @@ def sevo_kv8_tile_bytes(head_dim) -> int:
     return 2 * PAGE_SIZE * head_dim + 8 * PAGE_SIZE
 
 
-def _kv8_dims(kv_pool, name="kv_pool"):
-    """(pages, kv heads, head_dim) of an 8-bit pool uint8 [pages, hkv, 32 d + 128]."""
-    _need(name, kv_pool, torch.uint8, None, kv_pool.get_device())
-    if kv_pool.dim() != 3 or kv_pool.shape[2] not in (sevo_kv8_tile_bytes(64), sevo_kv8_tile_bytes(128)):
-        raise ValueError(f"{name}: shape {tuple(kv_pool.shape)}, expected [pages, kv heads, 32 d + 128], "
-                         "d 64 or 128")
-    pages, hkv, tile = kv_pool.shape
-    return pages, hkv, (tile - 8 * PAGE_SIZE) // (2 * PAGE_SIZE)
+_KV8_HEAD_DIM = {sevo_kv8_tile_bytes(d): d for d in (64, 128)}
 
 
 def sevo_qk_norm_rope_append_fp8(model, layer, qkv, positions, page_table, kv_pool, rows=None,
@@ -1039,7 +1032,8 @@ def sevo_qk_norm_rope_append_fp8(model, layer, qkv, positions, page_table, kv_po
         _need("positions", positions, i32t, (n,), i)
         _need("page_table", page_table, i32t, (n_rows, max_pages), i)
         _need("kv_pool", kv_pool, torch.uint8, (pages, hkv, sevo_kv8_tile_bytes(d)), i)
-    if rows is not None:
+    if rows is not None and not (rows.dtype is i32t and rows.shape == (n,) and
+                                 rows.is_contiguous() and rows.get_device() == i):
         _need("rows", rows, i32t, (n,), i)
     if q_out is None:
         q_out = torch.empty(n, hq, d, dtype=torch.bfloat16, device=qkv.device)
@@ -1052,23 +1046,26 @@ def sevo_qk_norm_rope_append_fp8(model, layer, qkv, positions, page_table, kv_po
 
 
 def _kv_pages(name, src, dst, hkv, d, src_pages, dst_pages):
-    """The pages entry points: page ids, counts, the call."""
+    """The pages entry points: page ids, the call.  ``dst``: a pool, or the shape and type of a
+    new one with a page per entry."""
     i = src.get_device()
-    lists = [(n, t) for n, t in (("src_pages", src_pages), ("dst_pages", dst_pages)) if t is not None]
-    count = lists[0][1].shape[0] if lists else src.shape[0]
-    for n, t in lists:
-        _need(n, t, torch.int32, (count,), i)
+    count = src.shape[0]
+    if src_pages is not None:
+        count = src_pages.shape[0]
+        if not (src_pages.dtype is torch.int32 and src_pages.dim() == 1 and
+                src_pages.is_contiguous() and src_pages.get_device() == i):
+            _need("src_pages", src_pages, torch.int32, (count,), i)
+    if dst_pages is not None:
+        count = dst_pages.shape[0] if src_pages is None else count
+        _need("dst_pages", dst_pages, torch.int32, (count,), i)
+    if type(dst) is tuple:
+        if dst_pages is not None:
+            raise ValueError("dst_pages: needs the pool that they are of")
+        dst = torch.empty((count, *dst[0]), dtype=dst[1], device=src.device)
     a = KvPagesArgs(hkv, d, count, src.shape[0], dst.shape[0], src.data_ptr(), dst.data_ptr(),
-                    _ptr(src_pages), _ptr(dst_pages))
+                    None if src_pages is None else src_pages.data_ptr(), _ptr(dst_pages))
     _call(name, i, C.byref(a))
     return dst
-
-
-def _made_pages(src, src_pages, dst_pages):
-    """Pages of the pool that a call without a destination makes: one per entry."""
-    if dst_pages is not None:
-        raise ValueError("dst_pages: needs the pool that they are of")
-    return src.shape[0] if src_pages is None else src_pages.shape[0]
 
 
 def sevo_pack_kv_fp8(kv_pool, kv_pool8=None, src_pages=None, dst_pages=None, stream=None):
@@ -1077,16 +1074,17 @@ def sevo_pack_kv_fp8(kv_pool, kv_pool8=None, src_pages=None, dst_pages=None, str
     src_pages[j] to page dst_pages[j] (int32, default j)."""
     if stream is not None:
         return _on_stream(stream, sevo_pack_kv_fp8, kv_pool, kv_pool8, src_pages, dst_pages)
-    _need("kv_pool", kv_pool, torch.bfloat16, None, kv_pool.get_device())
+    if not (kv_pool.dtype is torch.bfloat16 and kv_pool.is_contiguous()):
+        _need("kv_pool", kv_pool, torch.bfloat16, None, kv_pool.get_device())
     if kv_pool.dim() != 4 or kv_pool.shape[2] != 2 or kv_pool.shape[3] % PAGE_SIZE:
         raise ValueError(f"kv_pool: shape {tuple(kv_pool.shape)}, expected [pages, kv heads, 2, 16 d]")
-    hkv, d = kv_pool.shape[1], kv_pool.shape[3] // PAGE_SIZE
+    _, hkv, _, d = kv_pool.shape
+    d //= PAGE_SIZE
+    tile = sevo_kv8_tile_bytes(d)
     if kv_pool8 is None:
-        kv_pool8 = torch.empty(_made_pages(kv_pool, src_pages, dst_pages), hkv, sevo_kv8_tile_bytes(d),
-                               dtype=torch.uint8, device=kv_pool.device)
+        kv_pool8 = (hkv, tile), torch.uint8
     else:
-        _need("kv_pool8", kv_pool8, torch.uint8, (kv_pool8.shape[0], hkv, sevo_kv8_tile_bytes(d)),
-              kv_pool.get_device())
+        _need("kv_pool8", kv_pool8, torch.uint8, (kv_pool8.shape[0], hkv, tile), kv_pool.get_device())
     return _kv_pages("sevo_pack_kv_fp8", kv_pool, kv_pool8, hkv, d, src_pages, dst_pages)
 
 
@@ -1096,10 +1094,15 @@ def sevo_unpack_kv_fp8(kv_pool8, kv_pool=None, src_pages=None, dst_pages=None, s
     ``sevo_pack_kv_fp8``."""
     if stream is not None:
         return _on_stream(stream, sevo_unpack_kv_fp8, kv_pool8, kv_pool, src_pages, dst_pages)
-    _, hkv, d = _kv8_dims(kv_pool8, "kv_pool8")
+    if not (kv_pool8.dtype is torch.uint8 and kv_pool8.is_contiguous()):
+        _need("kv_pool8", kv_pool8, torch.uint8, None, kv_pool8.get_device())
+    if kv_pool8.dim() != 3 or kv_pool8.shape[2] not in _KV8_HEAD_DIM:
+        raise ValueError(f"kv_pool8: shape {tuple(kv_pool8.shape)}, expected [pages, kv heads, "
+                         "32 d + 128], d 64 or 128")
+    _, hkv, tile = kv_pool8.shape
+    d = _KV8_HEAD_DIM[tile]
     if kv_pool is None:
-        kv_pool = torch.empty(_made_pages(kv_pool8, src_pages, dst_pages), hkv, 2, PAGE_SIZE * d,
-                              dtype=torch.bfloat16, device=kv_pool8.device)
+        kv_pool = (hkv, 2, PAGE_SIZE * d), torch.bfloat16
     else:
         _need("kv_pool", kv_pool, torch.bfloat16, (kv_pool.shape[0], hkv, 2, PAGE_SIZE * d),
               kv_pool8.get_device())
@@ -1142,7 +1145,8 @@ def sevo_attn_decode_fp8(q, kv_pool, page_table, seq_lens, q_lens=None, out=None
         _need("kv_pool", kv_pool, torch.uint8, (pages, hkv, sevo_kv8_tile_bytes(d)), i)
         _need("page_table", page_table, i32t, (n, max_pages), i)
         _need("seq_lens", seq_lens, i32t, (n,), i)
-    if q_lens is not None:
+    if q_lens is not None and not (q_lens.dtype is i32t and q_lens.shape == (n,) and
+                                   q_lens.is_contiguous() and q_lens.get_device() == i):
         _need("q_lens", q_lens, i32t, (n,), i)
     clear = out is None
     if clear:
@@ -1172,11 +1176,12 @@ def sevo_verify_workspace_bytes(n, n_drafts, vocab) -> int:
 
 def _ld3(name, t, vocab):
     """Row stride of logits [n, rows, >= vocab] whose rows are equally spaced."""
-    n, r, v = t.shape
+    n, r, _ = t.shape
     if n * r <= 1:
         return -(-vocab // 4) * 4  # (one row has none)
-    ld = t.stride(1) if r > 1 else t.stride(0)
-    if n > 1 and t.stride(0) != r * ld:
+    s0, s1, _ = t.stride()
+    ld = s1 if r > 1 else s0
+    if n > 1 and s0 != r * ld:
         raise ValueError(f"{name}: strides {tuple(t.stride())}, expected equally spaced rows")
     return ld
 
@@ -1203,16 +1208,23 @@ def sevo_verify_drafts(logits, draft_tokens, uniforms, temperature=1.0, draft_lo
     if vocab > width:
         raise ValueError(f"vocab: {vocab}, logits of {width} columns")
     f32t, i32t = torch.float32, torch.int32
-    _need("logits", logits, f32t, None, i, contiguous=False)
-    _need("draft_tokens", draft_tokens, i32t, (n, T), i)
-    _need("uniforms", uniforms, f32t, (n, rows), i)
+    if not (logits.dtype is f32t and logits.is_contiguous() and draft_tokens.dtype is i32t and
+            draft_tokens.shape == (n, T) and draft_tokens.is_contiguous() and
+            uniforms.dtype is f32t and uniforms.shape == (n, rows) and uniforms.is_contiguous() and
+            draft_tokens.get_device() == uniforms.get_device() == i):
+        _need("logits", logits, f32t, None, i, contiguous=False)
+        _need("draft_tokens", draft_tokens, i32t, (n, T), i)
+        _need("uniforms", uniforms, f32t, (n, rows), i)
     ld, ldd = _ld3("logits", logits, vocab), 0
     if draft_logits is not None:
-        _need("draft_logits", draft_logits, f32t, None, i, contiguous=False)
+        if not (draft_logits.dtype is f32t and draft_logits.is_contiguous() and
+                draft_logits.get_device() == i):
+            _need("draft_logits", draft_logits, f32t, None, i, contiguous=False)
         if draft_logits.dim() != 3 or draft_logits.shape[:2] != (n, T) or draft_logits.shape[2] < vocab:
             raise ValueError(f"draft_logits: shape {tuple(draft_logits.shape)}, expected [{n}, {T}, ld]")
         ldd = _ld3("draft_logits", draft_logits, vocab)
-    if n_drafts is not None:
+    if n_drafts is not None and not (n_drafts.dtype is i32t and n_drafts.shape == (n,) and
+                                     n_drafts.is_contiguous() and n_drafts.get_device() == i):
         _need("n_drafts", n_drafts, i32t, (n,), i)
     if out_tokens is None:
         out_tokens = torch.empty(n, rows, dtype=i32t, device=dev)

@@ -57,7 +57,7 @@ def check(sevo, z, x, u, temp, y=None, count=None, **kw):
 @pytest.mark.parametrize("dist", [False, True])
 @pytest.mark.parametrize("n,T,v,temp", [
     (1, 0, 1, 1.0), (1, 1, 1, 1.0), (3, 2, 2, 0.5), (5, 3, 63, 1.0), (4, 4, 4096, 0.7), (3, 2, 4097, 1.0),
-    (7, 16, 1001, 1.3), (2, 5, 20483, 0.6), (2, 3, 151936, 1.0), (40, 1, 300, 1.0), (3, 4, 8191, 0.0), (6, 0, 5000, 1.0)])
+    (7, 16, 1001, 1.3), (2, 5, 20483, 0.6), (2, 3, 151936, 1.0), (1, 2, 250003, 1.0), (1, 1, 250003, 0.0), (40, 1, 300, 1.0), (3, 4, 8191, 0.0), (6, 0, 5000, 1.0)])
 def test_verify(sevo, n, T, v, temp, dist):
     g = gen(n * T + v)
     z = rows(n, T + 1, v, g)
