@@ -806,7 +806,8 @@ sevo_status sevo_unpack_kv_fp8(const sevo_kv_pages_args* a, void* stream); /* 8 
  *   q, out   bf16 [n][n_tokens][n_q_heads][head_dim];  a row that sees no key gets 0
  *   rows t >= m_i of out are left as they were, or set to 0 with clear_rest 1
  *   page_table int32 [n][max_pages];  seq_lens int32 [n], 0 <= len <= 16 max_pages
- * n_tokens 1..16; n_q_heads / n_kv_heads any whole number up to 16.  A page id outside
+ * n_tokens 1..16; n_q_heads / n_kv_heads any whole number up to 16; n up to about 65000, n max_pages
+ * up to 2^30 (else UNSUPPORTED).  A page id outside
  * [0, num_pages) contributes no keys.  The cache is cut into splits by the lengths of
  * all candidates (on the device) and joined in split order: the same call gives the same
  * bits, those of a row may depend on the other candidates' lengths.  Scores, softmax
@@ -858,7 +859,7 @@ size_t sevo_attn_fp8_workspace_bytes(int32_t n, int32_t n_tokens, int32_t n_q_he
  *   out_logprobs fp32 [n][n_drafts + 1]: log p_t of each emitted token, then 0
  *   out_accepted int32 [n]: a_i (a_i + 1 tokens are emitted)
  * n_drafts 0..16 (0: draft_tokens may be NULL); ld, ld_draft multiples of 4, at least
- * vocab; vocab up to 2^24.  The workspace is scratch of sevo_verify_workspace_bytes; calls
+ * vocab; vocab up to 2^24; temperature 0 or 1e-30..1e30; n (2 n_drafts + 1) vocab below about 2^34.  The workspace is scratch of sevo_verify_workspace_bytes; calls
  * that may overlap in time each need their own.  Errors: INVALID_ARGUMENT, UNSUPPORTED,
  * WORKSPACE_TOO_SMALL, HIP. */
 typedef struct {

@@ -20,6 +20,14 @@
 //        (to 2^-17 of itself): the probabilities keep their 32-bit accuracy.
 // More than 16 query rows per kv head are further column tiles of the same page (NC), so
 // the cache is read once for all new tokens.
+//
+// What bounds it: HBM for one token a candidate (16 flop a byte at 8 heads a kv head).  64
+// candidates of 16k-32k keys, 8 x 128 heads, 3.32 GB: 512-528 us, 6.3-6.5 TB/s, what the read probe
+// reaches; one candidate of 65537 keys, 138 MB: 32 us, of them 20 in the loop, the rest
+// the two launches, the way to the first page (lengths, page ids, page: three memory latencies) and
+// the join.  With 40 query rows (5 tokens of 8 heads; 16 candidates of 8k-16k keys, 209 MB, 52 us) the
+// loop is bound by instructions: a wave issues one vector instruction in 8 clocks, and registers
+// leave two waves a SIMD.
 #include <algorithm>
 
 #include "kernels.h"
@@ -41,6 +49,14 @@ __device__ __forceinline__ bf16x8v codes_bf16(uint32_t a, uint32_t b) {
             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true))});
 }
 
+// the largest of three (the compiler's fmaxf first makes quiet every operand that it has lost track of,
+// eight more instructions a column tile)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 __device__ __forceinline__ int keys_of(const int32_t* lens, int i, int max_pages) {
   const int len = lens[i];
   return len < 0 ? 0 : (len > max_pages * kPage ? max_pages * kPage : len);
@@ -49,8 +65,10 @@ __device__ __forceinline__ int pages_of(int keys) { return (keys + kPage - 1) / 
 
 // The split plan, the same in every wave of both kernels: candidate i has max(1, ceil(pages_i /
 // chunk)) splits.  The chunk is the least that gives all workgroups a place at once (then
-// nothing waits for a second round that would be part empty); where that leaves chunks of
-// more than kAttn8LongChunk pages, whose ends would be ragged, several rounds of shorter ones.
+// nothing waits for a second round that would be part empty: one candidate of 65537 keys 35 us
+// against 42 for 3 rounds); where that leaves chunks of more than kAttn8LongChunk pages, whose
+// ends would be ragged, several rounds of shorter ones (64 candidates of 16k-32k: 8 workgroups per
+// CU 515 us, 4 526, 2 575).
 struct Split {
   int cand, index, count, first;  // candidate, split of it, its number of splits, its first flat id
   int len;                        // its keys
@@ -308,56 +326,64 @@ __global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Ar
       }
     }
     load_k(r, n + PF);
-    bf16x8v ph[NC], pl[NC];
+    // four column tiles go in two halves, V's codes converted for each: the probabilities of all
+    // four take registers that are not there
+    constexpr int H = NC == 4 ? 2 : NC;
 #pragma unroll
-    for (int t = 0; t < NC; ++t) {
-      float z[8];
+    for (int t0 = 0; t0 < NC; t0 += H) {
+      bf16x8v ph[H], pl[H];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = s[t][e / 4][e & 3] * ks[e / 4][e & 3];
-      if (masked) {
-        const int v0 = ok0 ? lim[t] - u0 : 0, v1 = ok1 ? lim[t] - u0 - kPage : 0;
+      for (int t = t0; t < t0 + H; ++t) {
+        float z[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          z[e] = e < v0 ? z[e] : -INFINITY;
-          z[4 + e] = e < v1 ? z[4 + e] : -INFINITY;
+        for (int e = 0; e < 8; ++e) z[e] = s[t][e / 4][e & 3] * ks[e / 4][e & 3];
+        if (masked) {
+          const int v0 = ok0 ? lim[t] - u0 : 0, v1 = ok1 ? lim[t] - u0 - kPage : 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            z[e] = e < v0 ? z[e] : -INFINITY;
+            z[4 + e] = e < v1 ? z[4 + e] : -INFINITY;
+          }
         }
-      }
-      float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])),
-                        fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-      top = xor32_max(xor16_max(top));
-      const bool raise = top > m_run[t] + kLazyLog2;
-      if (__builtin_amdgcn_ballot_w64(raise)) {
-        const float mn = raise ? top : m_run[t];
-        const float alpha = __builtin_amdgcn_exp2f(m_run[t] - mn);  // 0 on the first page, 1 without a raise
-        l_run[t] *= alpha;
+        float top = max3(max3(max3(z[0], z[1], z[2]), z[3], z[4]), max3(z[5], z[6], z[7]), z[7]);
+        top = xor32_max(xor16_max(top));
+        const bool raise = top > m_run[t] + kLazyLog2;
+        if (__builtin_amdgcn_ballot_w64(raise)) {
+          const float mn = raise ? top : m_run[t];
+          const float alpha = __builtin_amdgcn_exp2f(m_run[t] - mn);  // 0 on the first page, 1 without a raise
+          l_run[t] *= alpha;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) acc[t][b] *= alpha;
-        m_run[t] = mn;
-      }
-      uint32_t hi[4], lo[4];
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        float p[2];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const float pr = __builtin_amdgcn_exp2f(z[e + y] - m_run[t]);
-          l_run[t] += pr;
-          p[y] = pr * vs[e / 4][(e + y) & 3];
+          for (int b = 0; b < NB; ++b) acc[t][b] *= alpha;
+          m_run[t] = mn;
         }
-        hi[e / 2] = pack_bf16x2(p[0], p[1]);
-        lo[e / 2] = pack_bf16x2(p[0] - bf16_lo(hi[e / 2]), p[1] - bf16_hi(hi[e / 2]));
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          float p[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float pr = __builtin_amdgcn_exp2f(z[e + y] - m_run[t]);
+            l_run[t] += pr;
+            p[y] = pr * vs[e / 4][(e + y) & 3];
+          }
+          hi[e / 2] = pack_bf16x2(p[0], p[1]);
+          asm("" : "+v"(hi[e / 2]));  // (else it is converted once more for what follows)
+          lo[e / 2] = pack_bf16x2(p[0] - bf16_lo(hi[e / 2]), p[1] - bf16_hi(hi[e / 2]));
+        }
+        ph[t - t0] = __builtin_bit_cast(bf16x8v, u32x4{hi[0], hi[1], hi[2], hi[3]});
+        pl[t - t0] = __builtin_bit_cast(bf16x8v, u32x4{lo[0], lo[1], lo[2], lo[3]});
       }
-      ph[t] = __builtin_bit_cast(bf16x8v, u32x4{hi[0], hi[1], hi[2], hi[3]});
-      pl[t] = __builtin_bit_cast(bf16x8v, u32x4{lo[0], lo[1], lo[2], lo[3]});
-    }
-    load_s(r);
+      if (t0 + H == NC) load_s(r);
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const bf16x8v w = codes_bf16(r.v[0][b / 4][b % 4], r.v[1][b / 4][b % 4]);
+      for (int b = 0; b < NB; ++b) {
+        uint32_t v0 = r.v[0][b / 4][b % 4], v1 = r.v[1][b / 4][b % 4];
+        if constexpr (H < NC) asm("" : "+v"(v0), "+v"(v1));  // (not kept converted)
+        const bf16x8v w = codes_bf16(v0, v1);
 #pragma unroll
-      for (int t = 0; t < NC; ++t) {
-        acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, pl[t], acc[t][b], 0, 0, 0);
-        acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, ph[t], acc[t][b], 0, 0, 0);
+        for (int t = t0; t < t0 + H; ++t) {
+          acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, pl[t - t0], acc[t][b], 0, 0, 0);
+          acc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, ph[t - t0], acc[t][b], 0, 0, 0);
+        }
       }
     }
     load_v(r);

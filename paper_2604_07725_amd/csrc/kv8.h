@@ -32,12 +32,18 @@ __host__ __device__ __forceinline__ uint32_t kv8_v_offset(int s, int e) {
 __device__ __forceinline__ float kv8_scale(uint32_t a) {
   return a < 0x7F800000u ? fmaxf(__uint_as_float(a) * (1.f / 448.f), 0x1p-64f) : NAN;
 }
-// four values to four codes (round to nearest even; |y| inv <= 448 (1 + 2^-22) rounds to at most 448)
+// four values, times the reciprocals of their scales, to four codes (round to nearest even;
+// |y| / s <= 448 (1 + 2^-22) rounds to at most 448)
+__device__ __forceinline__ uint32_t kv8_pack(float y0, float y1, float y2, float y3) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y0, y1, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y2, y3, w, true);
+  return (uint32_t)w;
+}
+// four values of one block
 __device__ __forceinline__ uint32_t kv8_codes(float y0, float y1, float y2, float y3, float scale) {
   const float inv = 1.f / scale;
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y0 * inv, y1 * inv, 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(y2 * inv, y3 * inv, w, true);
-  return scale == scale ? (uint32_t)w : 0u;
+  const uint32_t w = kv8_pack(y0 * inv, y1 * inv, y2 * inv, y3 * inv);
+  return scale == scale ? w : 0u;
 }
 
 }  // namespace sevo

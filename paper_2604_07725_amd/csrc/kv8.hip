@@ -11,13 +11,24 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ uint32_t mag(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
+// Calls whose data is larger than the last-level cache read their sources past the caches: kept
+// there they would only put out what is about to be written.  Plain / past the caches, us:
+// to 8 bits 199 MB 35.0 / 35.5, 288 MB 50.3 / 49.5, 407 MB 79.4 / 67.0; back, 407 MB 82.5 / 66.4;
+// append, 290 MB 53.4 / 52.0, 212 MB 41.7 / 40.6.
+constexpr size_t kOnceBytes = (size_t)256 << 20;
+template <bool ONCE, typename V>
+__device__ __forceinline__ V load(const V* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+
 }  // namespace
 
 // One workgroup per token and 4 NP * HPW of its heads.  D / 4 lanes hold a head, four
 // dims each, so a wave reads HPW = 256 / D heads of the projection in one 1 KB access; the
 // rotate-half partner of a dim is in the lane half a head away, the norm's sum and the
 // block's largest magnitude are lane reductions.
-template <int D, int NP>
+template <int D, int NP, bool ONCE>
 __global__ __launch_bounds__(256) void append8_kernel(RopeAppendArgs a, int n_rows,
                                                       uint8_t* __restrict__ pool) {
   constexpr int LPH = D / 4, HPW = 64 / LPH, HALF = D / 2;
@@ -31,7 +42,8 @@ __global__ __launch_bounds__(256) void append8_kernel(RopeAppendArgs a, int n_ro
 #pragma unroll
   for (int j = 0; j < NP; ++j) {
     const int hh = h0 + 4 * HPW * j;
-    u[j] = hh < H ? *reinterpret_cast<const f32x4*>(row + (size_t)hh * D + e) : f32x4{0.f, 0.f, 0.f, 0.f};
+    u[j] = hh < H ? load<ONCE>(reinterpret_cast<const f32x4*>(row + (size_t)hh * D + e))
+                  : f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const int p = a.positions[i];
   const bool pos_ok = p >= 0 && p < a.max_pos;
@@ -116,8 +128,12 @@ hipError_t launch_append8(const RopeAppendArgs& a, int n_rows, uint8_t* pool, hi
     hipLaunchKernelGGL(kern, dim3(a.n, (passes + np - 1) / np), dim3(256), 0, st, a, n_rows, pool);
     return hipGetLastError();
   };
-  if (a.n < 512) return a.d == 128 ? go(append8_kernel<128, 1>, 1) : go(append8_kernel<64, 1>, 1);
-  return a.d == 128 ? go(append8_kernel<128, 6>, 6) : go(append8_kernel<64, 3>, 3);
+  if (a.n < 512)
+    return a.d == 128 ? go(append8_kernel<128, 1, false>, 1) : go(append8_kernel<64, 1, false>, 1);
+  const size_t bytes = (size_t)a.n * a.d * (6 * (size_t)a.hq + 10 * (size_t)a.hkv);
+  if (bytes > kOnceBytes)
+    return a.d == 128 ? go(append8_kernel<128, 6, true>, 6) : go(append8_kernel<64, 3, true>, 3);
+  return a.d == 128 ? go(append8_kernel<128, 6, false>, 6) : go(append8_kernel<64, 3, false>, 3);
 }
 
 namespace {
@@ -140,8 +156,9 @@ __device__ __forceinline__ TilePair tile_pair(const KvPagesArgs& a, uint32_t til
   return t;
 }
 
+template <bool ONCE>
 __device__ __forceinline__ u32x4 load16(const char* p, uint32_t off) {
-  return p ? *reinterpret_cast<const u32x4*>(p + off) : u32x4{0u, 0u, 0u, 0u};
+  return p ? load<ONCE>(reinterpret_cast<const u32x4*>(p + off)) : u32x4{0u, 0u, 0u, 0u};
 }
 
 }  // namespace
@@ -150,7 +167,7 @@ __device__ __forceinline__ u32x4 load16(const char* p, uint32_t off) {
 // lanes a token, eight dims of every 32-dim block each.  V: lane (b, token half, a) holds
 // the dims 64 a + 16 c + b, c < 4, of eight tokens; a token's largest magnitude is over
 // the lanes of its half.
-template <int D>
+template <int D, bool ONCE>
 __global__ __launch_bounds__(256) void pack_kv8_kernel(KvPagesArgs a, uint32_t tiles) {
   constexpr int TPW = 128 / D, NI = D / 32;
   constexpr uint32_t kSrc = 64 * D, kDst = kv8_tile_bytes(D);
@@ -169,7 +186,7 @@ __global__ __launch_bounds__(256) void pack_kv8_kernel(KvPagesArgs a, uint32_t t
       uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const u32x4 v = load16(t.src, i * 1024 + lane * 16);
+        const u32x4 v = load16<ONCE>(t.src, i * 1024 + lane * 16);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           y[i][2 * k] = bf16_lo(v[k]);
@@ -198,7 +215,7 @@ __global__ __launch_bounds__(256) void pack_kv8_kernel(KvPagesArgs a, uint32_t t
     uint32_t top[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const u32x4 v = load16(t.src, 32 * D + (64 * a64 + 16 * c + b) * 32 + h * 16);
+      const u32x4 v = load16<ONCE>(t.src, 32 * D + (64 * a64 + 16 * c + b) * 32 + h * 16);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         y[c][2 * k] = bf16_lo(v[k]);
@@ -207,7 +224,7 @@ __global__ __launch_bounds__(256) void pack_kv8_kernel(KvPagesArgs a, uint32_t t
         top[2 * k + 1] = max(top[2 * k + 1], mag(y[c][2 * k + 1]));
       }
     }
-    float scale[8], use[8];
+    float scale[8], inv[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       uint32_t m = top[k];
@@ -216,28 +233,36 @@ __global__ __launch_bounds__(256) void pack_kv8_kernel(KvPagesArgs a, uint32_t t
       m = max(m, lane_xor<8>(m));
       m = max(m, lane_xor<16>(m));
       if constexpr (D == 128) m = max(m, lane_xor<32>(m));
-      scale[k] = t.src ? kv8_scale(m) : 0.f;
-      use[k] = t.src ? scale[k] : 1.f;
+      scale[k] = kv8_scale(m);
+      inv[k] = 1.f / scale[k];
     }
     if (!t.dst) continue;
+    bool nan = false;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) nan |= scale[k] != scale[k];
+    if (nan) {  // (rare: a token's codes are 0 where its block holds a NaN or an infinity)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (scale[k] != scale[k]) y[c][k] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (scale[k] != scale[k]) inv[k] = 0.f;
+    }
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       u32x4 w;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        w[c] = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int tok = 4 * g + k;
-          w[c] |= (kv8_codes(y[c][tok], 0.f, 0.f, 0.f, use[tok]) & 0xFFu) << (8 * k);
-        }
-      }
+      for (int c = 0; c < 4; ++c)
+        w[c] = kv8_pack(y[c][4 * g] * inv[4 * g], y[c][4 * g + 1] * inv[4 * g + 1],
+                        y[c][4 * g + 2] * inv[4 * g + 2], y[c][4 * g + 3] * inv[4 * g + 3]);
       *reinterpret_cast<u32x4*>(t.dst + 16 * D + a64 * 1024 + (2 * h + g) * 256 + b * 16) = w;
     }
     if (b == 0 && (D == 64 || up == 0)) {
       float* vs = reinterpret_cast<float*>(t.dst + 32 * D) + kPage + 8 * h;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) vs[k] = scale[k];
+      for (int k = 0; k < 8; ++k) vs[k] = t.src ? scale[k] : 0.f;
     }
   }
 }
@@ -245,7 +270,7 @@ __global__ __launch_bounds__(256) void pack_kv8_kernel(KvPagesArgs a, uint32_t t
 // 8-bit tiles to bf16 tiles, the product of code and scale rounded once.  A wave a tile:
 // K lane (token, 16 dims) as two 16-byte stores a 64-dim block, V lane (dims 16 c + b, four
 // tokens) as 8-byte stores.
-template <int D>
+template <int D, bool ONCE>
 __global__ __launch_bounds__(256) void unpack_kv8_kernel(KvPagesArgs a, uint32_t tiles) {
   constexpr int NA = D / 64;
   constexpr uint32_t kSrc = kv8_tile_bytes(D), kDst = 64 * D;
@@ -259,11 +284,11 @@ __global__ __launch_bounds__(256) void unpack_kv8_kernel(KvPagesArgs a, uint32_t
     u32x4 k[NA], v[NA];
 #pragma unroll
     for (int x = 0; x < NA; ++x) {
-      k[x] = load16(t.src, x * 1024 + lane * 16);
-      v[x] = load16(t.src, 16 * D + x * 1024 + lane * 16);
+      k[x] = load16<ONCE>(t.src, x * 1024 + lane * 16);
+      v[x] = load16<ONCE>(t.src, 16 * D + x * 1024 + lane * 16);
     }
     const float ks = t.src ? reinterpret_cast<const float*>(t.src + 32 * D)[s] : 0.f;
-    const u32x4 vsw = load16(t.src, 32 * D + 64 + g * 16);
+    const u32x4 vsw = load16<ONCE>(t.src, 32 * D + 64 + g * 16);
     const f32x4 vs = __builtin_bit_cast(f32x4, vsw);
 #pragma unroll
     for (int x = 0; x < NA; ++x) {
@@ -300,8 +325,12 @@ hipError_t launch_pack_kv8(const KvPagesArgs& a, int to8, hipStream_t st) {
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a, tiles);
     return hipGetLastError();
   };
-  if (to8) return a.d == 128 ? go(pack_kv8_kernel<128>) : go(pack_kv8_kernel<64>);
-  return a.d == 128 ? go(unpack_kv8_kernel<128>) : go(unpack_kv8_kernel<64>);
+  if ((size_t)tiles * (96 * a.d + 128) > kOnceBytes) {
+    if (to8) return a.d == 128 ? go(pack_kv8_kernel<128, true>) : go(pack_kv8_kernel<64, true>);
+    return a.d == 128 ? go(unpack_kv8_kernel<128, true>) : go(unpack_kv8_kernel<64, true>);
+  }
+  if (to8) return a.d == 128 ? go(pack_kv8_kernel<128, false>) : go(pack_kv8_kernel<64, false>);
+  return a.d == 128 ? go(unpack_kv8_kernel<128, false>) : go(unpack_kv8_kernel<64, false>);
 }
 
 }  // namespace sevo

@@ -1716,8 +1716,7 @@ sevo_status check_attn8_shape(int n, int tokens, int hq, int hkv, int d, int max
   if (hkv < 1 || hq < 1 || hq % hkv || hq / hkv > 16)
     return fail(SEVO_ERR_UNSUPPORTED, "n_q_heads %d / n_kv_heads %d: a whole number up to 16", hq,
                 hkv);
-  const int64_t grid = (int64_t)1 << 31;
-  if (max_pages > 0x7FFFFFFF / SEVO_PAGE_SIZE || (int64_t)n * max_pages >= grid || hkv > 65535)
+  if (max_pages > 0x7FFFFFFF / SEVO_PAGE_SIZE || (int64_t)n * max_pages > 1 << 30 || hkv > 65535)
     return fail(SEVO_ERR_UNSUPPORTED, "%d candidates of %d pages, %d kv heads: more than a call takes",
                 n, max_pages, hkv);
   if (n > 0 && (n > 65535 || sevo::plan_attn8(n, hq, hkv, d, tokens, max_pages).max_splits > 65535))
@@ -1865,9 +1864,9 @@ SEVO_API sevo_status sevo_verify_drafts(const sevo_verify_args* a, void* stream)
   if (sevo_status s = check_verify_shape(a->n, a->n_drafts, a->vocab)) return s;
   if (!std::isfinite(a->temperature) || a->temperature < 0.0)
     return fail(SEVO_ERR_INVALID_ARGUMENT, "temperature must be finite and >= 0");
-  // below, logits / temperature leaves the range in which they can be told apart
-  if (a->temperature > 0.0 && a->temperature < 1e-30)
-    return fail(SEVO_ERR_UNSUPPORTED, "temperature %g: 0 or at least 1e-30", a->temperature);
+  // (beyond, differences of logits / temperature leave the range of a double's exponent)
+  if (a->temperature > 0.0 && (a->temperature < 1e-30 || a->temperature > 1e30))
+    return fail(SEVO_ERR_UNSUPPORTED, "temperature %g: 0, or 1e-30 to 1e30", a->temperature);
   const bool dist = a->draft_logits && a->n_drafts > 0;
   if (a->ld < a->vocab || a->ld % 4 || (dist && (a->ld_draft < a->vocab || a->ld_draft % 4)))
     return fail(SEVO_ERR_INVALID_ARGUMENT, "ld %lld, ld_draft %lld: multiples of 4, at least vocab",

@@ -73,7 +73,8 @@ ATTN = dict(n=4, n_tokens=3, n_q_heads=8, n_kv_heads=2, head_dim=128, page_size=
     (dict(n=-1), BAD), (dict(max_pages=0), BAD), (dict(head_dim=32), UNS), (dict(n_tokens=0), UNS),
     (dict(n_tokens=17), UNS), (dict(n_q_heads=9), UNS), (dict(n_q_heads=34), UNS),
     (dict(n_kv_heads=0), UNS), (dict(n_q_heads=0), UNS), (dict(page_size=32), UNS),
-    (dict(max_pages=1 << 28), UNS), (dict(n=1 << 22), UNS), (dict(num_pages=0), BAD),
+    (dict(max_pages=1 << 28), UNS), (dict(n=1 << 22), UNS), (dict(n=1 << 17, max_pages=2), UNS),
+    (dict(n=1 << 15, max_pages=(1 << 15) + 1), UNS), (dict(num_pages=0), BAD),
     (dict(scale=0.0), BAD), (dict(scale=float("nan")), BAD), (dict(clear_rest=2), BAD),
     (dict(q=0), BAD), (dict(kv_pool=F + 8), BAD), (dict(page_table=0), BAD), (dict(seq_lens=0), BAD),
     (dict(out=0), BAD), (dict(q_lens=F + 2), BAD), (dict(seq_lens=F + 1), BAD), (dict(workspace=0), BAD),
@@ -105,7 +106,7 @@ VERIFY = dict(n=4, n_drafts=3, vocab=1000, ld=1000, ld_draft=1000, temperature=1
     (dict(n=-1), BAD), (dict(vocab=0), BAD), (dict(n_drafts=-1), UNS), (dict(n_drafts=17), UNS),
     (dict(vocab=(1 << 24) + 1, ld=1 << 25, ld_draft=1 << 25), UNS), (dict(n=1 << 22), UNS),
     (dict(temperature=-1.0), BAD), (dict(temperature=float("nan")), BAD),
-    (dict(temperature=float("inf")), BAD), (dict(temperature=1e-40), UNS), (dict(ld=996), BAD),
+    (dict(temperature=float("inf")), BAD), (dict(temperature=1e-40), UNS), (dict(temperature=1e31), UNS), (dict(ld=996), BAD),
     (dict(ld=1002), BAD), (dict(ld_draft=996), BAD), (dict(ld_draft=1001), BAD), (dict(logits=0), BAD),
     (dict(logits=F + 4), BAD), (dict(draft_logits=F + 4), BAD), (dict(draft_tokens=0), BAD),
     (dict(uniforms=0), BAD), (dict(counts=F + 2), BAD), (dict(out_tokens=0), BAD),
