@@ -341,6 +341,10 @@ struct alignas(16) VerifyPart {  // of a row, or kVerifyChunk entries of it
   float max;    // the largest logit
   int32_t arg;  // its first index (temp 0)
 };
+struct alignas(16) VerifyDecided {  // of a candidate
+  VerifyPart row[2 * kVerifyMaxDrafts + 1];  // its rows' sums: targets 0 .. drafts, then the drafts' own
+  int taken, count;
+};
 struct VerifyArgs {
   int n, drafts, vocab, chunks;
   int64_t ld, ld_draft;  // row strides; candidate i's rows are (drafts + 1) i .. and drafts i ..
@@ -355,6 +359,7 @@ struct VerifyArgs {
   int32_t* out_accepted;
   VerifyPart* parts;  // [rows][chunks]
   double* rest_sum;   // [n][chunks]: of max(p - q, 0)
+  VerifyDecided* decided;  // [n]
 };
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t st);
 

@@ -1840,7 +1840,7 @@ sevo_status check_verify_shape(int n, int drafts, int vocab) {
 }
 
 struct VerifyLayout {
-  size_t parts, rest, total;
+  size_t parts, rest, decided, total;
 };
 VerifyLayout verify_layout(int n, int drafts, int vocab) {
   const size_t chunks = (vocab + sevo::kVerifyChunk - 1) / sevo::kVerifyChunk;
@@ -1848,7 +1848,8 @@ VerifyLayout verify_layout(int n, int drafts, int vocab) {
   VerifyLayout L;
   L.parts = 0;
   L.rest = round_up(parts * sizeof(sevo::VerifyPart), 256);
-  L.total = L.rest + round_up(n * chunks * sizeof(double), 256);
+  L.decided = L.rest + round_up(n * chunks * sizeof(double), 256);
+  L.total = L.decided + round_up(n * sizeof(sevo::VerifyDecided), 256);
   return L;
 }
 
@@ -1891,6 +1892,7 @@ SEVO_API sevo_status sevo_verify_drafts(const sevo_verify_args* a, void* stream)
   char* ws = static_cast<char*>(a->workspace);
   v.parts = reinterpret_cast<sevo::VerifyPart*>(ws + L.parts);
   v.rest_sum = reinterpret_cast<double*>(ws + L.rest);
+  v.decided = reinterpret_cast<sevo::VerifyDecided*>(ws + L.decided);
   hipError_t e = sevo::launch_verify(v, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SEVO_OK : hip_fail(e, "sevo_verify_drafts");
 }

@@ -8,14 +8,18 @@
 //
 // A choice is a comparison of sums over the whole vocabulary: one entry of 150 thousand differs
 // from its neighbour by 1e-6 of the mass and less, so a sum in 32 bits would move
-// choices.  Exponentials and sums are in 64 bits throughout (2^-50 relative each), which
-// the rows' reads cover: bound by HBM, then by the vector ALU.  Three kernels:
-//   1. per (row, 2048 entries): the largest logit and the sum of exponentials relative to it;
+// choices.  Exponentials and sums are in 64 bits throughout (3e-15 relative an entry at most).
+// Three kernels (us: 64 candidates with 4 drafts and their distributions, 151936 entries, 350 MB):
+//   1. per (row, 2048 entries): the largest logit and the sum of exponentials relative to it (64
+//      to 72; 49 without the exponentials, 51 are the floor of its reads: the vector ALU, 19
+//      operations an entry, does not hide under them altogether);
 //   2. (a draft distribution given) per (candidate, 2048 entries): the sum of max(p - q, 0) of the
-//      row where the candidate's drafts end;
-//   3. per candidate: the chunk that holds the drawn point, and in it the entry.
-// Kernels 2 and 3 find the number of accepted drafts from 1's sums, each workgroup for its
-// candidate.
+//      row where the candidate's drafts end (21 to 23: 5 to find it, then the vector ALU, 2
+//      exponentials an entry);
+//   3. per candidate: the chunk that holds the drawn point, and in it the entry (7: a chain of
+//      loads and scans).
+// Kernel 2, or 3 where there is none, finds the number of accepted drafts from 1's sums, each workgroup
+// for its candidate: a kernel of its own for it would cost a launch more.
 #include "common.h"
 #include "kernels.h"
 
@@ -120,37 +124,36 @@ __device__ __forceinline__ double log2_scale(const VerifyArgs& a) {
 }
 
 
-// The sums' exponential, factor * 2^(d c): factor * 2^(k / 32) from a table in LDS (its 32 entries are
-// 64 banks: no two lanes conflict), times a degree-5 polynomial on [-1/64, 1/64] (1.4e-16 relative),
-// scaled by 2^n in the table entry's exponent: 11 operations in 64 bits an entry, half of exp2d's.
+// The sums' exponential, factor * 2^(d c): factor * 2^(k / 64) from a table in LDS, times a degree-4
+// polynomial on [-1/128, 1/128] (2.4e-15 relative), scaled by 2^n in the table entry's exponent: 10
+// operations in 64 bits an entry, half of exp2d's.
 // d at most 0; what is more than 2^900 below 1, also a -inf (and a NaN), is taken for 2^-900
 // (a factor of 2^-24 at least then stays a normal number).
 struct ExpTable {
-  double t[32];
+  double t[64];
 };
 __device__ __forceinline__ void make_table(ExpTable& T, double factor) {
   const int j = threadIdx.x & 63;
-  if (j < 32) T.t[j] = factor * exp2d(j * (1.0 / 32.0));
+  T.t[j] = factor * exp2d(j * (1.0 / 64.0));
 }
 struct ExpScale {
-  double c32, least;
-  __device__ __forceinline__ explicit ExpScale(double c) : c32(32.0 * c), least(-900.0 / c) {}
+  double c64, least;
+  __device__ __forceinline__ explicit ExpScale(double c) : c64(64.0 * c), least(-900.0 / c) {}
 };
 __device__ __forceinline__ void exp_parts(const ExpTable& T, const ExpScale& E, double d, double& poly,
                                           double& entry) {
-  const double magic = 6755399441055744.0;  // 1.5 2^52: the sum's low bits are d c32 rounded
+  const double magic = 6755399441055744.0;  // 1.5 2^52: the sum's low bits are d c64 rounded
   d = __builtin_fmax(d, E.least);
-  const double t = __builtin_fma(d, E.c32, magic);
+  const double t = __builtin_fma(d, E.c64, magic);
   const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
-  const double r = __builtin_fma(d, E.c32, magic - t);
-  const uint64_t b = __builtin_bit_cast(uint64_t, T.t[k & 31]);
-  double y = 3.9737266313166245e-11;
-  y = __builtin_fma(y, r, 9.172616498159851e-09);
-  y = __builtin_fma(y, r, 1.6938509724215757e-06);
-  y = __builtin_fma(y, r, 0.0002345961981972034);
-  y = __builtin_fma(y, r, 0.02166084939249829);
+  const double r = __builtin_fma(d, E.c64, magic - t);
+  const uint64_t b = __builtin_bit_cast(uint64_t, T.t[k & 63]);
+  double y = 5.732858693358711e-10;
+  y = __builtin_fma(y, r, 2.1173175961253437e-07);
+  y = __builtin_fma(y, r, 5.864904955051792e-05);
+  y = __builtin_fma(y, r, 0.010830424696224892);
   poly = __builtin_fma(y, r, 1.0);
-  const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)(k >> 5) << 20);
+  const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)(k >> 6) << 20);
   entry = __builtin_bit_cast(double, (uint64_t)(uint32_t)b | ((uint64_t)hi << 32));
 }
 
@@ -231,10 +234,7 @@ using RowSum = VerifyPart;
 struct Decision {
   int taken, count;
 };
-struct VerifyLds {
-  RowSum row[2 * kVerifyMaxDrafts + 1];  // targets 0 .. drafts, then the drafts' own
-  int taken;
-};
+using VerifyLds = VerifyDecided;
 
 // over the 16 lanes of a row of the wave, every lane gets it
 __device__ __forceinline__ float row16_max(float v) {
@@ -245,17 +245,20 @@ __device__ __forceinline__ float row16_max(float v) {
 }
 
 // 16 lanes: the row's partials joined, every lane gets the result
-__device__ __forceinline__ RowSum join_row(const VerifyArgs& a, size_t row) {
+constexpr int kPartsAhead = 5;  // partials of a lane in flight: 80 chunks, 163840 entries
+__device__ __forceinline__ void load_parts(const VerifyArgs& a, size_t row, VerifyPart (&v)[kPartsAhead]) {
+  const VerifyPart* p = a.parts + row * a.chunks;
+#pragma unroll
+  for (int u = 0; u < kPartsAhead; ++u) v[u] = p[min((int)(threadIdx.x & 15) + 16 * u, a.chunks - 1)];
+}
+__device__ __forceinline__ RowSum join_row(const VerifyArgs& a, size_t row,
+                                           const VerifyPart (&v)[kPartsAhead]) {
   const int q = threadIdx.x & 15;
   const VerifyPart* p = a.parts + row * a.chunks;
-  constexpr int U = 5;  // partials of a lane in flight: 80 chunks, 163840 entries
-  VerifyPart v[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) v[u] = p[min(q + 16 * u, a.chunks - 1)];
   float m = -INFINITY;
 #pragma unroll
-  for (int u = 0; u < U; ++u) m = fmaxf(m, v[u].max);
-  for (int k = q + 16 * U; k < a.chunks; k += 16) m = fmaxf(m, p[k].max);
+  for (int u = 0; u < kPartsAhead; ++u) m = fmaxf(m, v[u].max);
+  for (int k = q + 16 * kPartsAhead; k < a.chunks; k += 16) m = fmaxf(m, p[k].max);
   m = row16_max(m);
   const double mc = m == -INFINITY ? 0.0 : (double)m, c = log2_scale(a);
   double s = 0.0;
@@ -265,9 +268,9 @@ __device__ __forceinline__ RowSum join_row(const VerifyArgs& a, size_t row) {
     if (x.max == m) arg = min(arg, x.arg);
   };
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+  for (int u = 0; u < kPartsAhead; ++u)
     if (q + 16 * u < a.chunks) add(v[u]);
-  for (int k = q + 16 * U; k < a.chunks; k += 16) add(p[k]);
+  for (int k = q + 16 * kPartsAhead; k < a.chunks; k += 16) add(p[k]);
   s = row16_sum64(s);
   arg = min(arg, lane_xor<1>(arg));
   arg = min(arg, lane_xor<2>(arg));
@@ -284,45 +287,53 @@ __device__ __forceinline__ double prob(const VerifyArgs& a, const RowSum& r, flo
 }
 
 // The sums of candidate i's rows into LDS, and how many drafts are accepted.  All threads: 16 lanes
-// a row, so that a call with 4 drafts takes two memory latencies.
+// a row, so that a call with 4 drafts takes two memory latencies: the partials beside the count, the
+// drafts and their uniform numbers; then the drafts' logits.
 __device__ __forceinline__ Decision decide(const VerifyArgs& a, int i, VerifyLds& L) {
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const bool dist = a.draft_logits && a.temp != 0.0;
   const int rows = a.drafts + 1 + (dist ? a.drafts : 0);
-  // (rows behind the last draft are joined too, and not looked at: the count is read beside them)
-  const int count = drafts_of(a, i);
-  const bool mine = w == 0 && lane < count;
   int x = -1;
-  double u = 0.0;
-  float zx = 0.f, yx = 0.f;
-  if (mine) {
+  float u = 0.f;
+  if (w == 0 && lane < a.drafts) {
     x = a.draft_tokens[(size_t)i * a.drafts + lane];
     u = a.uniforms[(size_t)i * (a.drafts + 1) + lane];
-    if (x >= 0 && x < a.vocab) {
-      zx = row_ptr(a, target_row(a, i, lane))[x];
-      if (dist) yx = row_ptr(a, draft_row(a, i, lane))[x];
-    }
   }
-  for (int r0 = 0; r0 < rows; r0 += 16) {
-    const int r = r0 + (threadIdx.x >> 4);
-    if (r < rows) {
-      const RowSum s = join_row(a, r <= a.drafts ? target_row(a, i, r) : draft_row(a, i, r - a.drafts - 1));
-      if ((lane & 15) == 0) L.row[r <= a.drafts ? r : kVerifyMaxDrafts + r - a.drafts] = s;
-    }
+  // (rows behind the last draft are joined too, and not looked at)
+  const int count = drafts_of(a, i);
+  auto row_of = [&](int r) {
+    return r <= a.drafts ? target_row(a, i, r) : draft_row(a, i, r - a.drafts - 1);
+  };
+  int r = threadIdx.x >> 4;
+  VerifyPart v[kPartsAhead];
+  if (r < rows) load_parts(a, row_of(r), v);
+  float zx = 0.f, yx = 0.f;
+  const bool known = x >= 0 && x < a.vocab;
+  if (known) {
+    zx = row_ptr(a, target_row(a, i, lane))[x];
+    if (dist) yx = row_ptr(a, draft_row(a, i, lane))[x];
+  }
+  for (; r < rows; r += 16) {
+    if (r >= 16) load_parts(a, row_of(r), v);
+    const RowSum s = join_row(a, row_of(r), v);
+    if ((lane & 15) == 0) L.row[r <= a.drafts ? r : kVerifyMaxDrafts + r - a.drafts] = s;
   }
   __syncthreads();
   if (w == 0) {
     bool ok = true;
-    if (mine) {
-      const RowSum r = L.row[lane];
+    if (lane < count) {
+      const RowSum t = L.row[lane];
       ok = false;
-      if (x >= 0 && x < a.vocab && fine(r.sum))
-        ok = a.temp == 0.0
-                 ? x == r.arg
-                 : u * (dist ? prob(a, L.row[kVerifyMaxDrafts + 1 + lane], yx) : 1.0) < prob(a, r, zx);
+      if (known && fine(t.sum))
+        ok = a.temp == 0.0 ? x == t.arg
+                           : (double)u * (dist ? prob(a, L.row[kVerifyMaxDrafts + 1 + lane], yx) : 1.0) <
+                                 prob(a, t, zx);
     }
     const uint64_t bad = __builtin_amdgcn_ballot_w64(!ok);
-    if (lane == 0) L.taken = bad ? min(count, (int)__builtin_ctzll(bad)) : count;
+    if (lane == 0) {
+      L.taken = bad ? min(count, (int)__builtin_ctzll(bad)) : count;
+      L.count = count;
+    }
   }
   __syncthreads();
   return Decision{L.taken, count};
@@ -411,6 +422,11 @@ __global__ __launch_bounds__(256, 4) void verify_rest_kernel(VerifyArgs a) {
   const int i = blockIdx.x / groups;
   const int chunk = (blockIdx.x - i * groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Decision d = decide(a, i, L);
+  if (blockIdx.x == (unsigned)(i * groups)) {  // for the third kernel
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(&L);
+    uint32_t* to = reinterpret_cast<uint32_t*>(a.decided + i);
+    if (threadIdx.x < sizeof(VerifyLds) / 4) to[threadIdx.x] = from[threadIdx.x];
+  }
   if (d.taken == d.count) return;
   const RowSum t = L.row[d.taken], q = L.row[kVerifyMaxDrafts + 1 + d.taken];
   const float* tr = row_ptr(a, target_row(a, i, d.taken));
@@ -456,6 +472,8 @@ __global__ __launch_bounds__(256, 4) void verify_rest_kernel(VerifyArgs a) {
   if ((threadIdx.x & 63) == 0) a.rest_sum[(size_t)i * a.chunks + chunk] = s;
 }
 
+// DECIDED: the second kernel ran, and left what decide() finds
+template <bool DECIDED>
 __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
   __shared__ VerifyLds L;
   __shared__ double red[4], s_pre[4];
@@ -464,7 +482,16 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
   const int i = blockIdx.x;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const double point = a.uniforms[(size_t)i * (a.drafts + 1) + a.drafts];
-  const Decision d = decide(a, i, L);
+  Decision d;
+  if constexpr (DECIDED) {
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(a.decided + i);
+    uint32_t* to = reinterpret_cast<uint32_t*>(&L);
+    if (threadIdx.x < sizeof(VerifyLds) / 4) to[threadIdx.x] = from[threadIdx.x];
+    __syncthreads();
+    d = Decision{L.taken, L.count};
+  } else {
+    d = decide(a, i, L);
+  }
   const RowSum row = L.row[d.taken];
   const bool valid = fine(row.sum);
   if (threadIdx.x == 0) {
@@ -612,8 +639,10 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t st) {
                        0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(verify_pick_kernel<true>, dim3((unsigned)a.n), dim3(256), 0, st, a);
+  } else {
+    hipLaunchKernelGGL(verify_pick_kernel<false>, dim3((unsigned)a.n), dim3(256), 0, st, a);
   }
-  hipLaunchKernelGGL(verify_pick_kernel, dim3((unsigned)a.n), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
