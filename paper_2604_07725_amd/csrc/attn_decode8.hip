@@ -569,7 +569,7 @@ static hipError_t launch_attn8_d(const Attn8Args& a, int nc, hipStream_t st) {
   else go(attn8_split_kernel<D, 4, 1>);
   hipError_t e = hipGetLastError();
   // pages that one split holds: every candidate has one, nothing to join
-  if (e != hipSuccess || a.max_pages <= kAttn8OneSplit) return e;
+  if (e != hipSuccess || a.max_pages <= a.min_chunk) return e;
   const unsigned cols = (unsigned)(a.tokens * a.group);
   auto join = [&](auto kern, unsigned groups) {
     hipLaunchKernelGGL(kern, dim3(groups, (unsigned)a.hkv, (unsigned)a.n), dim3(256), 0, st, a);
@@ -590,8 +590,11 @@ Attn8Plan plan_attn8(int n, int hq, int hkv, int d, int tokens, int max_pages) {
   // all pages / chunk + n splits at most
   p.one_round = std::max(std::max(places - n, places / 2), 1);
   p.rounds = std::max(kAttn8Rounds * 256 / per, 1);
-  // a join costs 5 us: short candidates are one split
-  p.min_chunk = max_pages <= kAttn8OneSplit ? kAttn8OneSplit : kAttn8MinChunk;
+  // A join costs 5 us of the GPU and a launch: short candidates are one split, longer ones too where
+  // they fill the CUs (splits / one, us among others: 4 candidates of 512-1024 keys, 8 heads, 13.8 /
+  // 12.0, of 768-1536 13.4 / 16.2; 64 of 1280-2560 53 / 46, 64 of 256-4096 with 4 heads 33 / 39).
+  const bool one = max_pages <= ((long long)n * per >= 256 ? kAttn8OneSplitMany : kAttn8OneSplit);
+  p.min_chunk = one ? max_pages : kAttn8MinChunk;
   const long long most = (long long)n * ((max_pages + p.min_chunk - 1) / p.min_chunk);
   const long long s = (long long)std::max(p.one_round, p.rounds) + n;
   p.max_splits = s < most ? s : most;

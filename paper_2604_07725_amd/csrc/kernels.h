@@ -303,7 +303,9 @@ hipError_t launch_pack_kv8(const KvPagesArgs& a, int to8, hipStream_t st);
 
 // ---- attn_decode8.hip
 constexpr int kAttn8MinChunk = 16;   // pages of a split, at least (but for a candidate's only one)
-constexpr int kAttn8OneSplit = 32;   // page tables up to this width: one split a candidate
+// page tables up to this width: one split a candidate, and no join; the second where the candidates
+// alone are a workgroup per CU
+constexpr int kAttn8OneSplit = 64, kAttn8OneSplitMany = 160;
 constexpr int kAttn8LongChunk = 192;  // beyond, several rounds of workgroups
 constexpr int kAttn8Rounds = 8;       // workgroups per CU that those aim at
 constexpr int kAttn8MaxTiles = 4;       // column tiles of a workgroup
@@ -311,7 +313,7 @@ struct Attn8Plan {
   int nc, col_tiles;  // column tiles of 16 query rows per workgroup; workgroups per kv head and split
   int one_round;      // splits aimed at, over all candidates: all resident at once
   int rounds;         // in several rounds
-  int min_chunk;      // pages of a split, at least
+  int min_chunk;      // pages of a split, at least; max_pages: every candidate has one
   long long max_splits;
 };
 Attn8Plan plan_attn8(int n, int hq, int hkv, int d, int tokens, int max_pages);

@@ -1729,7 +1729,7 @@ struct Attn8Layout {
 };
 Attn8Layout attn8_layout(int hq, int tokens, int d, int max_pages, const sevo::Attn8Plan& p) {
   Attn8Layout L{0, 0, 0};
-  if (max_pages <= sevo::kAttn8OneSplit) return L;  // one split a candidate: no partials
+  if (max_pages <= p.min_chunk) return L;  // one split a candidate: no partials
   const size_t rows = (size_t)p.max_splits * hq * tokens;
   L.acc = round_up(rows * 2 * sizeof(float), 256);
   L.total = L.acc + round_up(rows * d * sizeof(float), 256);

@@ -283,7 +283,12 @@ def check_attention(sevo, pool, table, lens, q, m=None, **kw):
 def test_attention(sevo, hq, hkv, d, T):
     lens = [T, 16, T + 15, 33, 47, 300, 700]
     pool, table, g = cache(lens, hkv, d, seed=hq + T)
-    check_attention(sevo, pool, table, lens, torch.randn(len(lens), T, hq, d, generator=g).to(BF))
+    q = torch.randn(len(lens), T, hq, d, generator=g).to(BF)
+    check_attention(sevo, pool, table, lens, q)
+    # a page table that may hold long contexts: candidates in several splits
+    wide = torch.full((len(lens), 300), -1, dtype=torch.int32)
+    wide[:, :table.shape[1]] = table
+    check_attention(sevo, pool, wide, lens, q)
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -328,14 +333,20 @@ def test_attention_many_candidates(sevo):
     lens = [int(x) for x in torch.randint(0, 40, (300,), generator=g)]
     lens[257] = 900
     pool, table, g = cache(lens, 1, 64, seed=9)
-    check_attention(sevo, pool, table, lens, torch.randn(300, 1, 2, 64, generator=g).to(BF))
+    q = torch.randn(300, 1, 2, 64, generator=g).to(BF)
+    o = check_attention(sevo, pool, table, lens, q)
+    # a wider page table: splits, and their join
+    wide = torch.full((300, 200), -1, dtype=torch.int32)
+    wide[:, :table.shape[1]] = table
+    far = check_attention(sevo, pool, wide, lens, q)
+    assert (far.float() - o.float()).abs().max() <= 2.0 ** -6 * o.abs().max()
 
 
 @pytest.mark.parametrize("d,T", [(64, 1), (128, 1), (128, 4)])
 def test_attention_garbage_and_bad_pages(sevo, d, T):
     """What lies behind the last key, or in pages outside the pool, does not enter."""
     lens = [T + 5, 37, 64, 600]
-    pool, table, g = cache(lens, 2, d, seed=d)
+    pool, table, g = cache(lens, 2, d, seed=d, max_pages=100 if T > 1 else None)
     q = torch.randn(4, T, 8, d, generator=g).to(BF)
     table[3, 4], table[3, 20], table[2, 1] = 10 ** 6, -7, pool.shape[0]
     clean = check_attention(sevo, pool, table, lens, q)
