@@ -859,8 +859,9 @@ size_t sevo_attn_fp8_workspace_bytes(int32_t n, int32_t n_tokens, int32_t n_q_he
  *   out_logprobs fp32 [n][n_drafts + 1]: log p_t of each emitted token, then 0
  *   out_accepted int32 [n]: a_i (a_i + 1 tokens are emitted)
  * n_drafts 0..16 (0: draft_tokens may be NULL); ld, ld_draft multiples of 4, at least
- * vocab; vocab up to 2^24; temperature 0 or 1e-30..1e30; n (2 n_drafts + 1) vocab below about 2^34.  The workspace is scratch of sevo_verify_workspace_bytes; calls
- * that may overlap in time each need their own.  Errors: INVALID_ARGUMENT, UNSUPPORTED,
+ * vocab; vocab up to 2^24; temperature 0 or 1e-30..1e30; n (2 n_drafts + 1) vocab below
+ * about 2^34.  The workspace is scratch of sevo_verify_workspace_bytes; calls that may
+ * overlap in time each need their own.  Errors: INVALID_ARGUMENT, UNSUPPORTED,
  * WORKSPACE_TOO_SMALL, HIP. */
 typedef struct {
   int32_t n, n_drafts, vocab;

@@ -23,9 +23,9 @@
 //
 // What bounds it: HBM for one token a candidate (16 flop a byte at 8 heads a kv head).  64
 // candidates of 16k-32k keys, 8 x 128 heads, 3.32 GB: 512-528 us, 6.3-6.5 TB/s, what the read probe
-// reaches; one candidate of 65537 keys, 138 MB: 32 us, of them 20 in the loop, the rest
+// reaches; one candidate of 65537 keys, 138 MB: 30 us, of them 18 in the loop, the rest
 // the two launches, the way to the first page (lengths, page ids, page: three memory latencies) and
-// the join.  With 40 query rows (5 tokens of 8 heads; 16 candidates of 8k-16k keys, 209 MB, 52 us) the
+// the join.  With 40 query rows (5 tokens of 8 heads; 16 candidates of 8k-16k keys, 209 MB, 49 us) the
 // loop is bound by instructions: a wave issues one vector instruction in 8 clocks, and registers
 // leave two waves a SIMD.
 #include <algorithm>
@@ -66,7 +66,7 @@ __device__ __forceinline__ int pages_of(int keys) { return (keys + kPage - 1) / 
 // The split plan, the same in every wave of both kernels: candidate i has max(1, ceil(pages_i /
 // chunk)) splits.  The chunk is the least that gives all workgroups a place at once (then
 // nothing waits for a second round that would be part empty: one candidate of 65537 keys 35 us
-// against 42 for 3 rounds); where that leaves chunks of more than kAttn8LongChunk pages, whose
+// against 42 for 3 rounds, with an earlier loop; 30 now); where that leaves chunks of more than kAttn8LongChunk pages, whose
 // ends would be ragged, several rounds of shorter ones (64 candidates of 16k-32k: 8 workgroups per
 // CU 515 us, 4 526, 2 575).
 struct Split {

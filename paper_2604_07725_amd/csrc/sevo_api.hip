@@ -1746,7 +1746,7 @@ SEVO_API sevo_status sevo_qk_norm_rope_append_fp8(const sevo_model* m, int32_t l
                                                   void* q_out, void* kv_pool, void* stream) {
   if (!m) return fail(SEVO_ERR_INVALID_ARGUMENT, "null model");
   if (layer < 0 || layer >= m->cfg.n_layers) return fail(SEVO_ERR_INVALID_ARGUMENT, "bad layer");
-  if (n < 0 || n_rows < 1 || max_pages < 1 || num_pages < 1 || (!rows && n_rows < n))
+  if (n < 0 || n_rows < (n > 0 ? 1 : 0) || max_pages < 1 || num_pages < 1 || (!rows && n_rows < n))
     return fail(SEVO_ERR_INVALID_ARGUMENT, "n %d, n_rows %d, max_pages %d, num_pages %lld", n,
                 n_rows, max_pages, (long long)num_pages);
   // (a launch holds fewer than 2^32 threads)

@@ -153,6 +153,18 @@ def test_append_leaves_out_what_has_no_place(sevo):
     m.close()
 
 
+@pytest.mark.parametrize("rows", [False, True])
+def test_append_of_no_tokens(sevo, rows):
+    m = model(sevo, 4, 2, 64, max_position=60)
+    ids = torch.empty(0, dtype=torch.int32, device=DEV)
+    table = torch.zeros(2 if rows else 0, 3, dtype=torch.int32, device=DEV)
+    pool = torch.full((3, 2, 32 * 64 + 128), 0x11, dtype=torch.uint8, device=DEV)
+    q = sevo.sevo_qk_norm_rope_append_fp8(m, 0, torch.empty(0, 8 * 64, device=DEV), ids, table, pool,
+                                          rows=ids if rows else None)
+    assert q.shape == (0, 4, 64) and (pool == 0x11).all()
+    m.close()
+
+
 def test_append_nan_infinity_and_zeros(sevo):
     hq, hkv, d = 4, 2, 128
     m = model(sevo, hq, hkv, d, qk_norm=False)
