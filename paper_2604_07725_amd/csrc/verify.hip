@@ -10,11 +10,11 @@
 // from its neighbour by 1e-6 of the mass and less, so a sum in 32 bits would move
 // choices.  Exponentials and sums are in 64 bits throughout (3e-15 relative an entry at most).
 // Three kernels (us: 64 candidates with 4 drafts and their distributions, 151936 entries, 350 MB):
-//   1. per (row, 2048 entries): the largest logit and the sum of exponentials relative to it (64
-//      to 72; 49 without the exponentials, 51 are the floor of its reads: the vector ALU, 19
-//      operations an entry, does not hide under them altogether);
+//   1. per (row, 2048 entries): the largest logit and the sum of exponentials relative to it (57
+//      to 64; 51 are the floor of its reads: the vector ALU, 14 operations an entry and 5 for the
+//      chunk's sums, is busy most of the time);
 //   2. (a draft distribution given) per (candidate, 2048 entries): the sum of max(p - q, 0) of the
-//      row where the candidate's drafts end (21 to 23: 5 to find it, then the vector ALU, 2
+//      row where the candidate's drafts end (20 to 24: 5 to find it, then the vector ALU, 2
 //      exponentials an entry);
 //   3. per candidate: the chunk that holds the drawn point, and in it the entry (7: a chain of
 //      loads and scans).
@@ -124,37 +124,51 @@ __device__ __forceinline__ double log2_scale(const VerifyArgs& a) {
 }
 
 
-// The sums' exponential, factor * 2^(d c): factor * 2^(k / 64) from a table in LDS, times a degree-4
-// polynomial on [-1/128, 1/128] (2.4e-15 relative), scaled by 2^n in the table entry's exponent: 10
-// operations in 64 bits an entry, half of exp2d's.
+// The sums' exponential, factor * 2^(d c): factor * 2^(k / 256) from a table in LDS, times a degree-4
+// polynomial on [-1/512, 1/512] (5e-18 relative), scaled by 2^n in the table entry's exponent.
+// 256 entries make the index one instruction (a byte's shift): 64 candidates 97 -> 95 us.
 // d at most 0; what is more than 2^900 below 1, also a -inf (and a NaN), is taken for 2^-900
 // (a factor of 2^-24 at least then stays a normal number).
-struct ExpTable {
-  double t[64];
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+struct Exp2Steps {  // 2^(j / 256), from exp's series
+  double v[256];
+  constexpr Exp2Steps() : v() {
+    for (int j = 0; j < 256; ++j) {
+      const double x = j * (0.69314718055994530942 / 256);
+      double y = 1.0;
+      for (int n = 20; n > 0; --n) y = 1.0 + y * x / n;
+      v[j] = y;
+    }
+  }
 };
-__device__ __forceinline__ void make_table(ExpTable& T, double factor) {
-  const int j = threadIdx.x & 63;
-  T.t[j] = factor * exp2d(j * (1.0 / 64.0));
+__device__ const Exp2Steps kExp2Steps{};
+struct ExpTable {
+  u32x2 t[256];  // the exponent of entry j less j / 256: adding k / 256 to it gives n
+};
+__device__ __forceinline__ void make_table(ExpTable& T, double step, double factor) {
+  u32x2 b = __builtin_bit_cast(u32x2, factor * step);
+  b.y -= threadIdx.x << 12;
+  T.t[threadIdx.x] = b;
 }
 struct ExpScale {
-  double c64, least;
-  __device__ __forceinline__ explicit ExpScale(double c) : c64(64.0 * c), least(-900.0 / c) {}
+  double c256, least;
+  __device__ __forceinline__ explicit ExpScale(double c) : c256(256.0 * c), least(-900.0 / c) {}
 };
 __device__ __forceinline__ void exp_parts(const ExpTable& T, const ExpScale& E, double d, double& poly,
                                           double& entry) {
-  const double magic = 6755399441055744.0;  // 1.5 2^52: the sum's low bits are d c64 rounded
+  const double magic = 6755399441055744.0;  // 1.5 2^52: the sum's low bits are d c256 rounded
   d = __builtin_fmax(d, E.least);
-  const double t = __builtin_fma(d, E.c64, magic);
+  const double t = __builtin_fma(d, E.c256, magic);
   const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
-  const double r = __builtin_fma(d, E.c64, magic - t);
-  const uint64_t b = __builtin_bit_cast(uint64_t, T.t[k & 63]);
-  double y = 5.732858693358711e-10;
-  y = __builtin_fma(y, r, 2.1173175961253437e-07);
-  y = __builtin_fma(y, r, 5.864904955051792e-05);
-  y = __builtin_fma(y, r, 0.010830424696224892);
+  const double r = __builtin_fma(d, E.c256, magic - t);
+  u32x2 b = T.t[(uint8_t)k];
+  double y = 2.239395329901621e-12;
+  y = __builtin_fma(y, r, 3.30830298371135e-09);
+  y = __builtin_fma(y, r, 3.665565596910101e-06);
+  y = __builtin_fma(y, r, 0.0027076061740622767);
   poly = __builtin_fma(y, r, 1.0);
-  const uint32_t hi = (uint32_t)(b >> 32) + ((uint32_t)(k >> 6) << 20);
-  entry = __builtin_bit_cast(double, (uint64_t)(uint32_t)b | ((uint64_t)hi << 32));
+  b.y += (uint32_t)k << 12;
+  entry = __builtin_bit_cast(double, b);
 }
 
 }  // namespace
@@ -177,6 +191,7 @@ __global__ __launch_bounds__(256, 6) void verify_rows_kernel(VerifyArgs a) {
     const int i = (int)(own / each);
     on = (int)(own - i * each) < drafts_of(a, i) + (row < targets ? 1 : 0);
   }
+  const double step = kExp2Steps.v[threadIdx.x];
   f32x4 z[J];
   if (on) {
     const float* r = row_ptr(a, row);
@@ -190,7 +205,7 @@ __global__ __launch_bounds__(256, 6) void verify_rows_kernel(VerifyArgs a) {
       for (int j = 0; j < J; ++j) z[j] = row4(r, v0 + 256 * j, a.vocab);
     }
   }
-  if (threadIdx.x < 64) make_table(T, 1.0);
+  make_table(T, step, 1.0);
   __syncthreads();
   if (!on) return;
   float m = -INFINITY;
@@ -200,16 +215,16 @@ __global__ __launch_bounds__(256, 6) void verify_rows_kernel(VerifyArgs a) {
   const ExpScale E(log2_scale(a));
   const double md = m;
   double sum = 0.0;
-  bool none = false;  // a NaN or a +inf: no distribution
+  bool none = m == INFINITY;  // a NaN or a +inf: no distribution
 #pragma unroll
   for (int j = 0; j < J; ++j) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      none |= !(z[j][k] <= 3.402823466e38f);
       double y, e;
       exp_parts(T, E, (double)z[j][k] - md, y, e);
       sum = __builtin_fma(y, e, sum);
     }
+    none |= __builtin_isunordered(z[j].x, z[j].y) | __builtin_isunordered(z[j].z, z[j].w);
     __builtin_amdgcn_sched_barrier(0);  // (four at a time: all at once take twice the registers)
   }
   if (m == -INFINITY) sum = 0.0;
@@ -421,6 +436,7 @@ __global__ __launch_bounds__(256, 4) void verify_rest_kernel(VerifyArgs a) {
   const int groups = (a.chunks + 3) / 4;
   const int i = blockIdx.x / groups;
   const int chunk = (blockIdx.x - i * groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const double step = kExp2Steps.v[threadIdx.x];
   const Decision d = decide(a, i, L);
   if (blockIdx.x == (unsigned)(i * groups)) {  // for the third kernel
     const uint32_t* from = reinterpret_cast<const uint32_t*>(&L);
@@ -447,8 +463,8 @@ __global__ __launch_bounds__(256, 4) void verify_rest_kernel(VerifyArgs a) {
       y[j] = row4(dr, v0 + 256 * j, a.vocab);
     }
   }
-  if (threadIdx.x < 64) make_table(P, 1.0 / t.sum);
-  else if (threadIdx.x < 128) make_table(Q, 1.0 / q.sum);
+  make_table(P, step, 1.0 / t.sum);
+  make_table(Q, step, 1.0 / q.sum);
   __syncthreads();
   if (chunk >= a.chunks) return;
   const ExpScale E(log2_scale(a));
