@@ -137,8 +137,11 @@ __device__ __forceinline__ int token_of(const Attn8Args& a, int cc) {
 // running maxima start here: finite, so that what a column has not seen needs no case of its own
 constexpr float kNoScore = -3e38f;
 
-// waves per SIMD that the registers of NC column tiles leave room for
-constexpr int waves8(int d, int nc) { return nc == 1 || (nc == 2 && d == 64) ? 3 : 2; }
+// Waves per SIMD that the registers of NC column tiles leave room for.  At d = 128 two tiles fit three
+// times with q in LDS and one tile's probabilities at a time (16 candidates of 8k-16k keys, 5 tokens of 32
+// heads on 8: 94 -> 82 us; a second pair of pages in registers instead: 93); three tiles of d = 64
+// as they are (32 candidates, 5 tokens of 32 heads on 4: 63 -> 58.5).
+constexpr int waves8(int d, int nc) { return nc <= 2 || (nc == 3 && d == 64) ? 3 : 2; }
 
 }  // namespace
 
@@ -192,8 +195,8 @@ __global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Ar
   m = m < 0 ? 0 : (m > a.tokens ? a.tokens : m);
 
   // The query rows' fragments, dims 64 x + 16 grp + 8 h .. + 7 of the lane's column: in registers,
-  // or from three column tiles on, where those are short, in LDS, once for the four waves.
-  constexpr bool kQLds = NC >= 3;
+  // or where those are short in LDS, once for the four waves.
+  constexpr bool kQLds = NC >= 3 || (NC == 2 && D == 128);
   __shared__ __align__(16) u32x4 q_lds[kQLds ? NC * NA * 2 : 1][64];
   bf16x8v qf[kQLds ? 1 : NC][NA][2];
   int lim[NC];  // keys that the lane's column sees
@@ -326,9 +329,9 @@ __global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Ar
       }
     }
     load_k(r, n + PF);
-    // four column tiles go in two halves, V's codes converted for each: the probabilities of all
-    // four take registers that are not there
-    constexpr int H = NC == 4 ? 2 : NC;
+    // four column tiles go in two halves, two of d = 128 one by one, V's codes converted for each: the
+    // probabilities of all take registers that are not there
+    constexpr int H = NC == 4 ? 2 : (NC == 2 && D == 128 ? 1 : NC);
 #pragma unroll
     for (int t0 = 0; t0 < NC; t0 += H) {
       bf16x8v ph[H], pl[H];
@@ -346,10 +349,10 @@ __global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Ar
           }
         }
         float top = max3(max3(max3(z[0], z[1], z[2]), z[3], z[4]), max3(z[5], z[6], z[7]), z[7]);
-        top = xor32_max(xor16_max(top));
-        const bool raise = top > m_run[t] + kLazyLog2;
-        if (__builtin_amdgcn_ballot_w64(raise)) {
-          const float mn = raise ? top : m_run[t];
+        // (the column's largest is in one of its four lanes, and looked for only where one is too large)
+        if (__builtin_amdgcn_ballot_w64(top > m_run[t] + kLazyLog2)) {
+          top = xor32_max(xor16_max(top));
+          const float mn = top > m_run[t] + kLazyLog2 ? top : m_run[t];
           const float alpha = __builtin_amdgcn_exp2f(m_run[t] - mn);  // 0 on the first page, 1 without a raise
           l_run[t] *= alpha;
 #pragma unroll
@@ -368,6 +371,7 @@ __global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Ar
           }
           hi[e / 2] = pack_bf16x2(p[0], p[1]);
           asm("" : "+v"(hi[e / 2]));  // (else it is converted once more for what follows)
+          // p less its rounded value, exact, as a dot product with (-1, 0) and (0, -1)
           lo[e / 2] = pack_bf16x2(p[0] - bf16_lo(hi[e / 2]), p[1] - bf16_hi(hi[e / 2]));
         }
         ph[t - t0] = __builtin_bit_cast(bf16x8v, u32x4{hi[0], hi[1], hi[2], hi[3]});
