@@ -25,7 +25,7 @@
 // candidates of 16k-32k keys, 8 x 128 heads, 3.32 GB: 512-528 us, 6.3-6.5 TB/s, what the read probe
 // reaches; one candidate of 65537 keys, 138 MB: 30 us, of them 18 in the loop, the rest
 // the two launches, the way to the first page (lengths, page ids, page: three memory latencies) and
-// the join.  With 40 query rows (5 tokens of 8 heads; 16 candidates of 8k-16k keys, 209 MB, 49 us) the
+// the join.  With 40 query rows (5 tokens of 8 heads; 16 candidates of 8k-16k keys, 209 MB, 48 us) the
 // loop is bound by instructions: a wave issues one vector instruction in 8 clocks, and registers
 // leave two waves a SIMD.
 #include <algorithm>
