@@ -10,7 +10,7 @@
 //
 // Work: the pages of all candidates are cut into splits of about equal size, found on the
 // device from the lengths alone (a candidate with few pages gets one split, whatever the page table's
-// width), one 256-thread workgroup per (kv head, split).  Its waves take pairs of pages in
+// width), one workgroup of four or eight waves per (kv head, split).  Its waves take pairs of pages in
 // turn, each with its own running maximum and sum, and meet in LDS at the end; a second
 // kernel joins the splits of a candidate in order.  Per pair of pages and wave:
 //   QK   S = K Q^T, 16x16x32 matrix instructions: rows = the page's tokens, columns = 16 query
@@ -145,13 +145,13 @@ constexpr int waves8(int d, int nc) { return nc <= 2 || (nc == 3 && d == 64) ? 3
 
 }  // namespace
 
-template <int D, int NC, int PF>
-__global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Args a) {
+template <int D, int NC, int PF, int W>
+__global__ __launch_bounds__(64 * W, W == 4 ? waves8(D, NC) : 2) void attn8_split_kernel(Attn8Args a) {
   constexpr int NA = D / 64;   // 64-dim blocks of a tile
   constexpr int NB = D / 16;   // 16-dim blocks of the output
   constexpr int kStride = D + 4;
-  __shared__ float w_m[4][16], w_l[4][16];
-  __shared__ __align__(16) float w_acc[4][16][kStride];
+  __shared__ float w_m[W][16], w_l[W][16];
+  __shared__ __align__(16) float w_acc[W][16][kStride];
 
   // workgroups in the order (split, kv head, NC column tiles): the heads of a page, adjacent in
   // the pool, are read together, each through the XCD that its workgroup number falls to
@@ -175,11 +175,11 @@ __global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Ar
 
   const int32_t* ptr = a.page_table + (size_t)i * a.max_pages;
   const int pairs = (pend - pbeg + 1) / 2;                 // pairs of the split
-  const int mine = pairs > wave ? (pairs - wave + 3) / 4 : 0;  // the wave's: wave, wave + 4, ...
+  const int mine = pairs > wave ? (pairs - wave + W - 1) / W : 0;  // the wave's: wave, wave + W, ...
   // page ids of 64 of the wave's pairs, one pair per lane; -1: outside the pool
   int id0 = -1, id1 = -1;
   auto fetch_ids = [&](int k0) {
-    const int pg = pbeg + 2 * (wave + 4 * (k0 + lane));
+    const int pg = pbeg + 2 * (wave + W * (k0 + lane));
     id0 = id1 = -1;
     if (k0 + lane < mine) {
       const int x = ptr[pg];
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Ar
     }
   };
   auto step = [&](Pair& r, int n) {
-    const int pg = pbeg + 2 * (wave + 4 * n);  // the pair's first page
+    const int pg = pbeg + 2 * (wave + W * n);  // the pair's first page
     const bool ok0 = r.id[0] >= 0, ok1 = r.id[1] >= 0;
     const bool masked = pg + 2 > full || !ok0 || !ok1;
     const int u0 = pg * kPage + 4 * grp;  // the lane's tokens u0 .. + 3 and u0 + 16 .. + 3
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Ar
     }
   }
 
-  // The four waves of each column tile joined, in order: 16 threads a column, D / 16 dims each.
+  // The waves of each column tile joined, in order: 16 threads a column, D / 16 dims each.
   // A candidate's only split is the result.
   constexpr int E = D / 16;
   const int j = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * E;
@@ -426,13 +426,15 @@ __global__ __launch_bounds__(256, waves8(D, NC)) void attn8_split_kernel(Attn8Ar
       *reinterpret_cast<f32x4*>(&w_acc[wave][col][16 * b + 4 * grp]) = acc[t][b];
     __syncthreads();
     const int cc = (cg * NC + t) * 16 + j;
-    if (cc < cols) {
-      const float M = fmaxf(fmaxf(w_m[0][j], w_m[1][j]), fmaxf(w_m[2][j], w_m[3][j]));
+    if (j < 16 && cc < cols) {
+      float M = w_m[0][j];
+#pragma unroll
+      for (int w = 1; w < W; ++w) M = fmaxf(M, w_m[w][j]);
       float S = 0.f, O[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) O[e] = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float f = __builtin_amdgcn_exp2f(w_m[w][j] - M);
         S += w_l[w][j] * f;
 #pragma unroll
@@ -563,14 +565,20 @@ __global__ __launch_bounds__(256) void attn8_join_kernel(Attn8Args a) {
   for (int e = 0; e < E; ++e) o[lane + 64 * e] = f32_to_bf16(O[e] * inv);
 }
 
-template <int D>
-static hipError_t launch_attn8_d(const Attn8Args& a, int nc, hipStream_t st) {
+template <int D, int W>
+static void launch_split8(const Attn8Args& a, int nc, hipStream_t st) {
   const dim3 grid((unsigned)(a.hkv * a.col_tiles), (unsigned)a.max_splits);
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a); };
-  if (nc == 1) go(attn8_split_kernel<D, 1, D == 64 ? 2 : 1>);
-  else if (nc == 2) go(attn8_split_kernel<D, 2, 1>);
-  else if (nc == 3) go(attn8_split_kernel<D, 3, 1>);
-  else go(attn8_split_kernel<D, 4, 1>);
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(64 * W), 0, st, a); };
+  if (nc == 1) go(attn8_split_kernel<D, 1, D == 64 ? 2 : 1, W>);
+  else if (nc == 2) go(attn8_split_kernel<D, 2, 1, W>);
+  else if (nc == 3) go(attn8_split_kernel<D, 3, 1, W>);
+  else go(attn8_split_kernel<D, 4, 1, W>);
+}
+
+template <int D>
+static hipError_t launch_attn8_d(const Attn8Args& a, const Attn8Plan& p, hipStream_t st) {
+  if (p.waves == 8) launch_split8<D, 8>(a, p.nc, st);
+  else launch_split8<D, 4>(a, p.nc, st);
   hipError_t e = hipGetLastError();
   // pages that one split holds: every candidate has one, nothing to join
   if (e != hipSuccess || a.max_pages <= a.min_chunk) return e;
@@ -596,9 +604,13 @@ Attn8Plan plan_attn8(int n, int hq, int hkv, int d, int tokens, int max_pages) {
   p.rounds = std::max(kAttn8Rounds * 256 / per, 1);
   // A join costs 5 us of the GPU and a launch: short candidates are one split, longer ones too where
   // they fill the CUs (splits / one, us among others: 4 candidates of 512-1024 keys, 8 heads, 13.8 /
-  // 12.0, of 768-1536 13.4 / 16.2; 64 of 1280-2560 53 / 46, 64 of 256-4096 with 4 heads 33 / 39).
+  // 12.0, of 768-1536, in a graph, 9.5 / 11.5; 64 of 1280-2560 53 / 46, 64 of 256-4096 with 4 heads 33 / 39).
   const bool one = max_pages <= ((long long)n * per >= 256 ? kAttn8OneSplitMany : kAttn8OneSplit);
   p.min_chunk = one ? max_pages : kAttn8MinChunk;
+  // A workgroup that has its CU to itself takes eight waves (four / eight, us in a graph, 32 heads on 8:
+  // 4 candidates of 512-1024 keys 11.1 / 9.5, 16 12.3 / 10.5, of 4 tokens each 12.1 / 10.5;
+  // sixteen waves 10.7, 12.0).
+  p.waves = one && (long long)n * per <= 256 ? 8 : 4;
   const long long most = (long long)n * ((max_pages + p.min_chunk - 1) / p.min_chunk);
   const long long s = (long long)std::max(p.one_round, p.rounds) + n;
   p.max_splits = s < most ? s : most;
@@ -606,7 +618,7 @@ Attn8Plan plan_attn8(int n, int hq, int hkv, int d, int tokens, int max_pages) {
 }
 
 hipError_t launch_attn8(const Attn8Args& a, const Attn8Plan& p, hipStream_t st) {
-  return a.d == 128 ? launch_attn8_d<128>(a, p.nc, st) : launch_attn8_d<64>(a, p.nc, st);
+  return a.d == 128 ? launch_attn8_d<128>(a, p, st) : launch_attn8_d<64>(a, p, st);
 }
 
 }  // namespace sevo

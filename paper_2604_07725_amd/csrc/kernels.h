@@ -314,6 +314,7 @@ struct Attn8Plan {
   int one_round;      // splits aimed at, over all candidates: all resident at once
   int rounds;         // in several rounds
   int min_chunk;      // pages of a split, at least; max_pages: every candidate has one
+  int waves;          // of a workgroup
   long long max_splits;
 };
 Attn8Plan plan_attn8(int n, int hq, int hkv, int d, int tokens, int max_pages);
