@@ -445,6 +445,10 @@ __global__ __launch_bounds__(256, 4) void verify_rest_kernel(VerifyArgs a) {
   }
   if (d.taken == d.count) return;
   const RowSum t = L.row[d.taken], q = L.row[kVerifyMaxDrafts + 1 + d.taken];
+  if (!fine(t.sum) || !fine(q.sum)) {  // no difference of distributions
+    if (chunk < a.chunks && (threadIdx.x & 63) == 0) a.rest_sum[(size_t)i * a.chunks + chunk] = 0.0;
+    return;
+  }
   const float* tr = row_ptr(a, target_row(a, i, d.taken));
   const float* dr = row_ptr(a, draft_row(a, i, d.taken));
   const int v0 = chunk * kVerifyChunk + (threadIdx.x & 63) * 4;
