@@ -354,6 +354,69 @@ def test_attention_many_candidates(sevo):
     assert (far.float() - o.float()).abs().max() <= 2.0 ** -6 * o.abs().max()
 
 
+@pytest.mark.parametrize("hq,hkv,d,T", [(8, 8, 128, 1), (16, 8, 128, 9), (32, 8, 128, 9), (64, 8, 64, 7)])
+def test_attention_many_short_candidates(sevo, hq, hkv, d, T):
+    """More workgroups than the chip has units, one per candidate and head."""
+    g = gen(hq + T)
+    lens = [int(x) for x in torch.randint(1, 130, (40,), generator=g)]
+    pool, table, g = cache(lens, hkv, d, seed=T)
+    q = torch.randn(40, T, hq, d, generator=g).to(BF)
+    check_attention(sevo, pool, table, lens, q, [min(T, x) for x in lens])
+
+
+@pytest.mark.parametrize("width", [40, 300])
+def test_attention_in_graphs_with_other_lengths(sevo, width):
+    """Captured with some lengths, replayed with others, pages and queries too; two graphs on one
+    workspace, one after the other."""
+    hkv, d, T = 2, 128, 3
+    pool, table, g = cache([640] * 4, hkv, d, seed=11, max_pages=width)
+    pool = pool.to(DEV)
+    need = max(16, sevo.sevo_attn_fp8_workspace_bytes(4, T, 8, hkv, d, width))
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    sets = []
+    for lens in ([640, 3, 0, 97], [16, 620, 320, 1], [0, 0, 0, 640]):
+        sets.append([torch.randn(4, T, 8, d, generator=g).to(BF).to(DEV), table[torch.randperm(4, generator=g)].to(DEV),
+                     torch.tensor(lens, dtype=torch.int32, device=DEV),
+                     torch.tensor([min(T, x) for x in lens], dtype=torch.int32, device=DEV)])
+    call = lambda x, **k: sevo.sevo_attn_decode_fp8(x[0], pool, x[1], x[2], q_lens=x[3], **k)
+    want = [call(x).clone() for x in sets]
+    held = [[t.clone() for t in x] for x in sets[:2]]
+    outs = [torch.zeros_like(want[0]) for _ in held]
+    torch.cuda.synchronize()
+    graphs = []
+    for x, o in zip(held, outs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(x, out=o, workspace=ws)
+        graphs.append(graph)
+    for rep in range(3):
+        for k in range(2):
+            x = sets[(rep + k) % 3]
+            for t, v in zip(held[k], x):
+                t.copy_(v)
+            outs[k].zero_()                            # (rows past the new tokens stay as they were)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert torch.equal(outs[k], want[(rep + k) % 3])
+        assert torch.equal(call(sets[rep]), want[rep])
+
+
+def test_attention_on_two_streams_at_once(sevo):
+    pool, table, g = cache([3000, 40, 1500], 2, 128, seed=12, max_pages=400)
+    pool, table = pool.to(DEV), table.to(DEV)
+    lens = torch.tensor([3000, 40, 1500], dtype=torch.int32, device=DEV)
+    qs = [torch.randn(3, 8, 128, generator=g).to(BF).to(DEV) for _ in range(2)]
+    want = [sevo.sevo_attn_decode_fp8(q, pool, table, lens).clone() for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    got = [[sevo.sevo_attn_decode_fp8(q, pool, table, lens, stream=s) for _ in range(20)] for q, s in zip(qs, streams)]
+    torch.cuda.synchronize()
+    for w, o in zip(want, got):
+        assert all(torch.equal(x, w) for x in o)
+
+
 @pytest.mark.parametrize("d,T", [(64, 1), (128, 1), (128, 4)])
 def test_attention_garbage_and_bad_pages(sevo, d, T):
     """What lies behind the last key, or in pages outside the pool, does not enter."""

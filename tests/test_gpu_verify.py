@@ -192,3 +192,40 @@ def test_without_drafts_it_is_a_sample(sevo):
         assert [int(b[0]), float(b[1])] == [int(a[0][i]), float(a[1][i])]
     with pytest.raises(sevo.SevoError):
         sevo.sevo_verify_drafts(buf[:, None], none, u, 1.0)       # rows 1030 apart: no multiple of 4
+
+
+@pytest.mark.parametrize("dist", [False, True])
+def test_in_graphs_with_other_rows(sevo, dist):
+    """Captured once, replayed with other logits, drafts, counts and uniform numbers; two graphs on one
+    workspace."""
+    g = gen(13)
+    n, T, v = 5, 3, 9001
+    ws = torch.empty(sevo.sevo_verify_workspace_bytes(n, T, v), dtype=torch.uint8, device=DEV)
+    sets = []
+    for _ in range(3):
+        z, y = rows(n, T + 1, v, g), rows(n, T, v, g)
+        x = z[:, :T].argmax(2).to(torch.int32)
+        x[0] = torch.randint(0, v, (T,), generator=g).to(torch.int32)
+        sets.append([padded(z), padded(y), x.to(DEV), torch.rand(n, T + 1, generator=g).to(DEV),
+                     torch.randint(0, T + 2, (n,), generator=g).to(torch.int32).to(DEV)])
+    def call(s, **k):
+        return sevo.sevo_verify_drafts(s[0], s[2], s[3], 0.9, draft_logits=s[1] if dist else None, n_drafts=s[4], vocab=v, **k)
+    want = [[t.clone() for t in call(s)] for s in sets]
+    held = [[t.clone() for t in s] for s in sets[:2]]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for s in held:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(call(s, workspace=ws))
+        graphs.append(graph)
+    for rep in range(3):
+        for k in range(2):
+            for t, x in zip(held[k], sets[(rep + k) % 3]):
+                t.copy_(x)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(outs[k], want[(rep + k) % 3]))
+        assert all(torch.equal(a, b) for a, b in zip(call(sets[rep]), want[rep]))
