@@ -127,8 +127,8 @@ __device__ __forceinline__ double log2_scale(const VerifyArgs& a) {
 // The sums' exponential, factor * 2^(d c): factor * 2^(k / 256) from a table in LDS, times a degree-4
 // polynomial on [-1/512, 1/512] (5e-18 relative), scaled by 2^n in the table entry's exponent.
 // 256 entries make the index one instruction (a byte's shift): 64 candidates 97 -> 95 us.
-// d at most 0; what is more than 2^900 below 1, also a -inf (and a NaN), is taken for 2^-900
-// (a factor of 2^-24 at least then stays a normal number).
+// d at most 0; what is more than 2^reach below 1, also a -inf (and a NaN), is taken for 2^-reach
+// (factor 2^-reach has to be a normal number).
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 struct Exp2Steps {  // 2^(j / 256), from exp's series
   double v[256];
@@ -152,7 +152,7 @@ __device__ __forceinline__ void make_table(ExpTable& T, double step, double fact
 }
 struct ExpScale {
   double c256, least;
-  __device__ __forceinline__ explicit ExpScale(double c) : c256(256.0 * c), least(-900.0 / c) {}
+  __device__ __forceinline__ ExpScale(double c, double reach) : c256(256.0 * c), least(-reach / c) {}
 };
 __device__ __forceinline__ void exp_parts(const ExpTable& T, const ExpScale& E, double d, double& poly,
                                           double& entry) {
@@ -169,6 +169,23 @@ __device__ __forceinline__ void exp_parts(const ExpTable& T, const ExpScale& E, 
   poly = __builtin_fma(y, r, 1.0);
   b.y += (uint32_t)k << 12;
   entry = __builtin_bit_cast(double, b);
+}
+
+// max(p - q, 0) of an entry, dz and dy its logits less their rows' largest, P and Q tables with the factors
+// kShareUnit / the rows' sums.  Times 2^120 every share that float64 holds (2^-1074 and more of the mass, as a
+// subnormal number) is a normal number, and what stands for less (2^-980 and below, kShareReach) is told from it:
+// up to kNoShare, half the least share, nothing is left.  A -inf or a mask of the lowest number thus weighs
+// nothing, in both kernels alike: the second sums what the third walks through, so a chunk
+// with a sum has an entry with a weight.
+constexpr double kShareUnit = 0x1p120, kShareReach = 1100.0, kNoShare = 0x1p-955;
+__device__ __forceinline__ double share_left(const ExpTable& P, const ExpTable& Q, const ExpScale& E,
+                                             double dz, double dy) {
+  // no multiply-add into the difference: of equal rows nothing is left
+#pragma clang fp contract(off)
+  double pp, pe, qp, qe;
+  exp_parts(P, E, dz, pp, pe);
+  exp_parts(Q, E, dy, qp, qe);
+  return pp * pe - qp * qe;
 }
 
 }  // namespace
@@ -212,7 +229,7 @@ __global__ __launch_bounds__(256, 6) void verify_rows_kernel(VerifyArgs a) {
 #pragma unroll
   for (int j = 0; j < J; ++j) m = fmaxf(fmaxf(fmaxf(m, z[j].x), fmaxf(z[j].y, z[j].z)), z[j].w);
   m = wave_max(m);
-  const ExpScale E(log2_scale(a));
+  const ExpScale E(log2_scale(a), 900.0);
   const double md = m;
   double sum = 0.0;
   bool none = m == INFINITY;  // a NaN or a +inf: no distribution
@@ -297,8 +314,14 @@ __device__ __forceinline__ RowSum join_row(const VerifyArgs& a, size_t row,
 // a sum that a distribution can have: not of a row with a NaN, a +inf or nothing above -inf
 __device__ __forceinline__ bool fine(double s) { return s > 0.0 && s < INFINITY; }
 
+// an entry's share of the row's largest one (c: log2_scale; no multiply-add, so that it is the same bits wherever
+// it is computed)
+__device__ __forceinline__ double share(float z, double largest, double c) {
+#pragma clang fp contract(off)
+  return exp2d(((double)z - largest) * c);
+}
 __device__ __forceinline__ double prob(const VerifyArgs& a, const RowSum& r, float z) {
-  return exp2d(((double)z - (double)r.max) * log2_scale(a)) / r.sum;
+  return share(z, r.max, log2_scale(a)) / r.sum;
 }
 
 // The sums of candidate i's rows into LDS, and how many drafts are accepted.  All threads: 16 lanes
@@ -354,29 +377,18 @@ __device__ __forceinline__ Decision decide(const VerifyArgs& a, int i, VerifyLds
   return Decision{L.taken, count};
 }
 
-// The weights that the next token is drawn from, at entries v .. v + 3: max(p - q, 0), or without a
-// draft distribution p times the row's sum (the scale does not matter, and the sums of a flat
-// row are exact), there with or without the rejected draft
+// The weights that the next token is drawn from, at entries v .. v + 3, where no draft distribution is
+// taken off: p times the row's sum (the scale does not matter, and the sums of a flat row are exact), there
+// with or without the rejected draft
 struct Weights {
   const float* target;
-  const float* draft;  // null: none
-  double mt, inv_t, md, inv_d, c;
+  double mt, c;
   int without;  // -1: none
   int vocab;
   __device__ __forceinline__ void at(int v, double (&o)[4]) const {
-    // no multiply-add here: with a rounded product on either side, of equal rows nothing is left
-#pragma clang fp contract(off)
     const f32x4 z = row4(target, v, vocab);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = exp2d(((double)z[k] - mt) * c) * inv_t;
-    if (draft) {
-      const f32x4 y = row4(draft, v, vocab);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const double d = o[k] - exp2d(((double)y[k] - md) * c) * inv_d;
-        o[k] = v + k < vocab && !(d < 0.0) ? d : 0.0;  // a NaN stays one
-      }
-    }
+    for (int k = 0; k < 4; ++k) o[k] = share(z[k], mt, c);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (v + k == without) o[k] = 0.0;
@@ -385,30 +397,28 @@ struct Weights {
 
 __device__ __forceinline__ Weights weights(const VerifyArgs& a, int i, const Decision& d,
                                            const VerifyLds& L, bool residual) {
-  const RowSum t = L.row[d.taken];
   Weights w;
   w.target = row_ptr(a, target_row(a, i, d.taken));
-  w.draft = nullptr;
-  w.mt = t.max;
-  w.inv_t = 1.0;
-  w.md = 0.0;
-  w.inv_d = 1.0;
+  w.mt = L.row[d.taken].max;
   w.c = log2_scale(a);
-  w.without = -1;
+  w.without = residual ? a.draft_tokens[(size_t)i * a.drafts + d.taken] : -1;
   w.vocab = a.vocab;
-  if (residual && d.taken < d.count) {
-    if (a.draft_logits) {
-      const RowSum q = L.row[kVerifyMaxDrafts + 1 + d.taken];
-      w.inv_t = 1.0 / t.sum;
-      w.draft = row_ptr(a, draft_row(a, i, d.taken));
-      w.md = q.max;
-      w.inv_d = 1.0 / q.sum;
-    } else {
-      w.without = a.draft_tokens[(size_t)i * a.drafts + d.taken];
-    }
-  }
   return w;
 }
+
+// and where it is: max(p - q, 0) of the row behind the accepted drafts
+struct Residual {
+  const float* target;
+  const float* draft;
+  double mt, md;
+  ExpScale E;
+  __device__ __forceinline__ Residual(const VerifyArgs& a, int i, const Decision& d, const VerifyLds& L)
+      : target(row_ptr(a, target_row(a, i, d.taken))),
+        draft(row_ptr(a, draft_row(a, i, d.taken))),
+        mt(L.row[d.taken].max),
+        md(L.row[kVerifyMaxDrafts + 1 + d.taken].max),
+        E(log2_scale(a), kShareReach) {}
+};
 
 // sum of a chunk's weights over the workgroup, every thread gets it
 __device__ __forceinline__ double chunk_sum(const Weights& W, int chunk, double* red) {
@@ -449,46 +459,37 @@ __global__ __launch_bounds__(256, 4) void verify_rest_kernel(VerifyArgs a) {
     if (chunk < a.chunks && (threadIdx.x & 63) == 0) a.rest_sum[(size_t)i * a.chunks + chunk] = 0.0;
     return;
   }
-  const float* tr = row_ptr(a, target_row(a, i, d.taken));
-  const float* dr = row_ptr(a, draft_row(a, i, d.taken));
+  const Residual R(a, i, d, L);
   const int v0 = chunk * kVerifyChunk + (threadIdx.x & 63) * 4;
   constexpr int J = kVerifyChunk / 256;
   f32x4 z[J], y[J];
   if ((chunk + 1) * kVerifyChunk <= a.vocab) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      z[j] = *reinterpret_cast<const f32x4*>(tr + v0 + 256 * j);
-      y[j] = *reinterpret_cast<const f32x4*>(dr + v0 + 256 * j);
+      z[j] = *reinterpret_cast<const f32x4*>(R.target + v0 + 256 * j);
+      y[j] = *reinterpret_cast<const f32x4*>(R.draft + v0 + 256 * j);
     }
   } else {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      z[j] = row4(tr, v0 + 256 * j, a.vocab);
-      y[j] = row4(dr, v0 + 256 * j, a.vocab);
+      z[j] = row4(R.target, v0 + 256 * j, a.vocab);
+      y[j] = row4(R.draft, v0 + 256 * j, a.vocab);
     }
   }
-  make_table(P, step, 1.0 / t.sum);
-  make_table(Q, step, 1.0 / q.sum);
+  make_table(P, step, kShareUnit / t.sum);
+  make_table(Q, step, kShareUnit / q.sum);
   __syncthreads();
   if (chunk >= a.chunks) return;
-  const ExpScale E(log2_scale(a));
-  const double mt = t.max, mq = q.max;
   double s = 0.0;
 #pragma unroll
   for (int j = 0; j < J; ++j) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      // no multiply-add into the difference: of equal rows nothing is left
-#pragma clang fp contract(off)
-      double pp, pe, qp, qe;
-      exp_parts(P, E, (double)z[j][k] - mt, pp, pe);
-      exp_parts(Q, E, (double)y[j][k] - mq, qp, qe);
-      const double r = pp * pe - qp * qe;
-      s += __builtin_fmax(r, 0.0);
-    }
+    for (int k = 0; k < 4; ++k)
+      s += __builtin_fmax(share_left(P, Q, R.E, (double)z[j][k] - R.mt, (double)y[j][k] - R.md), kNoShare);
     __builtin_amdgcn_sched_barrier(0);
   }
-  s = wave_sum64(s);
+  // (every entry added kNoShare at least; of entries that added no more exactly 0 is left)
+  s = wave_sum64(s - 4 * J * kNoShare);
   if ((threadIdx.x & 63) == 0) a.rest_sum[(size_t)i * a.chunks + chunk] = s;
 }
 
@@ -498,9 +499,11 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
   __shared__ VerifyLds L;
   __shared__ double red[4], s_pre[4];
   __shared__ double s_total, s_target, s_before;
-  __shared__ int s_chunk, s_tok, s_last;
+  __shared__ int s_chunk, s_tok;
+  __shared__ ExpTable P, Q;
   const int i = blockIdx.x;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const double step = DECIDED ? kExp2Steps.v[threadIdx.x] : 0.0;
   const double point = a.uniforms[(size_t)i * (a.drafts + 1) + a.drafts];
   Decision d;
   if constexpr (DECIDED) {
@@ -514,23 +517,25 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
   }
   const RowSum row = L.row[d.taken];
   const bool valid = fine(row.sum);
-  if (threadIdx.x == 0) {
-    s_tok = valid && a.temp == 0.0 ? row.arg : -1;
-    s_last = -1;
-  }
+  if (threadIdx.x == 0) s_tok = valid && a.temp == 0.0 ? row.arg : -1;
   if (valid && a.temp != 0.0) {  // the same in every thread
     bool residual = d.taken < d.count;
-    Weights W = weights(a, i, d, L, true);
+    Weights W = weights(a, i, d, L, residual && !DECIDED);
+    if constexpr (DECIDED)
+      if (residual) {  // (tables of a row that is no distribution are not used: the second kernel's sums are 0)
+        make_table(P, step, kShareUnit / row.sum);
+        make_table(Q, step, kShareUnit / L.row[kVerifyMaxDrafts + 1 + d.taken].sum);
+      }
     const size_t prow = target_row(a, i, d.taken) * a.chunks;
     // the chunk without the rejected draft: summed again, a difference would lose the digits of what is left
     double left = 0.0;
     const int hole = W.without >= 0 && W.without < a.vocab ? W.without / kVerifyChunk : -1;
     if (hole >= 0) left = chunk_sum(W, hole, red);
     auto weight_of = [&](int k) -> double {
-      if (residual && a.draft_logits) return a.rest_sum[(size_t)i * a.chunks + k];
+      if (DECIDED && residual) return a.rest_sum[(size_t)i * a.chunks + k];
       if (residual && k == hole) return left;
       const VerifyPart p = a.parts[prow + k];
-      return p.sum * exp2d(((double)p.max - (double)row.max) * W.c);
+      return p.sum * share(p.max, row.max, W.c);
     };
     for (int pass = 0;; ++pass) {
       // wave 0: total, then the first chunk whose running sum passes the drawn point
@@ -572,8 +577,7 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
         }
       }
       __syncthreads();
-      // (far below any rounding of the differences: nothing but shares of 2^-900)
-      const bool good = s_total > 1e-250 && s_total < INFINITY;
+      const bool good = s_total > 0.0 && s_total < INFINITY;
       if (good || !residual) break;
       // nothing left of the residual: the target's own distribution
       residual = false;
@@ -587,7 +591,17 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a) {
 #pragma unroll
       for (int j = 0; j < kPer / 4; ++j) {
         double q[4];
-        W.at(v0 + 4 * j, q);
+        if (DECIDED && residual) {
+          const Residual R(a, i, d, L);
+          const f32x4 z = row4(R.target, v0 + 4 * j, a.vocab), y = row4(R.draft, v0 + 4 * j, a.vocab);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const double r = share_left(P, Q, R.E, (double)z[k] - R.mt, (double)y[k] - R.md);
+            q[k] = r > kNoShare ? r : 0.0;
+          }
+        } else {
+          W.at(v0 + 4 * j, q);
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           o[4 * j + k] = q[k];
