@@ -29,6 +29,7 @@
 // loop is bound by instructions: a wave issues one vector instruction in 8 clocks, and registers
 // leave two waves a SIMD.
 #include <algorithm>
+#include <limits>
 
 #include "kernels.h"
 #include "kv8.h"
@@ -134,8 +135,9 @@ __device__ __forceinline__ Split find_split(const Attn8Args& a, int flat) {
 __device__ __forceinline__ int token_of(const Attn8Args& a, int cc) {
   return (int)(((float)cc + 0.5f) * a.inv_group);
 }
-// running maxima start here: finite, so that what a column has not seen needs no case of its own
-constexpr float kNoScore = -3e38f;
+// running maxima start here: finite, so that what a column has not seen needs no case of its own, and at most
+// any finite score
+constexpr float kNoScore = -std::numeric_limits<float>::max();
 
 // Waves per SIMD that the registers of NC column tiles leave room for.  At d = 128 two tiles fit three
 // times with q in LDS and one tile's probabilities at a time (16 candidates of 8k-16k keys, 5 tokens of 32
