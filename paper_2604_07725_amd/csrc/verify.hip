@@ -337,7 +337,7 @@ __device__ __forceinline__ Decision decide(const VerifyArgs& a, int i, VerifyLds
     x = a.draft_tokens[(size_t)i * a.drafts + lane];
     u = a.uniforms[(size_t)i * (a.drafts + 1) + lane];
   }
-  // (rows behind the last draft are joined too, and not looked at)
+  // (partials of rows behind the last draft are joined too, whatever they hold, and not looked at)
   const int count = drafts_of(a, i);
   auto row_of = [&](int r) {
     return r <= a.drafts ? target_row(a, i, r) : draft_row(a, i, r - a.drafts - 1);
@@ -346,7 +346,8 @@ __device__ __forceinline__ Decision decide(const VerifyArgs& a, int i, VerifyLds
   VerifyPart v[kPartsAhead];
   if (r < rows) load_parts(a, row_of(r), v);
   float zx = 0.f, yx = 0.f;
-  const bool known = x >= 0 && x < a.vocab;
+  // (rows behind the last draft may not be there)
+  const bool known = lane < count && x >= 0 && x < a.vocab;
   if (known) {
     zx = row_ptr(a, target_row(a, i, lane))[x];
     if (dist) yx = row_ptr(a, draft_row(a, i, lane))[x];
