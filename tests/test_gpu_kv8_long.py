@@ -43,7 +43,7 @@ def attention(q, pool, table, length, m, scale, heads):
         K = (k * ks[..., None]).reshape(-1, d)
         V = (v * vs[..., None]).reshape(-1, d)
         for t in range(T):
-            seen = slot[:length - m + t + 1]
+            seen = slot[:max(0, length - m + t + 1)]
             count = torch.bincount(seen[seen >= 0], minlength=K.shape[0]).double()
             qh = q[t, c * G:(c + 1) * G].double().to(pool.device)
             z = torch.mm(K, qh.t().contiguous()) * scale                     # [slots, G]
