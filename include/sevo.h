@@ -751,8 +751,9 @@ sevo_status sevo_moe_linear_fp8(const sevo_moe_linear_fp8_args* a, void* stream)
  *     V codes   16 head_dim bytes further, element (s, e) at (e/64)*1024 + (s/4)*256
  *               + (e%16)*16 + ((e/16)%4)*4 + s%4
  *     scales    32 head_dim bytes in: fp32 [16] of K, then fp32 [16] of V, one a slot
- * A block is the head_dim values y of one token and head: scale = max(max |y| / 448,
- * 2^-64), code = y times the fp32 reciprocal of the scale, rounded to nearest even.  A
+ * A block is the head_dim values y of one token and head: scale = max(max |y| r, 2^-64),
+ * r = 1 / 448 rounded to fp32, code = y times the fp32 reciprocal of the scale, rounded to
+ * nearest even.  A
  * block that holds a NaN or an infinity gets the scale NaN and the codes 0: whoever sees
  * the token gets a NaN, whoever does not is left alone.
  * head_dim 64 or 128 (else UNSUPPORTED).  Here and below, arrays of int32 and of single fp32

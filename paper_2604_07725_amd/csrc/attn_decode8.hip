@@ -16,16 +16,16 @@
 //   QK   S = K Q^T, 16x16x32 matrix instructions: rows = the page's tokens, columns = 16 query
 //        rows.  Lane (column l % 16, g = l / 16) gets the scores of tokens 4 g .. + 3 of either page.
 //   PV   O^T = V^T P^T: the 32-deep axis is the pair's tokens in the order in which the lanes hold
-//        their scores, so p needs no exchange.  p vs is split into two bf16 parts, hi + lo
-//        (to 2^-17 of itself): the probabilities keep their 32-bit accuracy.
+//        their scores, so p needs no exchange.  p vs is split into two bf16 parts, hi + lo:
+//        2^-17 of itself is lost (of one part 2^-8, as much as the output's own rounding loses).
 // More than 16 query rows per kv head are further column tiles of the same page (NC), so
 // the cache is read once for all new tokens.
 //
 // What bounds it: HBM for one token a candidate (16 flop a byte at 8 heads a kv head).  64
 // candidates of 16k-32k keys, 8 x 128 heads, 3.32 GB: 512-528 us, 6.3-6.5 TB/s, what the read probe
 // reaches; one candidate of 65537 keys, 138 MB: 30 us, of them 18 in the loop, the rest
-// the two launches, the way to the first page (lengths, page ids, page: three memory latencies) and
-// the join.  With 40 query rows (5 tokens of 8 heads; 16 candidates of 8k-16k keys, 209 MB, 48 us) the
+// the two launches, the way to the first page (lengths, page ids, page: three memory latencies), workgroups
+// without a split (the launch has 257 rows of them, the most of either plan below; 94 find one) and the join.  With 40 query rows (5 tokens of 8 heads; 16 candidates of 8k-16k keys, 209 MB, 48 us) the
 // loop is bound by instructions: a wave issues one vector instruction in 8 clocks, and registers
 // leave two waves a SIMD.
 #include <algorithm>
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(64 * W, W == 4 ? waves8(D, NC) : 2) void attn8_spli
           }
           hi[e / 2] = pack_bf16x2(p[0], p[1]);
           asm("" : "+v"(hi[e / 2]));  // (else it is converted once more for what follows)
-          // p less its rounded value, exact, as a dot product with (-1, 0) and (0, -1)
+          // (p less its rounded value is exact)
           lo[e / 2] = pack_bf16x2(p[0] - bf16_lo(hi[e / 2]), p[1] - bf16_hi(hi[e / 2]));
         }
         ph[t - t0] = __builtin_bit_cast(bf16x8v, u32x4{hi[0], hi[1], hi[2], hi[3]});

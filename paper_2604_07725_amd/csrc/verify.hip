@@ -8,7 +8,8 @@
 //
 // A choice is a comparison of sums over the whole vocabulary: one entry of 150 thousand differs
 // from its neighbour by 1e-6 of the mass and less, so a sum in 32 bits would move
-// choices.  Exponentials and sums are in 64 bits throughout (3e-15 relative an entry at most).
+// choices.  Exponentials and sums are in 64 bits throughout (an entry x nats below its row's largest is off by
+// (4 x + 6) 1e-16 of itself at most, that is 6e-16 of the largest: log2 e / T and its product are rounded).
 // Three kernels (us: 64 candidates with 4 drafts and their distributions, 151936 entries, 350 MB):
 //   1. per (row, 2048 entries): the largest logit and the sum of exponentials relative to it (57
 //      to 64; 51 are the floor of its reads: the vector ALU, 14 operations an entry and 5 for the
